@@ -425,6 +425,160 @@ sp_status sp_assemble(const int32_t *target_ids_dev, int64_t M,
                       int64_t *out_src_dev, int64_t *out_len_dev,
                       void *ws_dev, size_t ws_bytes, void *hip_stream);
 
+/* ---- the draft model's forward pass around the importance pass ----
+ *
+ * What sp_score reads is left behind by a draft model's forward pass: the cache
+ * of the prompt's keys and the lookahead rows' queries (Algorithm 1,
+ * ForwardWithAttn). The calls below are that pass's work on the cache and on the
+ * logits, one decoder layer at a time: new keys and values go into a paged
+ * cache (sp_cache_append), queries attend over it (sp_attend), and the next
+ * token and the probabilities of given ones are read off the logits
+ * (sp_logprobs). A bf16 cache with pages of a multiple of 512 tokens is what
+ * sp_score_paged reads afterwards.
+ */
+
+/* How a paged cache holds its elements. SP_CACHE_BF16: as they are.
+ * SP_CACHE_E4M3: OCP E4M3 codes, one byte each, with one float scale for every
+ * SP_CACHE_BLOCK consecutive tokens of a page and kv head: value = scale * E4M3(code). */
+typedef enum { SP_CACHE_BF16 = 0, SP_CACHE_E4M3 = 1 } sp_cache_type;
+#define SP_CACHE_BLOCK 32
+
+/* A layer's paged cache: two pools (keys, values) of n_pages pages each with the
+ * same strides, in elements, head_dim contiguous:
+ *   K[b, kv, j, e] = k_pool[ page * page_stride + kv * stride_head
+ *                            + (j % page_tokens) * stride_token + e ],
+ *   page = block_table_dev[b * table_stride + j / page_tokens]
+ * block_table_dev: device, int32; table_stride entries for each request. E4M3
+ * pools come with dense float scale arrays
+ * [n_pages][n_kv_heads][page_tokens / SP_CACHE_BLOCK] (k_scale, v_scale; null for
+ * bf16). Pools, queries, keys and values are 16-byte aligned. Query head h reads
+ * kv head h / (n_q_heads / n_kv_heads).
+ * Supported: head_dim 64 or 128; n_q_heads a multiple of n_kv_heads with ratio
+ * G <= 16; n_kv_heads <= 4096; page_tokens a positive multiple of SP_CACHE_BLOCK, at most
+ * 2^24; strides multiples of 16 (E4M3) or 8 (bf16) elements, stride_token >=
+ * head_dim, none above 2^40; 1 <= n_pages < 2^31. */
+typedef struct {
+    int32_t n_q_heads;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t cache_type;       /* sp_cache_type */
+    int64_t n_pages;
+    int64_t page_tokens;
+    int64_t page_stride;
+    int64_t stride_head;
+    int64_t stride_token;
+} sp_cache_desc;
+
+/* Pairs that the rotation turns: SP_ROTATE_HALF elements (i, i + rot_dim/2),
+ * SP_ROTATE_PAIRS elements (2i, 2i + 1); i in [0, rot_dim/2). */
+typedef enum { SP_ROTATE_HALF = 0, SP_ROTATE_PAIRS = 1 } sp_rotate_style;
+
+/*
+ * Appends the keys and values of new tokens to a paged cache and rotates keys and
+ * (optionally) queries to their positions on the way. Request b brings tokens
+ * [offsets[b], offsets[b+1]) of the packed inputs (offsets in host and in device
+ * memory, the same B+1 non-decreasing values, offsets[0] == 0; 0 <= B <= 4096,
+ * requests without new tokens are allowed, fewer than 2^31 new tokens in all).
+ * Its i-th new token becomes token start_dev[b] + i of its cache.
+ *  - k_dev, v_dev: bf16, token t at t * k_stride (v_stride), n_kv_heads * head_dim
+ *    contiguous elements each; strides in elements, multiples of 8 (so keys, values and
+ *    queries can be parts of one projection's output);
+ *  - q_dev, q_out_dev: optional (both or neither): bf16 queries, n_q_heads * head_dim
+ *    contiguous elements a token at t * q_stride, and dense bf16
+ *    [tokens][n_q_heads][head_dim] for the rotated ones. q_out_dev may be q_dev if that is dense.
+ *  - rot_dim: rotated elements of each head, 0 (no rotation) or a multiple of 16 up to
+ *    head_dim; with c = cos_dev[p][i], s = sin_dev[p][i] (float, [n_pos][rot_dim/2],
+ *    16-byte aligned) the pair (x, y) of index i becomes (x c - y s, y c + x s), products and
+ *    sums rounded to float one by one. p = positions_dev[t] (device, int32, one for each packed
+ *    token), or without it (null) the token's index in its cache; p is clamped to [0, n_pos).
+ *  - bf16 caches take the result rounded to nearest. E4M3 caches: of the tokens of one block
+ *    of SP_CACHE_BLOCK slots and kv head that this call brings, the largest magnitude m gives
+ *    the smallest power of two s >= 2^-64 with m <= 448 s; a block that already holds tokens
+ *    before start_dev[b] keeps the larger of s and its present scale, and the codes of those
+ *    tokens are brought to it (exactly, but for values that fall among E4M3's subnormals); new codes
+ *    are E4M3(x / s), rounded to nearest. Results that are not finite are stored as NaN
+ *    codes and do not count for m.
+ * Slots at and behind start + new tokens are not touched, except that a new token may lie in a
+ * slot that is in use: then it is replaced (a rejected lookahead token), and with it
+ * whatever follows it in its block. Tokens whose slot lies beyond the block table's row, or whose page is not
+ * in [0, n_pages), are not stored (their queries are still rotated). Two requests
+ * of one call must not append to the same page's same block.
+ */
+sp_status sp_cache_append(const sp_cache_desc *desc, const void *k_dev, int64_t k_stride,
+                          const void *v_dev, int64_t v_stride, const void *q_dev,
+                          int64_t q_stride, void *q_out_dev, const int64_t *offsets_host,
+                          const int64_t *offsets_dev, int32_t B, const int32_t *start_dev,
+                          const int32_t *positions_dev, const int32_t *block_table_dev,
+                          int64_t table_stride, const float *cos_dev, const float *sin_dev,
+                          int64_t n_pos, int32_t rot_dim, int32_t rot_style,
+                          void *k_pool_dev, void *v_pool_dev, float *k_scale_dev,
+                          float *v_scale_dev, void *hip_stream);
+
+/* Bytes of workspace sp_attend needs for these queries and contexts of at most
+ * max_len tokens (0 where it needs none). */
+sp_status sp_attend_workspace(const sp_cache_desc *desc, const int64_t *offsets_host,
+                              int32_t B, int64_t max_len, size_t *bytes);
+
+/*
+ * Attention of ragged queries over a paged cache. Request b has query rows
+ * [offsets[b], offsets[b+1]) (n_b of them; offsets as in sp_cache_append) of q_dev, dense
+ * bf16 [rows][n_q_heads][head_dim], and a context of lens_dev[b] tokens (device, int32),
+ * which normally counts the new tokens that were appended before. Row r of request b
+ * sees key j iff j < lens[b] and, with causal = 1, j <= p and (window = 0 or
+ * j > p - window), where p = lens[b] - n_b + r is the row's own token. With
+ * causal = 0 the window must be 0.
+ *   out_dev[row, h] = sum_j p_j V[b, h/G, j],  p_j = softmax_j( scale * <q, K[b, h/G, j]> )
+ * as dense bf16 [rows][n_q_heads][head_dim], and lse_dev[row, h] (float, optional) the natural
+ * logarithm of the softmax's denominator. A row that sees no key gets zeros and an lse
+ * of minus infinity. Keys and values outside what a row sees (slots of a last page past the
+ * context among them) may hold anything, NaN included.
+ * max_len bounds the contexts from the host's side (a longer lens[b] counts as
+ * max_len, a negative one as 0) and must not exceed table_stride * page_tokens; the call reads the table entries
+ * of the tokens below lens[b] only. E4M3 scales should be the powers of two that
+ * sp_cache_append writes: a scale that is not one costs another rounding to bf16 for each element.
+ * The probabilities of the second product are rounded to bf16; sums and statistics are held in fp32. The
+ * result does not change from call to call on the same inputs. scale: finite and > 0.
+ */
+sp_status sp_attend(const sp_cache_desc *desc, const void *q_dev,
+                    const int64_t *offsets_host, const int64_t *offsets_dev, int32_t B,
+                    const int32_t *lens_dev, int64_t max_len,
+                    const int32_t *block_table_dev, int64_t table_stride,
+                    const void *k_pool_dev, const void *v_pool_dev,
+                    const float *k_scale_dev, const float *v_scale_dev, float scale,
+                    int32_t causal, int64_t window, void *out_dev, float *lse_dev,
+                    void *ws_dev, size_t ws_bytes, void *hip_stream);
+
+/* Type of logits. */
+typedef enum { SP_LOGITS_F32 = 0, SP_LOGITS_BF16 = 1 } sp_logits_type;
+
+/* Largest number of alternatives sp_logprobs reports. */
+#define SP_LOGPROBS_MAX_TOP 32
+
+/* Bytes of workspace sp_logprobs needs (0 where it needs none). */
+sp_status sp_logprobs_workspace(int64_t n_rows, int64_t vocab, int32_t n_top, size_t *bytes);
+
+/*
+ * Log probabilities of rows of logits x (dtype an sp_logits_type, row r at r * row_stride
+ * elements, vocab of them; row_stride >= vocab; only element alignment is needed).
+ * With lse = log sum_v exp(x_v), lp_v = x_v - lse and p_v = exp(lp_v):
+ *  - logprob_dev[r]  = lp of token targets_dev[r] (int32; both may be null); 0 for a target
+ *    outside [0, vocab), which is how rows without one are marked;
+ *  - entropy_dev[r]  = - sum_v p_v lp_v (optional);
+ *  - top_ids_dev[r][n_top], top_logprobs_dev[r][n_top]: the n_top likeliest tokens,
+ *    likeliest first, equal logits in favour of the lower token (0 <= n_top <=
+ *    SP_LOGPROBS_MAX_TOP, n_top <= vocab; n_top = 0: both may be null). The greedy
+ *    next token is top_ids[r][0].
+ * Minus infinity marks forbidden tokens (p = 0, lp = -inf). A row of nothing else has
+ * lp = -inf throughout and entropy 0. Logits must not be NaN or plus infinity.
+ * All arithmetic is in fp32, and the result does not change from call to call.
+ * 0 <= n_rows < 2^31, 1 <= vocab < 2^31.
+ */
+sp_status sp_logprobs(const void *logits_dev, int32_t dtype, int64_t n_rows, int64_t vocab,
+                      int64_t row_stride, const int32_t *targets_dev, int32_t n_top,
+                      float *logprob_dev, float *entropy_dev, int32_t *top_ids_dev,
+                      float *top_logprobs_dev, void *ws_dev, size_t ws_bytes,
+                      void *hip_stream);
+
 /*
  * Measurement aid: streams `bytes` bytes of buf_dev (device, 16-byte aligned,
  * bytes a positive multiple of 16) with plain wide loads and XORs what it read

@@ -13,6 +13,14 @@ from typing import Optional, Sequence
 
 SP_LAYER_MEAN = 0
 SP_LAYER_MAX = 1
+SP_CACHE_BF16 = 0
+SP_CACHE_E4M3 = 1
+SP_CACHE_BLOCK = 32
+SP_ROTATE_HALF = 0
+SP_ROTATE_PAIRS = 1
+SP_LOGITS_F32 = 0
+SP_LOGITS_BF16 = 1
+SP_LOGPROBS_MAX_TOP = 32
 
 _STATUS = {1: "SP_ERR_INVALID_ARG", 2: "SP_ERR_UNSUPPORTED", 3: "SP_ERR_WORKSPACE", 4: "SP_ERR_DEVICE"}
 
@@ -24,6 +32,7 @@ EXPORTS = (
     "sp_select", "sp_select_static", "sp_select_batch_workspace", "sp_select_batch", "sp_select_budget_workspace", "sp_select_budget", "sp_project", "sp_project_batch",
     "sp_assemble_workspace", "sp_assemble", "sp_last_error", "sp_version",
     "sp_debug_fused_giveup", "sp_debug_score_path", "sp_hbm_read_probe",
+    "sp_cache_append", "sp_attend_workspace", "sp_attend", "sp_logprobs_workspace", "sp_logprobs",
 )
 
 
@@ -46,6 +55,21 @@ class ScoreDesc(ctypes.Structure):
         ("layer_agg", ctypes.c_int32),
         ("k_stride_token", ctypes.c_int64),
         ("k_stride_head", ctypes.c_int64),
+    ]
+
+
+class CacheDesc(ctypes.Structure):
+    """Mirror of ``sp_cache_desc``."""
+    _fields_ = [
+        ("n_q_heads", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("cache_type", ctypes.c_int32),
+        ("n_pages", ctypes.c_int64),
+        ("page_tokens", ctypes.c_int64),
+        ("page_stride", ctypes.c_int64),
+        ("stride_head", ctypes.c_int64),
+        ("stride_token", ctypes.c_int64),
     ]
 
 
@@ -96,6 +120,14 @@ def load_library():
     lib.sp_project.argtypes = [P, c.c_int64, P, c.c_int64, P, P, c.c_int32, P, P, P, P, P]
     lib.sp_assemble_workspace.argtypes = [c.c_int32, c.POINTER(c.c_size_t)]
     lib.sp_assemble.argtypes = [P, c.c_int64, P, P, c.c_int32, P, c.c_int32, c.c_int64, P, P, P, P, P, c.c_size_t, P]
+    CD = c.POINTER(CacheDesc)
+    lib.sp_cache_append.argtypes = [CD, P, c.c_int64, P, c.c_int64, P, c.c_int64, P, I64P, P, c.c_int32, P, P, P, c.c_int64,
+                                    P, P, c.c_int64, c.c_int32, c.c_int32, P, P, P, P, P]
+    lib.sp_attend_workspace.argtypes = [CD, I64P, c.c_int32, c.c_int64, c.POINTER(c.c_size_t)]
+    lib.sp_attend.argtypes = [CD, P, I64P, P, c.c_int32, P, c.c_int64, P, c.c_int64, P, P, P, P, c.c_float, c.c_int32,
+                              c.c_int64, P, P, P, c.c_size_t, P]
+    lib.sp_logprobs_workspace.argtypes = [c.c_int64, c.c_int64, c.c_int32, c.POINTER(c.c_size_t)]
+    lib.sp_logprobs.argtypes = [P, c.c_int32, c.c_int64, c.c_int64, c.c_int64, P, c.c_int32, P, P, P, P, P, c.c_size_t, P]
     lib.sp_hbm_read_probe.argtypes = [P, c.c_size_t, P, P]
     lib.sp_hbm_read_probe.restype = c.c_int
     lib.sp_debug_fused_giveup.argtypes = [c.c_uint32, c.c_int32]
@@ -106,7 +138,8 @@ def load_library():
     lib.sp_version.restype = c.c_char_p
     for name in ("sp_score_workspace", "sp_score", "sp_score_look", "sp_score_paged", "sp_score_fp8", "sp_score_is_fused", "sp_score_batch", "sp_select_workspace", "sp_select",
                  "sp_select_static", "sp_select_batch_workspace", "sp_select_batch", "sp_select_budget_workspace", "sp_select_budget", "sp_project",
-                 "sp_project_batch", "sp_assemble_workspace", "sp_assemble"):
+                 "sp_project_batch", "sp_assemble_workspace", "sp_assemble", "sp_cache_append", "sp_attend_workspace", "sp_attend",
+                 "sp_logprobs_workspace", "sp_logprobs"):
         getattr(lib, name).restype = c.c_int
     _lib = lib
     return lib
@@ -413,3 +446,134 @@ def sp_assemble(target_ids, M: int, tspans, n_tspans, max_spans: int, delim_ids,
                                       _ptr(out_ids, "out_ids", 4 * oc), _ptr(out_pos, "out_pos", 4 * oc),
                                       _ptr(out_src, "out_src", 8 * oc), _ptr(out_len, "out_len", 8), _ptr(ws, "ws"),
                                       nbytes, _stream(stream)))
+
+
+# ---- the draft model's forward pass: paged cache, attention over it, log probabilities ----
+
+def host_offsets(values: Sequence[int]):
+    """Offsets as the array that the library reads: made once, it saves the conversion of a list in every call."""
+    return _host_i64(values)
+
+
+def _offsets(values):
+    return values if isinstance(values, ctypes.Array) and values._type_ is ctypes.c_int64 else _host_i64(values)
+
+
+def _rows(t, what: str, rows: int, width: int, stride: Optional[int], elem: int):
+    """(address, row stride in elements) of `rows` rows of `width` contiguous elements: a tensor whose first dimension
+    counts rows and whose others are dense, or an address with its stride."""
+    if t is None:
+        return None, 0
+    if isinstance(t, int):
+        return t, width if stride is None else stride
+    if not getattr(t, "is_cuda", False):
+        raise SpError(1, f"{what} is not a device tensor")
+    shape, strides = t.shape, t.stride()
+    if not shape or shape[0] < rows or t.element_size() != elem:
+        raise SpError(1, f"{what} is {tuple(shape)} of {t.element_size()} bytes an element, the call needs {rows} rows of {elem}")
+    dense = 1
+    for n, s in zip(reversed(shape[1:]), reversed(strides[1:])):
+        if n != 1 and s != dense:
+            raise SpError(1, f"{what} is not dense within a row")
+        dense *= n
+    if dense < width:
+        raise SpError(1, f"{what} has {dense} elements a row, the call needs {width}")
+    if stride is not None and stride != strides[0] and rows > 1:
+        raise SpError(1, f"{what} has a row stride of {strides[0]}, the call says {stride}")
+    # the stride of a single row means nothing
+    return t.data_ptr(), (strides[0] if rows > 1 else max(width, 8))
+
+
+def _table(block_table, B: int, table_stride: Optional[int]):
+    """(address, entries of a request) of a dense [B][table_stride] int32 block table."""
+    if isinstance(block_table, int) or block_table is None:
+        return block_table, 0 if table_stride is None else table_stride
+    if table_stride is None:
+        if block_table.dim() != 2:
+            raise SpError(1, "block_table has to be [requests][entries]")
+        table_stride = block_table.shape[1]
+    return _ptr(block_table, "block_table", 4 * B * table_stride), table_stride
+
+
+def _pool_bytes(desc: CacheDesc) -> int:
+    elem = 1 if desc.cache_type == SP_CACHE_E4M3 else 2
+    return ((desc.n_pages - 1) * desc.page_stride + (desc.n_kv_heads - 1) * desc.stride_head
+            + (desc.page_tokens - 1) * desc.stride_token + desc.head_dim) * elem
+
+
+def _scale_bytes(desc: CacheDesc) -> int:
+    return 4 * desc.n_pages * desc.n_kv_heads * (desc.page_tokens // SP_CACHE_BLOCK)
+
+
+def sp_cache_append(desc: CacheDesc, k, v, offsets_host, offsets_dev, start, block_table, k_pool, v_pool, k_scale=None,
+                    v_scale=None, q=None, q_out=None, cos=None, sin=None, n_pos: Optional[int] = None, rot_dim: int = 0,
+                    rot_style: int = SP_ROTATE_HALF, positions=None, k_stride: Optional[int] = None,
+                    v_stride: Optional[int] = None, q_stride: Optional[int] = None, table_stride: Optional[int] = None,
+                    stream=None) -> None:
+    off = _offsets(offsets_host)
+    B = len(off) - 1
+    T = max(off[B], 0) if B >= 0 else 0
+    kw, qw = desc.n_kv_heads * desc.head_dim, desc.n_q_heads * desc.head_dim
+    kp, ks = _rows(k, "k", T, kw, k_stride, 2)
+    vp, vs = _rows(v, "v", T, kw, v_stride, 2)
+    qp, qs = _rows(q, "q", T, qw, q_stride, 2)
+    tab, width = _table(block_table, B, table_stride)
+    if n_pos is None:
+        n_pos = 0 if cos is None or isinstance(cos, int) else cos.shape[0]
+    pool, scales, trig = _pool_bytes(desc), _scale_bytes(desc), 2 * n_pos * rot_dim
+    _check(load_library().sp_cache_append(
+        ctypes.byref(desc), kp, ks, vp, vs, qp, qs, _ptr(q_out, "q_out", 2 * T * qw), off,
+        _ptr(offsets_dev, "offsets_dev", 8 * (B + 1)), B, _ptr(start, "start", 4 * B),
+        _ptr(positions, "positions", 4 * T), tab, width, _ptr(cos, "cos", trig), _ptr(sin, "sin", trig), n_pos, rot_dim, rot_style,
+        _ptr(k_pool, "k_pool", pool), _ptr(v_pool, "v_pool", pool), _ptr(k_scale, "k_scale", scales),
+        _ptr(v_scale, "v_scale", scales), _stream(stream)))
+
+
+def sp_attend_workspace(desc: CacheDesc, offsets_host, B: Optional[int] = None, max_len: int = 0) -> int:
+    off = _offsets(offsets_host)
+    n = ctypes.c_size_t(0)
+    if B is None:
+        B = len(off) - 1
+    if B >= len(off):
+        raise SpError(1, f"offsets_host has {len(off)} entries, {B} requests need {B + 1}")
+    _check(load_library().sp_attend_workspace(ctypes.byref(desc), off, B, max_len, ctypes.byref(n)))
+    return int(n.value)
+
+
+def sp_attend(desc: CacheDesc, q, offsets_host, offsets_dev, lens, max_len: int, block_table, k_pool, v_pool, k_scale,
+              v_scale, scale: float, out, lse, ws, causal: int = 1, window: int = 0, table_stride: Optional[int] = None,
+              ws_bytes: Optional[int] = None, stream=None) -> None:
+    off = _offsets(offsets_host)
+    B = len(off) - 1
+    T = max(off[B], 0) if B >= 0 else 0
+    tab, width = _table(block_table, B, table_stride)
+    rows, pool, scales = T * desc.n_q_heads, _pool_bytes(desc), _scale_bytes(desc)
+    _check(load_library().sp_attend(
+        ctypes.byref(desc), _ptr(q, "q", 2 * rows * desc.head_dim), off, _ptr(offsets_dev, "offsets_dev", 8 * (B + 1)), B,
+        _ptr(lens, "lens", 4 * B), max_len, tab, width, _ptr(k_pool, "k_pool", pool), _ptr(v_pool, "v_pool", pool),
+        _ptr(k_scale, "k_scale", scales), _ptr(v_scale, "v_scale", scales), scale, causal, window,
+        _ptr(out, "out", 2 * rows * desc.head_dim), _ptr(lse, "lse", 4 * rows), _ptr(ws, "ws"), _ws_bytes(ws, ws_bytes),
+        _stream(stream)))
+
+
+def sp_logprobs_workspace(n_rows: int, vocab: int, n_top: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().sp_logprobs_workspace(n_rows, vocab, n_top, ctypes.byref(n)))
+    return int(n.value)
+
+
+def sp_logprobs(logits, n_rows: int, vocab: int, targets, n_top: int, logprob, entropy, top_ids, top_logprobs, ws,
+                dtype: Optional[int] = None, row_stride: Optional[int] = None, ws_bytes: Optional[int] = None,
+                stream=None) -> None:
+    if dtype is None:       # from the tensor: four bytes an element are fp32, two are bf16 (or its bits)
+        if not hasattr(logits, "element_size"):
+            raise SpError(1, "logits given as an address need a dtype")
+        if logits.element_size() not in (2, 4):
+            raise SpError(1, "logits have to be fp32 or bf16")
+        dtype = SP_LOGITS_F32 if logits.element_size() == 4 else SP_LOGITS_BF16
+    x, stride = _rows(logits, "logits", n_rows, vocab, row_stride, 4 if dtype == SP_LOGITS_F32 else 2)
+    n, k = max(n_rows, 0), max(n_top, 0)
+    _check(load_library().sp_logprobs(
+        x, dtype, n_rows, vocab, max(stride, vocab) if n_rows <= 1 else stride, _ptr(targets, "targets", 4 * n), n_top,
+        _ptr(logprob, "logprob", 4 * n), _ptr(entropy, "entropy", 4 * n), _ptr(top_ids, "top_ids", 4 * n * k),
+        _ptr(top_logprobs, "top_logprobs", 4 * n * k), _ptr(ws, "ws"), _ws_bytes(ws, ws_bytes), _stream(stream)))
