@@ -456,7 +456,7 @@ typedef enum { SP_CACHE_BF16 = 0, SP_CACHE_E4M3 = 1 } sp_cache_type;
  * Supported: head_dim 64 or 128; n_q_heads a multiple of n_kv_heads with ratio
  * G <= 16; n_kv_heads <= 4096; page_tokens a positive multiple of SP_CACHE_BLOCK, at most
  * 2^24; strides multiples of 16 (E4M3) or 8 (bf16) elements, stride_token >=
- * head_dim, none above 2^40; 1 <= n_pages < 2^31. */
+ * head_dim and <= 2^24, none above 2^40; 1 <= n_pages < 2^31. */
 typedef struct {
     int32_t n_q_heads;
     int32_t n_kv_heads;
@@ -530,13 +530,11 @@ sp_status sp_attend_workspace(const sp_cache_desc *desc, const int64_t *offsets_
  *   out_dev[row, h] = sum_j p_j V[b, h/G, j],  p_j = softmax_j( scale * <q, K[b, h/G, j]> )
  * as dense bf16 [rows][n_q_heads][head_dim], and lse_dev[row, h] (float, optional) the natural
  * logarithm of the softmax's denominator. A row that sees no key gets zeros and an lse
- * of minus infinity. Keys and values outside what a row sees (slots of a last page past the
+ * of minus infinity. Slots that no row of the request sees (those of a last page past the
  * context among them) may hold anything, NaN included.
  * max_len bounds the contexts from the host's side (a longer lens[b] counts as
  * max_len, a negative one as 0) and must not exceed table_stride * page_tokens; the call reads the table entries
- * of the tokens below lens[b] only. E4M3 scales should be the powers of two that
- * sp_cache_append writes: a scale that is not one costs another rounding to bf16 for each element.
- * The probabilities of the second product are rounded to bf16; sums and statistics are held in fp32. The
+ * of the tokens below lens[b] only. The probabilities of the second product are rounded to bf16; sums and statistics are held in fp32. The
  * result does not change from call to call on the same inputs. scale: finite and > 0.
  */
 sp_status sp_attend(const sp_cache_desc *desc, const void *q_dev,

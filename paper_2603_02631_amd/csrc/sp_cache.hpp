@@ -42,6 +42,8 @@ inline sp_status check_cache(const sp_cache_desc *d)
                         (long long)unit);
     if (d->stride_token < d->head_dim)
         return fail(SP_ERR_INVALID_ARG, "stride_token = %lld is less than head_dim = %d", (long long)d->stride_token, d->head_dim);
+    if (d->stride_token > (1 << 24))
+        return fail(SP_ERR_INVALID_ARG, "stride_token = %lld exceeds 2^24", (long long)d->stride_token);
     if (d->n_kv_heads > 1 && d->stride_head < d->head_dim)
         return fail(SP_ERR_INVALID_ARG, "stride_head = %lld is less than head_dim = %d", (long long)d->stride_head, d->head_dim);
     if (d->n_pages > 1 && d->page_stride < d->head_dim)
