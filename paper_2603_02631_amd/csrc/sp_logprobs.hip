@@ -2,122 +2,424 @@
 // ForwardWithAttn, the end of a draft model's forward pass, where the next lookahead token is picked).
 //
 // With m = max x, s = sum exp(x - m), u = sum (x - m) exp(x - m):
-//   lse = m + log s,  lp_t = (x_t - m) - log s,  H = log s - u / s.
+//   lse = m + log s,  lp_t = (x_t - m) - log s,  H = log s - u / s,
+// in one pass: every thread keeps (m, s, u) of its own chunks of 16 bytes (every kThreads-th one) and moves m when a chunk exceeds
+// it; the threads' parts are joined at the end.
 //
-// One workgroup takes a row: one pass for m, s and u, then one pass for every alternative, which finds the best token
-// behind the last one found (larger logit first, lower token first among equals).
+// The likeliest k tokens come out of the same pass. A thread's m and the first chunk that reached it are all that is kept. The k-th best of 64
+// groups' maxima is a bound that k elements reach, so the k best elements of the row do, and they lie in the chunks of threads
+// whose maximum reaches it: usually k threads of 512. Only those threads' chunks are read a second time. Values are compared together with
+// the chunk, lower first, so that rows full of equal logits (forbidden tokens) leave no more to do than others.
+// What reached the bound is ranked by counting. Should it not fit the list (hundreds of the best in one thread's chunks),
+// the k best are found one by one in the same chunks.
+//
+// A row belongs to one workgroup; few rows are split among several (a segment of the vocabulary each), whose parts a second launch joins.
+// Bound by HBM for many rows (each logit costs an exponential and five more operations; at 16 bits a logit that is as long as its
+// bytes take), by latency for few.
 #include "sp_common.hpp"
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / 64;
+constexpr int kTop = SP_LOGPROBS_MAX_TOP;
+constexpr int kList = 1024;                 // elements that reach the bound
+constexpr int kMaxSplits = 32;
+constexpr int64_t kMinSplit = 4096;         // logits of a segment
+constexpr float kFar = 1e4f;                // exp(-kFar) is 0
+constexpr float kLowest = -3.402823466e38f;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
 
-constexpr float kFar = 1e4f;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
+struct Args {
+    const uint8_t *logits;
+    int64_t vocab, row_stride;
+    const int32_t *targets;
+    float *logprob, *entropy;
+    int32_t *top_ids;
+    float *top_logprobs;
+    int32_t n_top, splits;
+    float *part;            // [row][split][4]: m, s, u
+    uint64_t *part_keys;    // [row][split][n_top], best first
+};
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_huge_valf(); }
+__device__ __forceinline__ float exp_(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+__device__ __forceinline__ float log_(float x) { return __builtin_amdgcn_logf(x) * kLn2; }
 
-template <bool BF16>
-__device__ __forceinline__ float logit(const void *row, int64_t i)
+// Order of logits as unsigned integers, zeros of both signs alike; 0 stands for no logit.
+__device__ __forceinline__ uint32_t order_of(float x)
 {
-    if (BF16) return __uint_as_float((uint32_t)static_cast<const uint16_t *>(row)[i] << 16);
-    return static_cast<const float *>(row)[i];
+    const uint32_t u = x == 0.f ? 0u : __float_as_uint(x);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// (m, s, u) of two parts of a row. A part without a finite logit is (-inf, 0, 0).
-__device__ __forceinline__ void join(float &m, float &s, float &u, float m2, float s2, float u2)
-{
-    const float mm = fmaxf(m, m2);
-    if (mm == neg_inf()) return;
-    const float a = m == neg_inf() ? 0.f : __expf(m - mm), b = m2 == neg_inf() ? 0.f : __expf(m2 - mm);
-    // what lies more than kFar below the maximum has no weight; the product below must not overflow for it (logits of the type's
-    // lowest value)
-    const float d = fmaxf(m - mm, -kFar), d2 = fmaxf(m2 - mm, -kFar);
-    u = a * (u + d * s) + b * (u2 + d2 * s2);
-    s = a * s + b * s2;
-    m = mm;
-}
+__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
 
-// Whether (x, i) comes before (y, j).
-__device__ __forceinline__ bool before(float x, int64_t i, float y, int64_t j) { return x > y || (x == y && i < j); }
+// Larger key: larger logit, lower token among equals.
+__device__ __forceinline__ uint64_t key_of(float x, int64_t i) { return (uint64_t)order_of(x) << 32 | (0xffffffffu - (uint32_t)i); }
 
-template <bool BF16>
-__global__ __launch_bounds__(kThreads) void sp_logprobs_row_kernel(const void *logits, int64_t vocab, int64_t row_stride,
-                                                                   const int32_t *targets, int n_top, float *logprob,
-                                                                   float *entropy, int32_t *top_ids, float *top_logprobs)
-{
-    __shared__ float sm[kWaves], ss[kWaves], su[kWaves];
-    __shared__ int64_t si[kWaves];
-    const int64_t r = blockIdx.x;
-    const int tid = threadIdx.x;
-    const void *row = static_cast<const uint8_t *>(logits) + r * row_stride * (BF16 ? 2 : 4);
-    float m = neg_inf(), s = 0.f, u = 0.f;
-    for (int64_t i = tid; i < vocab; i += kThreads) {
-        const float x = logit<BF16>(row, i);
-        if (x != neg_inf()) join(m, s, u, x, 1.f, 0.f);
+// Sums of a part of a row about its maximum (kLowest where it has no finite logit).
+struct Sums {
+    float m, s, u;
+
+    __device__ __forceinline__ void move(float to)          // to >= m
+    {
+        const float d = fmaxf(m - to, -kFar), f = exp_(d);
+        u = f * (u + d * s);
+        s *= f;
+        m = to;
     }
-    for (int o = 32; o; o >>= 1) join(m, s, u, __shfl_xor(m, o), __shfl_xor(s, o), __shfl_xor(u, o));
-    if ((tid & 63) == 0) {
-        sm[tid >> 6] = m;
-        ss[tid >> 6] = s;
-        su[tid >> 6] = u;
+
+    __device__ __forceinline__ void join(float m2, float s2, float u2)
+    {
+        const float to = fmaxf(m, m2);
+        Sums o{m2, s2, u2};
+        move(to);
+        o.move(to);
+        s += o.s;
+        u += o.u;
+    }
+};
+
+// A row in chunks of 16 bytes that begin at multiples of 16 bytes: the first and the last may hold less than E logits of it.
+template <bool BF16>
+struct Row {
+    static constexpr int E = BF16 ? 8 : 4;
+    const uint8_t *base;        // of chunk 0
+    int64_t skip, vocab;        // elements of chunk 0 before the row
+    uint32_t chunks;
+
+    __device__ __forceinline__ Row(const Args &a, int64_t r)
+    {
+        const uint8_t *row = a.logits + r * a.row_stride * (BF16 ? 2 : 4);
+        const int64_t odd = (int64_t)(reinterpret_cast<uintptr_t>(row) & 15);
+        base = row - odd;
+        skip = odd / (BF16 ? 2 : 4);
+        vocab = a.vocab;
+        chunks = (uint32_t)((vocab + skip + E - 1) / E);
+    }
+
+    __device__ __forceinline__ int64_t index(uint32_t c, int e) const { return (int64_t)c * E + e - skip; }
+
+    __device__ __forceinline__ bool whole(uint32_t c) const { return index(c, 0) >= 0 && index(c, E) <= vocab; }
+
+    // Logits of a chunk; -inf in the places that are not the row's, which are not read.
+    __device__ __forceinline__ void load(uint32_t c, float (&x)[E]) const
+    {
+        if (whole(c)) {
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(base + (int64_t)c * 16);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                x[e] = BF16 ? __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16) : __uint_as_float(w[e % 4]);
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            x[e] = neg_inf();
+            if (index(c, e) >= 0 && index(c, e) < vocab) {
+                if (BF16) x[e] = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(base + (int64_t)c * 16 + 2 * e) << 16);
+                else x[e] = *reinterpret_cast<const float *>(base + (int64_t)c * 16 + 4 * e);
+            }
+        }
+    }
+
+    __device__ __forceinline__ float at(int64_t i) const
+    {
+        const uint8_t *p = base + (i + skip) * (BF16 ? 2 : 4);
+        return BF16 ? __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(p) << 16) : *reinterpret_cast<const float *>(p);
+    }
+};
+
+// The k-th largest of 64 lanes' values, 0 if fewer than k lanes hold one, and the last chunk that counts among lanes that hold it:
+// exactly k of the lanes (or all, if fewer hold a value) are at or before (value, chunk).
+__device__ __forceinline__ void bound_of(uint32_t v, uint32_t chunk, int k, uint32_t *value, uint32_t *last)
+{
+    uint32_t t = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t c = t | 1u << bit;
+        if (__popcll(__ballot(v >= c)) >= k) t = c;
+    }
+    *value = t;
+    *last = 0xffffffffu;
+    const bool same = v == t;
+    const int want = k - __popcll(__ballot(v > t));
+    if (t != 0 && __popcll(__ballot(same)) > want) {
+        uint32_t lo = 0;                                    // the want-th smallest chunk among them
+        for (int bit = 29; bit >= 0; --bit)
+            if (__popcll(__ballot(same && chunk < lo + (1u << bit))) < want) lo += 1u << bit;
+        *last = lo;
+    }
+}
+
+struct Shared {
+    uint32_t order[kThreads], chunk[kThreads];
+    float sums[kWaves][3];
+    uint64_t list[kList];
+    uint64_t best[kWaves];
+    uint16_t column[kThreads];
+    uint32_t bound, last, columns, found;
+};
+
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void sp_logprobs_kernel(Args a)
+{
+    __shared__ Shared sh;
+    constexpr int E = Row<BF16>::E;
+    const int64_t r = blockIdx.y;
+    const int split = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const Row<BF16> row(a, r);
+    const uint32_t each = (row.chunks + a.splits - 1) / a.splits;
+    const uint32_t from = min(row.chunks, split * each), to = min(row.chunks, from + each);
+
+    Sums t{kLowest, 0.f, 0.f};
+    float best = neg_inf();
+    uint32_t best_chunk = from + tid;
+    constexpr int kUnroll = 4;
+    for (uint32_t c0 = from + tid; c0 < to; c0 += kThreads * kUnroll) {
+        float x[kUnroll][E];
+#pragma unroll
+        for (int i = 0; i < kUnroll; ++i) {
+            const uint32_t c = c0 + i * kThreads;
+            if (c < to) row.load(c, x[i]);
+            else
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[i][e] = neg_inf();
+        }
+#pragma unroll
+        for (int i = 0; i < kUnroll; ++i) {
+            float top = x[i][0];
+#pragma unroll
+            for (int e = 1; e < E; ++e) top = fmaxf(top, x[i][e]);
+            if (top > best) {
+                best = top;
+                best_chunk = c0 + i * kThreads;
+                t.move(top);
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float d = fmaxf(x[i][e] - t.m, -kFar), p = exp_(d);
+                t.s += p;
+                t.u += d * p;
+            }
+        }
+    }
+
+    if (a.n_top > 0) {
+        sh.order[tid] = from + tid < to ? order_of(best) : 0u;
+        sh.chunk[tid] = best_chunk;
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) t.join(__shfl_xor(t.m, o), __shfl_xor(t.s, o), __shfl_xor(t.u, o));
+    if (lane == 0) {
+        sh.sums[wave][0] = t.m;
+        sh.sums[wave][1] = t.s;
+        sh.sums[wave][2] = t.u;
+    }
+    if (tid == 0) sh.columns = sh.found = 0;
+    __syncthreads();
+    t = Sums{sh.sums[0][0], sh.sums[0][1], sh.sums[0][2]};
+    for (int w = 1; w < kWaves; ++w) t.join(sh.sums[w][0], sh.sums[w][1], sh.sums[w][2]);
+    const float log_s = t.s > 0.f ? log_(t.s) : 0.f;
+    if (tid == 0) {
+        if (a.splits > 1) {
+            float *p = a.part + (r * a.splits + split) * 4;
+            p[0] = t.m;
+            p[1] = t.s;
+            p[2] = t.u;
+        } else {
+            if (a.logprob) {
+                const int64_t i = a.targets[r];
+                float lp = 0.f;
+                if (i >= 0 && i < a.vocab) {
+                    const float x = row.at(i);
+                    lp = x == neg_inf() ? x : (x - t.m) - log_s;
+                }
+                a.logprob[r] = lp;
+            }
+            if (a.entropy) a.entropy[r] = t.s > 0.f ? log_s - t.u / t.s : 0.f;
+        }
+    }
+    const int k = a.n_top;
+    if (k == 0) return;
+
+    if (wave == 0) {                        // lane l: the best of threads l, l + 64, ...
+        uint32_t v = 0, c = 0xffffffffu;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const uint32_t v2 = sh.order[lane + 64 * w], c2 = sh.chunk[lane + 64 * w];
+            if (v2 > v || (v2 == v && c2 < c)) {
+                v = v2;
+                c = c2;
+            }
+        }
+        uint32_t bound, last;
+        bound_of(v, c, k, &bound, &last);
+        if (lane == 0) {
+            sh.bound = bound;
+            sh.last = last;
+        }
     }
     __syncthreads();
-    m = sm[0];
-    s = ss[0];
-    u = su[0];
-    for (int w = 1; w < kWaves; ++w) join(m, s, u, sm[w], ss[w], su[w]);
-    const float log_s = s > 0.f ? __logf(s) : 0.f;
-    if (tid == 0) {
-        if (logprob) {
-            const int64_t t = targets[r];
-            float lp = 0.f;
-            if (t >= 0 && t < vocab) {
-                const float x = logit<BF16>(row, t);
-                lp = x == neg_inf() ? x : (x - m) - log_s;
+    const uint32_t bound = sh.bound, last = sh.last, mine = sh.order[tid];
+    if (mine != 0 && (mine > bound || (mine == bound && sh.chunk[tid] <= last))) sh.column[atomicAdd(&sh.columns, 1u)] = (uint16_t)tid;
+    __syncthreads();
+    const uint32_t depth = (to - from + kThreads - 1) / kThreads, items = sh.columns * depth;
+    for (uint32_t n = tid; n < items; n += kThreads) {
+        const uint32_t c = from + sh.column[n / depth] + n % depth * kThreads;
+        if (c >= to) continue;
+        float x[E];
+        row.load(c, x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const uint32_t o = order_of(x[e]);
+            const int64_t i = row.index(c, e);
+            if (i >= 0 && i < a.vocab && (o > bound || (o == bound && c <= last))) {
+                const uint32_t at = atomicAdd(&sh.found, 1u);
+                if (at < kList) sh.list[at] = key_of(x[e], i);
             }
-            logprob[r] = lp;
         }
-        if (entropy) entropy[r] = s > 0.f ? log_s - u / s : 0.f;
     }
-    float last = __builtin_huge_valf();
-    int64_t last_i = -1;
-    for (int k = 0; k < n_top; ++k) {
-        float best = neg_inf();
-        int64_t best_i = INT64_MAX;
-        for (int64_t i = tid; i < vocab; i += kThreads) {
-            const float x = logit<BF16>(row, i);
-            if (before(last, last_i, x, i) && before(x, i, best, best_i)) {
-                best = x;
-                best_i = i;
+    __syncthreads();
+    const uint32_t found = sh.found;
+    const auto report = [&](int rank, uint64_t key) {
+        if (a.splits > 1) {
+            a.part_keys[(r * a.splits + split) * k + rank] = key;
+            return;
+        }
+        const float x = value_of((uint32_t)(key >> 32));
+        a.top_ids[r * k + rank] = (int32_t)(0xffffffffu - (uint32_t)key);
+        a.top_logprobs[r * k + rank] = x == neg_inf() ? x : (x - t.m) - log_s;
+    };
+    if (found <= kList) {
+        for (uint32_t i = tid; i < found; i += kThreads) {
+            const uint64_t key = sh.list[i];
+            int rank = 0;
+            for (uint32_t j = 0; j < found; ++j) rank += sh.list[j] > key;
+            if (rank < k) report(rank, key);
+        }
+        for (int i = tid; i < k; i += kThreads)             // a segment with fewer than k logits
+            if (i >= (int)found) report(i, 0);
+        return;
+    }
+    uint64_t above = ~0ull;
+    for (int i = 0; i < k; ++i) {
+        uint64_t top = 0;
+        for (uint32_t n = tid; n < items; n += kThreads) {
+            const uint32_t c = from + sh.column[n / depth] + n % depth * kThreads;
+            if (c >= to) continue;
+            float x[E];
+            row.load(c, x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int64_t j = row.index(c, e);
+                const uint64_t key = j >= 0 && j < a.vocab ? key_of(x[e], j) : 0;
+                if (key < above && key > top) top = key;
             }
         }
+#pragma unroll
         for (int o = 32; o; o >>= 1) {
-            const float y = __shfl_xor(best, o);
-            const int64_t j = __shfl_xor(best_i, o);
-            if (before(y, j, best, best_i)) {
-                best = y;
-                best_i = j;
-            }
+            const uint64_t y = __shfl_xor((unsigned long long)top, o);
+            top = y > top ? y : top;
         }
         __syncthreads();
-        if ((tid & 63) == 0) {
-            sm[tid >> 6] = best;
-            si[tid >> 6] = best_i;
-        }
+        if (lane == 0) sh.best[wave] = top;
         __syncthreads();
-        last = sm[0];
-        last_i = si[0];
-        for (int w = 1; w < kWaves; ++w)
-            if (before(sm[w], si[w], last, last_i)) {
-                last = sm[w];
-                last_i = si[w];
+        for (int w = 0; w < kWaves; ++w) top = sh.best[w] > top ? sh.best[w] : top;
+        if (tid == 0) report(i, top);
+        above = top;
+    }
+}
+
+// Joins the segments of a row. A key's rank is its place in its own segment plus, for every other segment, the number of larger
+// keys there, found by bisection (segments are sorted).
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void sp_logprobs_join_kernel(Args a)
+{
+    __shared__ uint64_t keys[kMaxSplits * kTop];
+    const int64_t r = blockIdx.x;
+    const int tid = threadIdx.x, k = a.n_top;
+    for (int i = tid; i < a.splits * k; i += kThreads) keys[i] = a.part_keys[r * a.splits * k + i];
+    Sums t{kLowest, 0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s) {
+        const float *p = a.part + (r * a.splits + s) * 4;
+        t.join(p[0], p[1], p[2]);
+    }
+    const float log_s = t.s > 0.f ? log_(t.s) : 0.f;
+    if (tid == 0) {
+        if (a.logprob) {
+            const int64_t i = a.targets[r];
+            float lp = 0.f;
+            if (i >= 0 && i < a.vocab) {
+                const float x = Row<BF16>(a, r).at(i);
+                lp = x == neg_inf() ? x : (x - t.m) - log_s;
             }
-        if (tid == 0) {
-            top_ids[r * n_top + k] = (int32_t)last_i;
-            top_logprobs[r * n_top + k] = last == neg_inf() ? last : (last - m) - log_s;
+            a.logprob[r] = lp;
+        }
+        if (a.entropy) a.entropy[r] = t.s > 0.f ? log_s - t.u / t.s : 0.f;
+    }
+    __syncthreads();
+    for (int i = tid; i < a.splits * k; i += kThreads) {
+        const uint64_t key = keys[i];
+        if (key == 0) continue;
+        int rank = 0;
+        for (int s = 0; s < a.splits && rank < k; ++s) {
+            int lo = 0, hi = k;                 // larger keys of segment s
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (keys[s * k + mid] > key) lo = mid + 1; else hi = mid;
+            }
+            rank += lo;
+        }
+        if (rank < k) {
+            const float x = value_of((uint32_t)(key >> 32));
+            a.top_ids[r * k + rank] = (int32_t)(0xffffffffu - (uint32_t)key);
+            a.top_logprobs[r * k + rank] = x == neg_inf() ? x : (x - t.m) - log_s;
         }
     }
+}
+
+// Segments of a row: as many as keep the device busy (two workgroups of 512 threads on each of 256 compute units), each worth its launch.
+int splits_of(int64_t n_rows, int64_t vocab)
+{
+    const int64_t want = n_rows > 0 ? 512 / n_rows : 1, most = vocab / kMinSplit;
+    const int64_t s = want < most ? want : most;
+    return (int)(s < 1 ? 1 : (s > kMaxSplits ? kMaxSplits : s));
+}
+
+size_t keys_at(int64_t n_rows, int splits) { return sp::align_up((size_t)n_rows * splits * 4 * sizeof(float), 256); }
+
+size_t workspace_need(int64_t n_rows, int splits, int n_top)
+{
+    if (splits <= 1) return 0;
+    return keys_at(n_rows, splits) + sp::align_up((size_t)n_rows * splits * n_top * sizeof(uint64_t), 256);
+}
+
+template <bool BF16>
+sp_status run(const Args &a, int64_t n_rows, hipStream_t st)
+{
+    // rows go to the second grid dimension, 65535 at a time
+    for (int64_t r0 = 0; r0 < n_rows; r0 += 65535) {
+        const int64_t n = n_rows - r0 < 65535 ? n_rows - r0 : 65535;
+        Args b = a;
+        b.logits += r0 * a.row_stride * (BF16 ? 2 : 4);
+        if (b.targets) b.targets += r0;
+        if (b.logprob) b.logprob += r0;
+        if (b.entropy) b.entropy += r0;
+        if (b.n_top) {
+            b.top_ids += r0 * a.n_top;
+            b.top_logprobs += r0 * a.n_top;
+        }
+        hipLaunchKernelGGL((sp_logprobs_kernel<BF16>), dim3((unsigned)a.splits, (unsigned)n), dim3(kThreads), 0, st, b);
+        SP_HIP_CHECK(hipGetLastError());
+    }
+    if (a.splits > 1) {
+        hipLaunchKernelGGL((sp_logprobs_join_kernel<BF16>), dim3((unsigned)n_rows), dim3(kThreads), 0, st, a);
+        SP_HIP_CHECK(hipGetLastError());
+    }
+    return SP_OK;
 }
 
 }  // namespace
@@ -131,7 +433,7 @@ extern "C" sp_status sp_logprobs_workspace(int64_t n_rows, int64_t vocab, int32_
         return sp::fail(SP_ERR_INVALID_ARG, "vocab = %lld outside 1..2^31-1", (long long)vocab);
     if (n_top < 0 || n_top > SP_LOGPROBS_MAX_TOP || n_top > vocab)
         return sp::fail(SP_ERR_INVALID_ARG, "n_top = %d outside 0..min(%d, vocab)", n_top, SP_LOGPROBS_MAX_TOP);
-    *bytes = 0;
+    *bytes = workspace_need(n_rows, splits_of(n_rows, vocab), n_top);
     return SP_OK;
 }
 
@@ -159,14 +461,9 @@ extern "C" sp_status sp_logprobs(const void *logits_dev, int32_t dtype, int64_t 
         if ((uintptr_t)ws_dev % 256 != 0) return sp::fail(SP_ERR_WORKSPACE, "ws_dev is not 256-byte aligned");
         if (ws_bytes < need) return sp::fail(SP_ERR_WORKSPACE, "workspace too small: %zu < %zu", ws_bytes, need);
     }
+    Args a{static_cast<const uint8_t *>(logits_dev), vocab, row_stride, targets_dev, logprob_dev, entropy_dev, top_ids_dev,
+           top_logprobs_dev, n_top, splits_of(n_rows, vocab), static_cast<float *>(ws_dev), nullptr};
+    a.part_keys = reinterpret_cast<uint64_t *>(static_cast<uint8_t *>(ws_dev) + keys_at(n_rows, a.splits));
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const dim3 grid((unsigned)n_rows);
-    if (dtype == SP_LOGITS_BF16)
-        hipLaunchKernelGGL((sp_logprobs_row_kernel<true>), grid, dim3(kThreads), 0, st, logits_dev, vocab, row_stride,
-                           targets_dev, (int)n_top, logprob_dev, entropy_dev, top_ids_dev, top_logprobs_dev);
-    else
-        hipLaunchKernelGGL((sp_logprobs_row_kernel<false>), grid, dim3(kThreads), 0, st, logits_dev, vocab, row_stride,
-                           targets_dev, (int)n_top, logprob_dev, entropy_dev, top_ids_dev, top_logprobs_dev);
-    SP_HIP_CHECK(hipGetLastError());
-    return SP_OK;
+    return dtype == SP_LOGITS_BF16 ? run<true>(a, n_rows, st) : run<false>(a, n_rows, st);
 }

@@ -168,3 +168,23 @@ def test_logprobs_rows_beyond_32_bit_offsets():
     for r in range(rows):
         lp, h, ids, lps, mean = ou.logprobs(x[r], 4 + r, 3)
         assert got[2][r].tolist() == ids and abs(got[0][r] - lp) < 2e-5 and abs(got[1][r] - h) < 2e-5 * (1 + mean)
+
+
+@pytest.mark.parametrize("bf16,width", [(True, 8), (False, 4)])
+@pytest.mark.parametrize("rows", [1, 520])
+def test_logprobs_with_the_best_thousands_in_a_few_places(bf16, width, rows):
+    """All large logits in the chunks of 16 bytes that eight neighbouring threads of 512 read: thousands of them exceed what a bound on
+    threads' maxima can exclude. 520 equal rows take one workgroup each."""
+    vocab = 120000
+    rng = np.random.default_rng(9)
+    x = ou.bf16_round(rng.standard_normal(vocab))
+    i = np.arange(vocab)
+    here = (i // width) % 512 < 8
+    x[here] = ou.bf16_round(20 + rng.standard_normal(int(here.sum())) * 3)
+    got = call(to_dev(np.repeat(x[None], rows, axis=0), bf16), rows, vocab, [77] * rows, 32)
+    lp, h, ids, lps, mean = ou.logprobs(x, 77, 32)
+    assert got[2][0].tolist() == ids
+    assert abs(got[0][0] - lp) <= 1e-3 and abs(got[1][0] - h) <= 1e-3
+    np.testing.assert_allclose(got[3][0], lps, atol=1e-4)
+    for a in got:
+        assert (a == a[:1]).all()
