@@ -532,6 +532,7 @@ sp_status sp_attend_workspace(const sp_cache_desc *desc, const int64_t *offsets_
  * logarithm of the softmax's denominator. A row that sees no key gets zeros and an lse
  * of minus infinity. Slots that no row of the request sees (those of a last page past the
  * context among them) may hold anything, NaN included.
+ * At most 2^26 query tokens and contexts of at most 2^30 tokens.
  * max_len bounds the contexts from the host's side (a longer lens[b] counts as
  * max_len, a negative one as 0) and must not exceed table_stride * page_tokens; the call reads the table entries
  * of the tokens below lens[b] only. The probabilities of the second product are rounded to bf16; sums and statistics are held in fp32. The

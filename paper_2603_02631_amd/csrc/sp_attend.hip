@@ -6,9 +6,13 @@
 // in one pass over the keys: a reference m and a sum l that run along, and the partial output, scaled whenever m moves.
 //
 // Query rows of one request that share a kv head (n_b tokens of G heads) are taken together, so that a key is read once for
-// all of them. Requests of up to kFewRows rows go to sp_attend_few_kernel, which is bound by the cache's bytes and splits
-// a context among workgroups; others to sp_attend_many_kernel, tiles of 256 rows, which is bound by its operations and splits contexts only
-// where there are too few tiles. The join kernels put splits together.
+// all of them. Requests of up to few_rows_of() rows go to sp_attend_few_kernel, which is bound by the cache's bytes, others to
+// sp_attend_many_kernel, tiles of 256 rows, which is bound by its operations.
+//
+// Shares. Contexts differ and only the device knows them, so work is shared out there: the blocks of all (request, kv head) lines
+// are laid end to end, and workgroup i of N takes the i-th of N equal stretches. A line that lies in one stretch is finished there;
+// of others every stretch leaves a partial result (reference, sum, unscaled output), at most two a workgroup, which a second
+// launch joins. Nothing is added atomically: the order of every sum is fixed by the lengths.
 #include "sp_cache.hpp"
 
 namespace {
@@ -22,7 +26,9 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kFewRows = 64;        // query rows of a kv head that sp_attend_few_kernel takes at most
+// Query rows of a kv head that sp_attend_few_kernel takes at most. More rows need more registers than its latency hiding can spare at head_dim
+// 128: 64 rows over two contexts of 20000 tokens take 102 us there and 46 in the other kernel (head_dim 64, four of 30000 to 64000: 83 and 179).
+constexpr int few_rows_of(int d) { return d == 128 ? 32 : 64; }
 constexpr int kManyList = 64;
 constexpr int kBlock = sp::kCacheBlock;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -37,19 +43,20 @@ struct AttendArgs {
     const float *k_scale, *v_scale;
     uint16_t *out;
     float *lse;
-    int64_t max_len, window;
+    int32_t max_len, window;            // a window is shorter than max_len, or 0
     int32_t B, causal;
     float scale;
     int32_t page_blocks, page_shift;    // blocks of 32 tokens in a page; their logarithm, or -1
-    // splits of sp_attend_few_kernel: `splits` of `split_blocks` blocks; `few_rows` rows a request and kv head in the workspace
-    int32_t splits, split_blocks, few_rows;
-    f32x2 *part_ml;                     // [split][request][kv head][few_rows]: reference (in units of log 2), sum
-    float *part_o;                      // [...][head_dim]
-    // tiles of sp_attend_many_kernel, and its splits of `many_keys` keys
-    int32_t tiles, many_splits;
-    int64_t many_keys;
-    f32x2 *many_ml;                     // [split][tile][kv head][kManyRows]
+    // sp_attend_few_kernel: workgroups that share the work (0: one for each request and kv head), rows of a partial result
+    int32_t few_shares, few_rows;
+    f32x2 *few_ml;                      // [2 few_shares][few_rows]: reference (in units of log 2), sum
+    float *few_o;                       // [2 few_shares][few_rows][head_dim]
+    int64_t *few_before;                // [B + 1]: units of work before each request
+    // sp_attend_many_kernel: tiles of query rows, workgroups that share the work (0: one for each tile and kv head)
+    int32_t tiles, many_shares;
+    f32x2 *many_ml;                     // as above, kManyRows rows
     float *many_o;
+    int64_t *many_before;               // [tiles + 1]
     // the requests with many rows and their first tiles, if there are at most kManyList of them (else many_count is 0)
     int32_t many_count, many_b[kManyList], many_tile[kManyList];
 };
@@ -65,23 +72,23 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
 
 // ---- a few rows: single tokens, lookahead rows -----------------------------------------------------------------------
 
-// What a request's rows see: row r (token r / G) keys [first(r), last(r)), all rows together [lo, hi).
+// What a request's rows see: row r (token r / G) keys [first(r), last(r)), all rows together [lo, hi). Key indices fit 32 bits:
+// contexts are limited to 2^30 tokens, queries to 2^26.
 struct Range {
-    int64_t len, n;
-    int64_t lo, hi;
+    int len, n, lo, hi;
 };
 
 __device__ __forceinline__ Range range_of(const AttendArgs &a, int b)
 {
     Range g;
-    g.n = a.off[b + 1] - a.off[b];
+    g.n = (int)(a.off[b + 1] - a.off[b]);
     g.len = a.lens[b];
     g.len = g.len < 0 ? 0 : (g.len > a.max_len ? a.max_len : g.len);
     g.lo = 0;
     g.hi = g.len;
     if (a.causal && a.window > 0) {
-        const int64_t f = g.len - g.n - a.window + 1;
-        g.lo = f > 0 ? f : 0;
+        const int64_t f = (int64_t)g.len - g.n - a.window + 1;
+        g.lo = f > 0 ? (int)f : 0;
     }
     return g;
 }
@@ -91,12 +98,15 @@ __device__ __forceinline__ uint32_t page_of_block(const AttendArgs &a, uint32_t 
     return a.page_shift >= 0 ? blk >> a.page_shift : blk / (uint32_t)a.page_blocks;
 }
 
-__device__ __forceinline__ int page_at(const AttendArgs &a, int b, uint32_t blk)
+// An entry of request b's row of the block table.
+__device__ __forceinline__ int page_entry(const AttendArgs &a, int b, uint32_t i)
 {
-    int page = a.c.table[b * a.c.table_stride + page_of_block(a, blk)];
+    int page = a.c.table[b * a.c.table_stride + i];
     page = page < 0 ? 0 : page;                                     // never outside the pools
     return page >= (int)a.c.n_pages ? (int)a.c.n_pages - 1 : page;
 }
+
+__device__ __forceinline__ int page_at(const AttendArgs &a, int b, uint32_t blk) { return page_entry(a, b, page_of_block(a, blk)); }
 
 // Eight E4M3 codes as eight bf16, exactly: the upper halves of their float images.
 __device__ __forceinline__ bf16x8 widen8(uint32_t c0, uint32_t c1)
@@ -123,38 +133,47 @@ struct Block {
     uint32_t v[8][kLoads];
     float ks, vs;
 
-    __device__ __forceinline__ void load(const AttendArgs &a, int kvh, int page, uint32_t blk, uint32_t k_lane, uint32_t v_lane)
+    static constexpr int ES = E4M3 ? 1 : 2;
+
+    __device__ __forceinline__ static int64_t base_of(const AttendArgs &a, int kvh, int page, uint32_t in_page)
     {
-        constexpr int ES = E4M3 ? 1 : 2;
+        return (page * a.c.page_stride + kvh * a.c.stride_head + (int64_t)(in_page * kBlock) * a.c.stride_token) * ES;
+    }
+
+    __device__ __forceinline__ void load_keys(const AttendArgs &a, int kvh, int page, uint32_t blk, uint32_t lane)
+    {
         const uint32_t in_page = blk - page_of_block(a, blk) * (uint32_t)a.page_blocks;
-        const int64_t base = (page * a.c.page_stride + kvh * a.c.stride_head + (int64_t)(in_page * kBlock) * a.c.stride_token) * ES;
-        const int64_t row = a.c.stride_token * ES;
-        const uint8_t *kp = a.k_pool + base, *vp = a.v_pool + base;
+        const uint8_t *p = a.k_pool + base_of(a, kvh, page, in_page);
+        const int64_t half = 16 * a.c.stride_token * ES;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i)
-                k[t][i] = *reinterpret_cast<const u32x4 *>(kp + t * 16 * row + i * 64 + k_lane);
+            for (int i = 0; i < kLoads; ++i) k[t][i] = *reinterpret_cast<const u32x4 *>(p + t * half + i * 64 + lane);
+        ks = 1.f;
+        if (E4M3) ks = a.k_scale[((int64_t)page * a.c.n_kv_heads + kvh) * a.page_blocks + in_page];
+    }
+
+    __device__ __forceinline__ void load_values(const AttendArgs &a, int kvh, int page, uint32_t blk, uint32_t lane)
+    {
+        const uint32_t in_page = blk - page_of_block(a, blk) * (uint32_t)a.page_blocks;
+        const uint8_t *p = a.v_pool + base_of(a, kvh, page, in_page);
+        const int64_t row = a.c.stride_token * ES;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const uint8_t *p = vp + ((j & 3) + (j >> 2) * 16) * row + v_lane;
-            if constexpr (kLoads == 1) v[j][0] = *reinterpret_cast<const uint32_t *>(p);
+            const uint8_t *x = p + ((j & 3) + (j >> 2) * 16) * row + lane;
+            if constexpr (kLoads == 1) v[j][0] = *reinterpret_cast<const uint32_t *>(x);
             else if constexpr (kLoads == 2) {
-                const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
+                const u32x2 w = *reinterpret_cast<const u32x2 *>(x);
                 v[j][0] = w[0];
                 v[j][1] = w[1];
             } else {
-                const u32x4 w = *reinterpret_cast<const u32x4 *>(p);
+                const u32x4 w = *reinterpret_cast<const u32x4 *>(x);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[j][i] = w[i];
             }
         }
-        ks = vs = 1.f;
-        if (E4M3) {
-            const int64_t at = ((int64_t)page * a.c.n_kv_heads + kvh) * a.page_blocks + in_page;
-            ks = a.k_scale[at];
-            vs = a.v_scale[at];
-        }
+        vs = 1.f;
+        if (E4M3) vs = a.v_scale[((int64_t)page * a.c.n_kv_heads + kvh) * a.page_blocks + in_page];
     }
 
     // Elements of step s of tile t's rows.
@@ -191,11 +210,11 @@ struct Block {
     }
 
     // Values of tokens outside [lo, hi) may be NaN: they become zero.
-    __device__ __forceinline__ void clear_values(int g, int64_t first, int64_t lo, int64_t hi)
+    __device__ __forceinline__ void clear_values(int g, int first, int lo, int hi)
     {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int64_t key = first + 4 * g + (j & 3) + (j >> 2) * 16;
+            const int key = first + 4 * g + (j & 3) + (j >> 2) * 16;
             if (key < lo || key >= hi)
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) v[j][i] = 0;
@@ -260,37 +279,127 @@ struct Rows {
     }
 };
 
-// Bound by the bytes of the cache. Four waves take every fourth block of 32 tokens of the workgroup's split; a wave holds its rows'
+// A value that is the same in all lanes, as a scalar.
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)x >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// Where a stretch of work begins: the unit `pos` lies in item `item`, whose units begin at `before`; all items have `total`.
+struct Start {
+    int item;
+    int64_t pos, before, total, each;
+};
+
+// Items 0 .. count - 1 have units(item) units each; workgroup `share` of `shares` takes `each` of them (at least `least`). The first
+// workgroup leaves the items' beginnings in before[0 .. count] for the joining launch.
+template <int THREADS, class Units>
+__device__ __forceinline__ Start start_of(int share, int shares, int count, int64_t times, int64_t least, int64_t *before, Units units)
+{
+    __shared__ int64_t wave_sum[THREADS / 64], found_before;
+    __shared__ int found_item;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    Start s;
+    if (count <= 64) {                                      // every wave for itself
+        const int64_t sum = lane < count ? units(lane) : 0;
+        int64_t upto = sum;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int64_t y = __shfl_up(upto, o);
+            if (lane >= o) upto += y;
+        }
+        s.total = uniform(__shfl(upto, 63));
+        s.each = (s.total * times + shares - 1) / shares;
+        s.each = s.each < least ? least : s.each;
+        s.pos = share * s.each;
+        const int64_t at = times == 1 || s.total == 0 ? s.pos : s.pos % s.total;
+        const uint64_t in = __ballot(at >= upto - sum && at < upto);
+        s.item = in ? __ffsll((unsigned long long)in) - 1 : 0;
+        s.before = uniform(__shfl(upto - sum, s.item));
+        if (share == 0 && tid < count) before[tid] = upto - sum;
+        if (share == 0 && tid == 0) before[count] = s.total;
+        return s;
+    }
+    const int each_items = (count + THREADS - 1) / THREADS, i0 = min(tid * each_items, count), i1 = min(i0 + each_items, count);
+    int64_t sum = 0;
+    for (int i = i0; i < i1; ++i) sum += units(i);
+    int64_t upto = sum;                                     // inclusive within the wave
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t y = __shfl_up(upto, o);
+        if (lane >= o) upto += y;
+    }
+    if (lane == 63) wave_sum[wave] = upto;
+    __syncthreads();
+    int64_t base = upto - sum, total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+        if (w < wave) base += wave_sum[w];
+        total += wave_sum[w];
+    }
+    total = uniform(total);
+    s.total = total;
+    s.each = (total * times + shares - 1) / shares;
+    s.each = s.each < least ? least : s.each;
+    s.pos = share * s.each;
+    const int64_t at = times == 1 || total == 0 ? s.pos : s.pos % total;
+    if (at >= base && at < base + sum) {
+        int64_t x = base;
+        int i = i0;
+        for (int64_t n = units(i); at >= x + n; n = units(i)) {
+            x += n;
+            ++i;
+        }
+        found_item = i;
+        found_before = x;
+    }
+    if (share == 0) {
+        int64_t x = base;
+        for (int i = i0; i < i1; ++i) {
+            before[i] = x;
+            x += units(i);
+        }
+        if (tid == 0) before[count] = total;
+    }
+    __syncthreads();
+    s.item = __builtin_amdgcn_readfirstlane(found_item);
+    s.before = uniform(found_before);
+    return s;
+}
+
+// Blocks of request b for sp_attend_few_kernel; one for a request that sees nothing, whose rows are still written.
+template <int D>
+__device__ __forceinline__ int few_blocks(const AttendArgs &a, int b)
+{
+    const Range g = range_of(a, b);
+    if (g.n == 0 || g.n > few_rows_of(D) / a.c.group) return 0;
+    const int n = (g.hi + kBlock - 1) / kBlock - g.lo / kBlock;
+    return n < 1 ? 1 : n;
+}
+
+// Bound by the bytes of the cache. Four waves take every fourth block of 32 tokens of a stretch; a wave holds its rows'
 // statistics and output by itself and loads a block ahead, the four meet in LDS at the end.
+// Blocks [k0, k1) of request b and kv head kvh; `slot` of the partial results, or -1 if that is all of them.
 template <int D, bool E4M3, int MT>
-__global__ __launch_bounds__(kThreads) void sp_attend_few_kernel(AttendArgs a)
+__device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh, int k0, int k1, int slot)
 {
     constexpr int kSteps = D / 32, kTiles = D / 16;
     __shared__ float merge_o[2][16 * MT][D];
     __shared__ f32x2 merge_ml[2][16 * MT];
-    const int b = blockIdx.z, kvh = blockIdx.y, split = blockIdx.x, G = a.c.group;
+    const int G = a.c.group;
     const Range rg = range_of(a, b);
-    if (rg.n == 0 || rg.n * G > kFewRows) return;
-    const int rows = (int)rg.n * G;
-    const int64_t blk_lo = rg.lo / kBlock, blk_hi = (rg.hi + kBlock - 1) / kBlock;
-    const int64_t from = blk_lo + (int64_t)split * a.split_blocks;
-    const int64_t to = from + a.split_blocks < blk_hi ? from + a.split_blocks : blk_hi;
-    if (from >= to && split > 0) return;
-
+    const int rows = rg.n * G;
+    const int blk_lo = rg.lo / kBlock, blk_hi = (rg.hi + kBlock - 1) / kBlock;
+    const int from = blk_lo + k0, to = min(blk_lo + k1, blk_hi);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
     const float scale2 = a.scale * kLog2e;
     bf16x8 q[MT][kSteps];
-    int64_t first[MT], last[MT];
+    int last[MT];                           // row c of tile t sees keys [last - window or 0, last)
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         const int r = 16 * t + c, token = r / G, head = kvh * G + r % G;
-        first[t] = rg.lo;
-        last[t] = rg.hi;
-        if (a.causal) {
-            const int64_t p = rg.len - rg.n + token;
-            last[t] = p + 1;
-            first[t] = a.window > 0 && p - a.window + 1 > 0 ? p - a.window + 1 : 0;
-        }
+        last[t] = a.causal ? rg.len - rg.n + token + 1 : rg.hi;
         const uint16_t *src = a.q + ((a.off[b] + token) * a.c.n_q_heads + head) * D;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
@@ -301,58 +410,70 @@ __global__ __launch_bounds__(kThreads) void sp_attend_few_kernel(AttendArgs a)
         }
     }
     // every row sees the keys of [all_lo, all_hi)
-    const int64_t all_lo = a.causal && a.window > 0 && rg.len - a.window > 0 ? rg.len - a.window : 0;
-    const int64_t all_hi = a.causal ? rg.len - rg.n + 1 : rg.hi;
+    const int all_lo = a.causal && a.window > 0 && rg.len - a.window > 0 ? rg.len - a.window : 0;
+    const int all_hi = a.causal ? rg.len - rg.n + 1 : rg.hi;
 
     Rows<D, MT> acc;
     acc.clear();
     const uint32_t row_bytes = (uint32_t)a.c.stride_token * (E4M3 ? 1 : 2);
     const uint32_t k_lane = c * row_bytes + 16 * g, v_lane = 4 * g * row_bytes + c * (D / 16) * (E4M3 ? 1 : 2);
-    Block<D, E4M3> cur, nxt;
-    int64_t blk = from + wave;
+    // The next block's keys are loaded once this one's are in the first product, its values once these are in operand form.
+    Block<D, E4M3> kv;
+    int blk = from + wave;
     if (blk < to) {
-        cur.load(a, kvh, page_at(a, b, (uint32_t)blk), (uint32_t)blk, k_lane, v_lane);
-        int page = page_at(a, b, (uint32_t)(blk + kWaves < to ? blk + kWaves : blk));
-        for (; blk < to; blk += kWaves) {
-            const int64_t ahead = blk + kWaves < to ? blk + kWaves : blk, later = ahead + kWaves < to ? ahead + kWaves : ahead;
-            nxt.load(a, kvh, page, (uint32_t)ahead, k_lane, v_lane);
-            page = page_at(a, b, (uint32_t)later);
-
-            bf16x8 kf[2][kSteps], vf[kTiles];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int s = 0; s < kSteps; ++s) kf[t][s] = cur.key(t, s);
-            const int64_t key0 = blk * kBlock;
+        const auto next = [&](int x) { return x + kWaves < to ? x + kWaves : x; };
+        int page = page_at(a, b, (uint32_t)blk);
+        kv.load_keys(a, kvh, page, (uint32_t)blk, k_lane);
+        kv.load_values(a, kvh, page, (uint32_t)blk, v_lane);
+        page = page_at(a, b, (uint32_t)next(blk));
+        for (;;) {
+            const int ahead = next(blk), key0 = blk * kBlock;
+            const int page2 = page_at(a, b, (uint32_t)next(ahead));
             const bool whole = key0 >= all_lo && key0 + kBlock <= all_hi;
-            if (!whole) cur.clear_values(g, key0, rg.lo, rg.hi);
-            cur.values(vf);
-            const float sc = scale2 * cur.ks;
+            f32x4 s0[MT], s1[MT];
+            {
+                bf16x8 kf[2][kSteps];
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int s = 0; s < kSteps; ++s) kf[t][s] = kv.key(t, s);
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    s0[t] = s1[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int s = 0; s < kSteps; ++s) {
+                        s0[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[0][s], q[t][s], s0[t], 0, 0, 0);
+                        s1[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[1][s], q[t][s], s1[t], 0, 0, 0);
+                    }
+                }
+            }
+            const float sc = scale2 * kv.ks, vs = kv.vs;
+            kv.load_keys(a, kvh, page, (uint32_t)ahead, k_lane);
+            bf16x8 vf[kTiles];
+            if (!whole) kv.clear_values(g, key0, rg.lo, rg.hi);
+            kv.values(vf);
+            kv.load_values(a, kvh, page, (uint32_t)ahead, v_lane);
+            page = page2;
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
-                f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
-#pragma unroll
-                for (int s = 0; s < kSteps; ++s) {
-                    s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[0][s], q[t][s], s0, 0, 0, 0);
-                    s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[1][s], q[t][s], s1, 0, 0, 0);
-                }
                 float x[8];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    x[j] = s0[j] * sc;
-                    x[4 + j] = s1[j] * sc;
+                    x[j] = s0[t][j] * sc;
+                    x[4 + j] = s1[t][j] * sc;
                 }
                 if (!whole)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const int64_t key = key0 + 4 * g + (j & 3) + (j >> 2) * 16;
-                        if (key < first[t] || key >= last[t]) x[j] = neg_inf();
+                        const int key = key0 + 4 * g + (j & 3) + (j >> 2) * 16;
+                        if (key >= last[t] || (a.window > 0 && key < last[t] - a.window)) x[j] = neg_inf();
                     }
-                const bf16x8 p = acc.weigh(t, x, cur.vs);
+                const bf16x8 p = acc.weigh(t, x, vs);
 #pragma unroll
                 for (int i = 0; i < kTiles; ++i) acc.o[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], p, acc.o[t][i], 0, 0, 0);
             }
-            cur = nxt;
+            if (ahead == blk) break;
+            blk = ahead;
         }
     }
 #pragma unroll
@@ -392,10 +513,10 @@ __global__ __launch_bounds__(kThreads) void sp_attend_few_kernel(AttendArgs a)
     for (int t = 0; t < MT; ++t) {
         const int r = 16 * t + c;
         if (r >= rows) continue;
-        if (a.splits > 1) {
-            const int64_t at = (((int64_t)split * a.B + b) * a.c.n_kv_heads + kvh) * a.few_rows + r;
-            if (g == 0) a.part_ml[at] = f32x2{acc.m[t], acc.l[t]};
-            float *dst = a.part_o + at * D + 4 * g * kTiles;
+        if (slot >= 0) {
+            const int64_t at = (int64_t)slot * a.few_rows + r;
+            if (g == 0) a.few_ml[at] = f32x2{acc.m[t], acc.l[t]};
+            float *dst = a.few_o + at * D + 4 * g * kTiles;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -414,51 +535,105 @@ __global__ __launch_bounds__(kThreads) void sp_attend_few_kernel(AttendArgs a)
     }
 }
 
-// Joins `count` splits of one row, the first at index `at` of the workspace's rows and `step` rows apart: their weights exp2(m_s - m)
-// first, then the weighted sum, the splits shared out among the waves.
-template <int D>
-__device__ __forceinline__ void join_row(const AttendArgs &a, const f32x2 *ml, const float *po, int64_t at, int64_t step, int count, int64_t row)
+constexpr int kFewLeast = 16;       // blocks of a stretch: four for each wave
+
+template <int D, bool E4M3, int MT, bool SHARED>
+__global__ __launch_bounds__(kThreads, D == 128 && MT > 1 ? 1 : 2) void sp_attend_few_kernel(AttendArgs a)
+{
+    const int kv = a.c.n_kv_heads, share = blockIdx.x;
+    int64_t pos = 0, end, begin = 0;        // units of work; `begin` of them before request b
+    int b;
+    if constexpr (!SHARED) {                // a line each
+        b = share / kv;
+        const int n = few_blocks<D>(a, b);
+        pos = (int64_t)(share % kv) * n;
+        end = pos + n;
+    } else {
+        const Start s = start_of<kThreads>(share, a.few_shares, a.B, 1, kFewLeast, a.few_before, [&](int i) { return (int64_t)few_blocks<D>(a, i) * kv; });
+        b = s.item;
+        begin = s.before;
+        pos = s.pos;
+        end = min(s.pos + s.each, s.total);
+    }
+    for (int part = 0; pos < end; ++part) {
+        const int n = few_blocks<D>(a, b);
+        if (pos >= begin + (int64_t)n * kv) {
+            begin += (int64_t)n * kv;
+            ++b;
+            --part;
+            continue;
+        }
+        const int rel = (int)(pos - begin), kvh = rel / n, k0 = rel % n, k1 = (int)min((int64_t)n, k0 + (end - pos));
+        few_stretch<D, E4M3, MT>(a, b, kvh, k0, k1, k0 == 0 && k1 == n ? -1 : 2 * share + (part > 0));
+        pos += k1 - k0;
+        __syncthreads();                    // the merge's LDS is used again
+    }
+}
+
+// Joins the partial results of one row: units [begin, end) of the work, `each` to a workgroup, `rows` rows in a partial result. WAVES waves
+// share them out; their weights exp2(m_s - m) come first, then the weighted sum.
+template <int D, int WAVES>
+__device__ __forceinline__ void join_row(const AttendArgs &a, const f32x2 *ml, const float *po, int rows, int r, int64_t begin, int64_t end,
+                                         int64_t each, int64_t row)
 {
     __shared__ float part[kWaves][D];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, part_wave = wave % WAVES;
+    const int i0 = (int)(begin / each), i1 = (int)((end - 1) / each), count = i1 - i0 + 1;
+    // a line that begins inside a workgroup's stretch is that workgroup's second partial result
+    const int first = 2 * i0 + (begin != i0 * each);
+    const auto at = [&](int s) { return (int64_t)(s == 0 ? first : 2 * (i0 + s)) * rows + r; };
     float m = neg_inf();
-    for (int s = lane; s < count; s += 64) m = fmaxf(m, ml[at + s * step][0]);
+    for (int s = lane; s < count; s += 64) m = fmaxf(m, ml[at(s)][0]);
 #pragma unroll
     for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    float l = 0.f;
-    for (int s = lane; s < count; s += 64) {
-        const f32x2 x = ml[at + s * step];
-        if (x[0] != neg_inf()) l += x[1] * exp2_(x[0] - m);
+    float l = 0.f, acc[D / 64] = {};
+    for (int s0 = 0; s0 < count; s0 += 64) {
+        float w = 0.f;
+        if (s0 + lane < count) {
+            const f32x2 x = ml[at(s0 + lane)];
+            w = x[0] == neg_inf() ? 0.f : exp2_(x[0] - m);
+            l += x[1] * w;
+        }
+        const int n = min(64, count - s0);
+        for (int s = part_wave; s < n; s += WAVES) {
+            const float f = __shfl(w, s);
+            const float *src = po + at(s0 + s) * D + lane;
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) acc[i] += src[64 * i] * f;
+        }
     }
 #pragma unroll
     for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o);
-    float acc[D / 64] = {};
-    for (int s = wave; s < count; s += kWaves) {
-        const float ms = ml[at + s * step][0], f = ms == neg_inf() ? 0.f : exp2_(ms - m);
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    if (WAVES > 1) {
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) acc[i] += po[(at + s * step) * D + lane + 64 * i] * f;
+        for (int i = 0; i < D / 64; ++i) part[wave][lane + 64 * i] = acc[i];
+        __syncthreads();
+        if (wave != 0) return;
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+            acc[i] = part[0][lane + 64 * i];
+            for (int w = 1; w < WAVES; ++w) acc[i] += part[w][lane + 64 * i];
+        }
     }
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) part[wave][lane + 64 * i] = acc[i];
-    __syncthreads();
-    if (tid < D) {
-        const float o = ((part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid])) * (l > 0.f ? 1.f / l : 0.f);
-        a.out[row * D + tid] = __builtin_bit_cast(uint16_t, (__bf16)o);
-    }
-    if (a.lse && tid == 0) a.lse[row] = l > 0.f ? (m + log2_(l)) * kLn2 : neg_inf();
+    for (int i = 0; i < D / 64; ++i) a.out[row * D + lane + 64 * i] = __builtin_bit_cast(uint16_t, (__bf16)(acc[i] * inv));
+    if (a.lse && lane == 0) a.lse[row] = l > 0.f ? (m + log2_(l)) * kLn2 : neg_inf();
 }
 
+// Row r of every kv head and request whose line lies in more than one stretch.
 template <int D>
-__global__ __launch_bounds__(kThreads) void sp_attend_join_kernel(AttendArgs a)
+__global__ __launch_bounds__(kThreads) void sp_attend_few_join_kernel(AttendArgs a)
 {
     const int b = blockIdx.z, kvh = blockIdx.y, r = blockIdx.x, G = a.c.group;
-    const Range rg = range_of(a, b);
-    if (rg.n * G > kFewRows || r >= rg.n * G) return;
-    const int64_t blocks = (rg.hi + kBlock - 1) / kBlock - rg.lo / kBlock;
-    int count = (int)((blocks + a.split_blocks - 1) / a.split_blocks);
-    count = count < 1 ? 1 : (count > a.splits ? a.splits : count);          // split 0 always writes
-    const int64_t at = ((int64_t)b * a.c.n_kv_heads + kvh) * a.few_rows + r, step = (int64_t)a.B * a.c.n_kv_heads * a.few_rows;
-    join_row<D>(a, a.part_ml, a.part_o, at, step, count, (a.off[b] + r / G) * a.c.n_q_heads + kvh * G + r % G);
+    const int64_t before = a.few_before[b], total = a.few_before[a.B];
+    const int n = (int)((a.few_before[b + 1] - before) / a.c.n_kv_heads), rows = (int)min((int64_t)few_rows_of(D) + 1, a.off[b + 1] - a.off[b]) * G;
+    if (n == 0 || r >= rows) return;
+    int64_t each = (total + a.few_shares - 1) / a.few_shares;
+    each = each < kFewLeast ? kFewLeast : each;
+    const int64_t begin = before + (int64_t)kvh * n, end = begin + n;
+    if (begin / each == (end - 1) / each) return;
+    join_row<D, kWaves>(a, a.few_ml, a.few_o, a.few_rows, r, begin, end, each, (a.off[b] + r / G) * a.c.n_q_heads + kvh * G + r % G);
 }
 
 // ---- many rows: prompt chunks -----------------------------------------------------------------------------------------
@@ -473,10 +648,10 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 struct Tile {
     Range rg;
     int b, row0, rows;              // rows of this tile
-    int64_t lo, hi;
+    int lo, hi;
 };
 
-__device__ __forceinline__ bool tile_of(const AttendArgs &a, int x, Tile *t)
+__device__ __forceinline__ bool tile_of(const AttendArgs &a, int few_rows, int x, Tile *t)
 {
     const int G = a.c.group;
     int lo = 0, hi = a.many_count ? a.many_count : a.B;
@@ -487,14 +662,14 @@ __device__ __forceinline__ bool tile_of(const AttendArgs &a, int x, Tile *t)
     }
     t->b = a.many_count ? a.many_b[lo] : lo;
     t->rg = range_of(a, t->b);
-    const int64_t row0 = (x - (a.many_count ? a.many_tile[lo] : a.off[lo] * G / kManyRows + lo)) * kManyRows, rows = t->rg.n * G - row0;
-    if (t->rg.n * G <= kFewRows || rows <= 0) return false;
+    const int64_t row0 = (x - (a.many_count ? a.many_tile[lo] : a.off[lo] * G / kManyRows + lo)) * kManyRows, rows = (int64_t)t->rg.n * G - row0;
+    if (t->rg.n <= few_rows / G || rows <= 0) return false;
     t->row0 = (int)row0;
     t->rows = (int)(rows < kManyRows ? rows : kManyRows);
     t->lo = 0;
     t->hi = t->rg.len;
     if (a.causal) {
-        const int64_t p0 = t->rg.len - t->rg.n + t->row0 / G, p1 = t->rg.len - t->rg.n + (t->row0 + t->rows - 1) / G;
+        const int p0 = t->rg.len - t->rg.n + t->row0 / G, p1 = t->rg.len - t->rg.n + (t->row0 + t->rows - 1) / G;
         t->hi = p1 + 1 > 0 ? p1 + 1 : 0;
         if (a.window > 0 && p0 - a.window + 1 > 0) t->lo = p0 - a.window + 1;
     }
@@ -514,9 +689,11 @@ struct Stage {
     static constexpr int kKeyLoads = E4M3 ? 1 : 2;              // 16-byte loads of a thread
     static constexpr int kKeyLanes = D * ES / 16;               // threads of a key's row
     static constexpr int kValueLanes = D / 4;                   // threads of four keys' values, four elements each
-    u32x4 k[kKeyLoads];
-    uint32_t v[4][ES];
-    float scale;                                                // thread i < 2 kBlocks: key or value scale of a block
+    struct Raw {                                                // what a thread loads of a tile
+        u32x4 k[kKeyLoads];
+        uint32_t v[4][ES];
+        float scale;                                            // thread i < 2 kBlocks: key or value scale of a block
+    };
     int key_row, key_col, value_key, value_octet, value_half, value_col;
 
     __device__ __forceinline__ Stage()
@@ -531,53 +708,108 @@ struct Stage {
         value_key = 32 * (value_octet >> 2) + 16 * ((value_octet >> 1) & 1) + 4 * (value_octet & 1) + 8 * value_half;
     }
 
-    // Pages of the blocks that this wave loads from, for the tile that begins at block blk.
-    struct Pages {
-        int key[kKeyLoads], value, scale;
+    // Where a wave loads from, tile after tile: a pointer that moves along a page and is looked up again at its end. Behind the last
+    // page it stays where it is: what is loaded there is masked.
+    struct Cursor {
+        const uint8_t *p;
+        uint32_t in, page;                                      // block of the page; place in the block table
     };
 
-    __device__ __forceinline__ int block_of_keys(int i) const
+    __device__ __forceinline__ static const uint8_t *place(const AttendArgs &a, const uint8_t *pool, int b, int kvh, const Cursor &c)
     {
-        return __builtin_amdgcn_readfirstlane((key_row + i * (kManyThreads / kKeyLanes)) / kBlock);
+        return pool + (page_entry(a, b, c.page) * a.c.page_stride + kvh * a.c.stride_head + (int64_t)(c.in * kBlock) * a.c.stride_token) * ES;
     }
 
-    __device__ __forceinline__ Pages pages(const AttendArgs &a, int b, uint32_t blk, uint32_t last) const
+    __device__ __forceinline__ static Cursor cursor(const AttendArgs &a, const uint8_t *pool, int b, int kvh, uint32_t blk, uint32_t last_page)
     {
-        Pages p;
+        Cursor c;
+        c.page = page_of_block(a, blk);
+        c.in = blk - c.page * (uint32_t)a.page_blocks;
+        if (c.page > last_page) {                               // a tile's end behind the last page
+            c.page = last_page;
+            c.in = 0;
+        }
+        c.p = place(a, pool, b, kvh, c);
+        return c;
+    }
+
+    __device__ __forceinline__ static void advance(const AttendArgs &a, const uint8_t *pool, int b, int kvh, uint32_t last_page, Cursor &c)
+    {
+        c.in += kBlocks;
+        if (c.in < (uint32_t)a.page_blocks) {
+            c.p += (int64_t)kKeys * a.c.stride_token * ES;
+            return;
+        }
+        uint32_t page = c.page;
+        do {
+            c.in -= a.page_blocks;
+            ++page;
+        } while (c.in >= (uint32_t)a.page_blocks);
+        if (page > last_page) return;
+        c.page = page;
+        c.p = place(a, pool, b, kvh, c);
+    }
+
+    struct Cursors {
+        Cursor key[kKeyLoads], value;
+        const float *scale;                                     // of thread i < 2 kBlocks: key or value scale of block i % kBlocks
+        uint32_t scale_in, scale_page;
+    };
+
+    __device__ __forceinline__ static const float *scale_place(const AttendArgs &a, int b, int kvh, const Cursors &c)
+    {
+        const float *scales = threadIdx.x < kBlocks ? a.k_scale : a.v_scale;
+        return scales + ((int64_t)page_entry(a, b, c.scale_page) * a.c.n_kv_heads + kvh) * a.page_blocks + c.scale_in;
+    }
+
+    __device__ __forceinline__ Cursors cursors(const AttendArgs &a, int b, int kvh, uint32_t blk, uint32_t last_page) const
+    {
+        Cursors c;
 #pragma unroll
-        for (int i = 0; i < kKeyLoads; ++i) p.key[i] = page_at(a, b, min(blk + block_of_keys(i), last));
-        p.value = page_at(a, b, min(blk + __builtin_amdgcn_readfirstlane(value_octet >> 2), last));
-        p.scale = 0;
-        if (E4M3 && threadIdx.x < 2 * kBlocks) p.scale = page_at(a, b, min(blk + threadIdx.x % kBlocks, last));
-        return p;
+        for (int i = 0; i < kKeyLoads; ++i)
+            c.key[i] = cursor(a, a.k_pool, b, kvh, blk + __builtin_amdgcn_readfirstlane((key_row + i * (kManyThreads / kKeyLanes)) / kBlock), last_page);
+        c.value = cursor(a, a.v_pool, b, kvh, blk + __builtin_amdgcn_readfirstlane(value_octet >> 2), last_page);
+        if (E4M3) {
+            const uint32_t mine = blk + threadIdx.x % kBlocks;
+            c.scale_page = min(page_of_block(a, mine), last_page);
+            c.scale_in = mine - page_of_block(a, mine) * (uint32_t)a.page_blocks;
+            c.scale = scale_place(a, b, kvh, c);
+        }
+        return c;
     }
 
-    // Blocks behind the last one are read as the last one: they are masked.
-    __device__ __forceinline__ void load(const AttendArgs &a, int kvh, const Pages &p, uint32_t blk, uint32_t last)
+    // Loads the tile at the cursors and moves them to the next.
+    __device__ __forceinline__ void load(const AttendArgs &a, int b, int kvh, uint32_t last_page, Cursors &c, Raw &w) const
     {
         const int64_t row = a.c.stride_token * ES;
 #pragma unroll
         for (int i = 0; i < kKeyLoads; ++i) {
-            const uint32_t at = min(blk + block_of_keys(i), last), in_page = at - page_of_block(a, at) * (uint32_t)a.page_blocks;
-            const uint8_t *base = a.k_pool + (p.key[i] * a.c.page_stride + kvh * a.c.stride_head + (int64_t)(in_page * kBlock) * a.c.stride_token) * ES;
-            const uint32_t r = (key_row + i * (kManyThreads / kKeyLanes)) % kBlock;
-            k[i] = *reinterpret_cast<const u32x4 *>(base + r * (uint32_t)row + key_col * 16);
+            const uint32_t lane = (key_row + i * (kManyThreads / kKeyLanes)) % kBlock * (uint32_t)row + key_col * 16;
+            w.k[i] = *reinterpret_cast<const u32x4 *>(c.key[i].p + lane);
+            advance(a, a.k_pool, b, kvh, last_page, c.key[i]);
         }
-        const uint32_t at = min(blk + __builtin_amdgcn_readfirstlane(value_octet >> 2), last), in_page = at - page_of_block(a, at) * (uint32_t)a.page_blocks;
-        const uint8_t *base = a.v_pool + (p.value * a.c.page_stride + kvh * a.c.stride_head + (int64_t)(in_page * kBlock) * a.c.stride_token) * ES;
-        const uint32_t lane = (value_key % kBlock) * (uint32_t)row + value_col * 4 * ES;
+        const uint32_t lane = value_key % kBlock * (uint32_t)row + value_col * 4 * ES;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if constexpr (E4M3) v[j][0] = *reinterpret_cast<const uint32_t *>(base + j * row + lane);
+            if constexpr (E4M3) w.v[j][0] = *reinterpret_cast<const uint32_t *>(c.value.p + j * row + lane);
             else {
-                const u32x2 w = *reinterpret_cast<const u32x2 *>(base + j * row + lane);
-                v[j][0] = w[0];
-                v[j][1] = w[1];
+                const u32x2 x = *reinterpret_cast<const u32x2 *>(c.value.p + j * row + lane);
+                w.v[j][0] = x[0];
+                w.v[j][1] = x[1];
             }
         }
+        advance(a, a.v_pool, b, kvh, last_page, c.value);
         if (E4M3 && threadIdx.x < 2 * kBlocks) {
-            const uint32_t sb = min(blk + threadIdx.x % kBlocks, last), in = sb - page_of_block(a, sb) * (uint32_t)a.page_blocks;
-            scale = (threadIdx.x < kBlocks ? a.k_scale : a.v_scale)[((int64_t)p.scale * a.c.n_kv_heads + kvh) * a.page_blocks + in];
+            w.scale = *c.scale;
+            c.scale += kBlocks;
+            c.scale_in += kBlocks;
+            if (c.scale_in >= (uint32_t)a.page_blocks) {
+                do {
+                    c.scale_in -= a.page_blocks;
+                    c.scale_page = min(c.scale_page + 1, last_page);
+                } while (c.scale_in >= (uint32_t)a.page_blocks);
+                c.scale = scale_place(a, b, kvh, c);
+            }
         }
     }
 
@@ -586,8 +818,10 @@ struct Stage {
     static __device__ __forceinline__ int value_slot(int d, int o) { return d * (kKeys / 8) + (o ^ ((d ^ (d >> 2)) & 7)); }
 
     // Values of keys outside [lo, hi) become zero; `first` is the tile's first key.
-    __device__ __forceinline__ void store(u32x4 *keys, u32x4 *values, float *scales, int64_t first, int64_t lo, int64_t hi)
+    __device__ __forceinline__ void store(Raw &w, u32x4 *keys, u32x4 *values, float *scales, int first, int lo, int hi) const
     {
+        auto &k = w.k;
+        auto &v = w.v;
 #pragma unroll
         for (int i = 0; i < kKeyLoads; ++i) {
             const int r = key_row + i * (kManyThreads / kKeyLanes);
@@ -600,7 +834,7 @@ struct Stage {
         if (first < lo || first + kKeys > hi)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int64_t key = first + value_key + j;
+                const int key = first + value_key + j;
                 if (key < lo || key >= hi)
 #pragma unroll
                     for (int i = 0; i < ES; ++i) v[j][i] = 0;
@@ -623,45 +857,44 @@ struct Stage {
                 }
 #pragma unroll
         for (int i = 0; i < 4; ++i) reinterpret_cast<u32x2 *>(values)[2 * value_slot(4 * value_col + i, value_octet) + value_half] = r[i];
-        if (E4M3 && threadIdx.x < 2 * kBlocks) scales[threadIdx.x] = scale;
+        if (E4M3 && threadIdx.x < 2 * kBlocks) scales[threadIdx.x] = w.scale;
     }
 };
 
+// Tiles of keys that a tile of rows sees; one for a tile that sees nothing, whose rows are still written.
+template <int D>
+__device__ __forceinline__ int many_units(const Tile &t)
+{
+    constexpr int kKeys = 8192 / D;
+    const int n = (t.hi + kKeys - 1) / kKeys - t.lo / kKeys;
+    return t.hi <= t.lo || n < 1 ? 1 : n;
+}
+
+// Tiles [k0, k1) of the keys that tile t of query rows sees; `slot` of the partial results, or -1 if that is all of them.
 template <int D, bool E4M3>
-__global__ __launch_bounds__(kManyThreads) void sp_attend_many_kernel(AttendArgs a)
+__device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t, int kvh, int k0, int k1, int slot)
 {
     using S = Stage<D, E4M3>;
     constexpr int kKeys = S::kKeys, kBlocks = S::kBlocks, kSteps = D / 16, kOut = D / 32;
     constexpr float kSlack = 8.f;
     __shared__ u32x4 keys[2][1024], values[2][1024];            // 16 KB each
     __shared__ float scales[2][2 * kBlocks];
-    // neighbouring workgroups take different kv heads: with eight of them, each die's L2 holds one head's cache
-    const int kvh = blockIdx.x % a.c.n_kv_heads, rest = blockIdx.x / a.c.n_kv_heads;
-    const int x = a.tiles - 1 - rest % a.tiles, split = rest / a.tiles;     // later tiles of a prompt see more: they go first
-    Tile t;
-    if (!tile_of(a, x, &t)) return;
-    const int64_t tile0 = t.lo / kKeys * kKeys;                 // first key of the first tile of keys
-    const int64_t from = tile0 + (int64_t)split * a.many_keys;
-    const int64_t to = from + a.many_keys < t.hi ? from + a.many_keys : t.hi;
-    if (from >= to && split > 0) return;
-
+    const int from = (t.lo / kKeys + k0) * kKeys, to = min((t.lo / kKeys + k1) * kKeys, t.hi);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = lane >> 5, c = lane & 31;
     const int G = a.c.group, r = 32 * wave + c;                 // this lane's row of the tile
     const int token = (t.row0 + r) / G, head = kvh * G + (t.row0 + r) % G;
     const int64_t row = (a.off[t.b] + token) * a.c.n_q_heads + head;
-    int64_t first = 0, last = t.rg.len;
-    // keys that every row of this wave sees: [all_lo, all_hi); that some row sees: up to any_hi
-    int64_t all_lo = 0, all_hi = t.rg.len, any_hi = t.rg.len, any_lo = 0;
+    int last = t.rg.len;                    // this lane's row sees keys [last - window or 0, last)
+    // keys that every row of this wave sees: [all_lo, all_hi); that some row sees: [any_lo, any_hi)
+    int all_lo = 0, all_hi = t.rg.len, any_hi = t.rg.len, any_lo = 0;
     if (a.causal) {
-        const int64_t p = t.rg.len - t.rg.n;
+        const int p = t.rg.len - t.rg.n;
         last = p + token + 1;
-        first = a.window > 0 && last - a.window > 0 ? last - a.window : 0;
-        const int64_t low = p + (t.row0 + 32 * wave) / G + 1, high = p + (t.row0 + 32 * wave + 31) / G + 1;
-        all_hi = low;
-        any_hi = high;
+        all_hi = p + (t.row0 + 32 * wave) / G + 1;
+        any_hi = p + (t.row0 + 32 * wave + 31) / G + 1;
         if (a.window > 0) {
-            all_lo = high - a.window;
-            any_lo = low - a.window;
+            all_lo = any_hi - a.window;
+            any_lo = all_hi - a.window;
         }
     }
     const bool busy = 32 * wave < t.rows;
@@ -684,48 +917,60 @@ __global__ __launch_bounds__(kManyThreads) void sp_attend_many_kernel(AttendArgs
     if (from < to) {
         S st;
         const uint32_t last_blk = (uint32_t)((t.hi - 1) / kBlock);
-        uint32_t blk = (uint32_t)(from / kBlock);
-        typename S::Pages pg = st.pages(a, t.b, blk, last_blk);
-        st.load(a, kvh, pg, blk, last_blk);
-        pg = st.pages(a, t.b, blk + kBlocks, last_blk);
-        st.store(keys[0], values[0], scales[0], from, t.lo, t.hi);
+        const uint32_t last_page = page_of_block(a, last_blk);
+        const int last_tile = (to - from + kKeys - 1) / kKeys - 1;
+        typename S::Raw ra, rb;
+        typename S::Cursors cur = st.cursors(a, t.b, kvh, (uint32_t)(from / kBlock), last_page);
+        st.load(a, t.b, kvh, last_page, cur, ra);
+        st.load(a, t.b, kvh, last_page, cur, rb);
+        st.store(ra, keys[0], values[0], scales[0], from, t.lo, t.hi);
         __syncthreads();
-        int buf = 0;
-        for (int64_t key0 = from; key0 < to; key0 += kKeys, buf ^= 1, blk += kBlocks) {
-            const bool more = key0 + kKeys < to;
-            if (more) {
-                st.load(a, kvh, pg, blk + kBlocks, last_blk);
-                pg = st.pages(a, t.b, blk + 2 * kBlocks, last_blk);
-            }
+        // Tile n is taken from buffer n % 2, while tile n + 1 lies in `ready`, loaded or under way, and tile n + 2 is requested into `fresh`.
+        const auto take = [&](int n, int buf, typename S::Raw &ready, typename S::Raw &fresh) {
+            const int key0 = from + n * kKeys;
+            const bool more = n < last_tile;
+            if (n + 2 <= last_tile) st.load(a, t.b, kvh, last_page, cur, fresh);
             if (busy && key0 < any_hi && key0 + kKeys > any_lo) {
                 const bool whole = key0 >= all_lo && key0 + kKeys <= all_hi;
+                // two blocks at a time: two independent chains of the first product, one look at the reference
 #pragma unroll
-                for (int u = 0; u < kBlocks; ++u) {
-                    // blocks that no row of the tile sees: their scales may be anything
-                    if (!whole && (key0 + 32 * u >= t.hi || key0 + 32 * u + 32 <= t.lo)) continue;
-                    f32x16 x;
+                for (int u = 0; u < kBlocks; u += 2) {
+                    f32x16 x[2];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) x[e] = 0.f;
+                    for (int w = 0; w < 2; ++w)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[w][e] = 0.f;
 #pragma unroll
                     for (int s = 0; s < kSteps; ++s)
-                        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, keys[buf][S::key_slot(32 * u + c, 2 * s + h)]), q[s], x, 0, 0, 0);
+#pragma unroll
+                        for (int w = 0; w < 2; ++w)
+                            x[w] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, keys[buf][S::key_slot(32 * (u + w) + c, 2 * s + h)]), q[s], x[w], 0, 0, 0);
                     if (!whole)
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const int64_t key = key0 + 32 * u + 8 * (e >> 2) + 4 * h + (e & 3);
-                            if (key < first || key >= last) x[e] = neg_inf();
-                        }
-                    float sc = scale2, vexp = 0.f, vinv = 1.f;
-                    if (E4M3) {
-                        const float vs = scales[buf][kBlocks + u];
-                        sc *= scales[buf][u];
-                        vexp = log2_(vs);
-                        vinv = 1.f / vs;
-                    }
-                    float top = x[0];
+                        for (int w = 0; w < 2; ++w)
 #pragma unroll
-                    for (int e = 1; e < 16; ++e) top = fmaxf(top, x[e]);
-                    top *= sc;
+                            for (int e = 0; e < 16; ++e) {
+                                const int key = key0 + 32 * (u + w) + 8 * (e >> 2) + 4 * h + (e & 3);
+                                if (key >= last || (a.window > 0 && key < last - a.window)) x[w][e] = neg_inf();
+                            }
+                    float sc[2], vexp[2], vinv[2], top = neg_inf();
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        sc[w] = scale2;
+                        vexp[w] = 0.f;
+                        vinv[w] = 1.f;
+                        // blocks that no row of the tile sees may have any scale: they are masked, and take none
+                        if (E4M3 && (whole || (key0 + 32 * (u + w) < t.hi && key0 + 32 * (u + w) + 32 > t.lo))) {
+                            const float vs = scales[buf][kBlocks + u + w];
+                            sc[w] *= scales[buf][u + w];
+                            vexp[w] = log2_(vs);
+                            vinv[w] = 1.f / vs;
+                        }
+                        float y = x[w][0];
+#pragma unroll
+                        for (int e = 1; e < 16; ++e) y = fmaxf(y, x[w][e]);
+                        top = fmaxf(top, y * sc[w]);
+                    }
                     if (__any(top > m + kSlack)) {
                         const float mx = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
                         const float f = m == neg_inf() ? 0.f : exp2_(m - mx);
@@ -734,34 +979,42 @@ __global__ __launch_bounds__(kManyThreads) void sp_attend_many_kernel(AttendArgs
                         for (int i = 0; i < kOut; ++i) o[i] *= f;
                         m = mx;
                     }
-                    const float ref = (m == neg_inf() ? 0.f : m) - vexp;
-                    float sum = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        x[e] = exp2_(x[e] * sc - ref);
-                        sum += x[e];
-                    }
-                    l += sum * vinv;
+                    for (int w = 0; w < 2; ++w) {
+                        const float ref = (m == neg_inf() ? 0.f : m) - vexp[w];
+                        float sum[2] = {0.f, 0.f};
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const u32x4 w = {pack2(x[8 * k], x[8 * k + 1]), pack2(x[8 * k + 2], x[8 * k + 3]), pack2(x[8 * k + 4], x[8 * k + 5]),
-                                         pack2(x[8 * k + 6], x[8 * k + 7])};
-                        const bf16x8 p = __builtin_bit_cast(bf16x8, w);
+                        for (int e = 0; e < 16; ++e) x[w][e] = exp2_(x[w][e] * sc[w] - ref);
 #pragma unroll
-                        for (int i = 0; i < kOut; ++i)
-                            o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values[buf][S::value_slot(32 * i + c, 4 * u + 2 * k + h)]),
-                                                                          p, o[i], 0, 0, 0);
+                        for (int k = 0; k < 2; ++k) {
+                            u32x4 p;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                p[e] = pack2(x[w][8 * k + 2 * e], x[w][8 * k + 2 * e + 1]);
+                                sum[0] += x[w][8 * k + 2 * e];
+                                sum[1] += x[w][8 * k + 2 * e + 1];
+                            }
+#pragma unroll
+                            for (int i = 0; i < kOut; ++i)
+                                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values[buf][S::value_slot(32 * i + c, 4 * (u + w) + 2 * k + h)]),
+                                                                              __builtin_bit_cast(bf16x8, p), o[i], 0, 0, 0);
+                        }
+                        l += (sum[0] + sum[1]) * vinv[w];
                     }
                 }
             }
-            if (more) st.store(keys[buf ^ 1], values[buf ^ 1], scales[buf ^ 1], key0 + kKeys, t.lo, t.hi);
+            if (more) st.store(ready, keys[buf ^ 1], values[buf ^ 1], scales[buf ^ 1], key0 + kKeys, t.lo, t.hi);
             __syncthreads();
+        };
+        for (int n = 0; n <= last_tile; n += 2) {
+            take(n, 0, rb, ra);
+            if (n < last_tile) take(n + 1, 1, ra, rb);
         }
     }
     l += __shfl_xor(l, 32);
     if (r >= t.rows) return;
-    if (a.many_splits > 1) {
-        const int64_t at = (((int64_t)split * a.tiles + x) * a.c.n_kv_heads + kvh) * kManyRows + r;
+    if (slot >= 0) {
+        const int64_t at = (int64_t)slot * kManyRows + r;
         if (h == 0) a.many_ml[at] = f32x2{m, l};
 #pragma unroll
         for (int i = 0; i < kOut; ++i)
@@ -780,58 +1033,96 @@ __global__ __launch_bounds__(kManyThreads) void sp_attend_many_kernel(AttendArgs
     if (a.lse && h == 0) a.lse[row] = l > 0.f ? (m + log2_(l)) * kLn2 : neg_inf();
 }
 
-template <int D, bool E4M3>
+constexpr int kManyLeastTiles = 16;     // tiles of keys of a stretch: worth writing 256 rows of partial results
+
+template <int D, bool E4M3, bool SHARED>
+__global__ __launch_bounds__(kManyThreads) void sp_attend_many_kernel(AttendArgs a)
+{
+    const int kv = a.c.n_kv_heads;
+    Tile t;
+    if constexpr (!SHARED) {
+        // A line each. Neighbouring workgroups take different kv heads: with eight of them, each die's L2 holds one head's cache. Later
+        // tiles of a prompt see more: they go first
+        if (tile_of(a, few_rows_of(D), a.tiles - 1 - blockIdx.x / kv, &t)) many_stretch<D, E4M3>(a, t, blockIdx.x % kv, 0, many_units<D>(t), -1);
+    } else {
+        // stretches of one kv head lie on one die, as far as they divide
+        const int per_die = a.many_shares / 8, x = blockIdx.x;
+        const int share = x < 8 * per_die ? x % 8 * per_die + x / 8 : x;
+        const Start s = start_of<kManyThreads>(share, a.many_shares, a.tiles, kv, kManyLeastTiles, a.many_before, [&](int j) {
+            Tile u;
+            return tile_of(a, few_rows_of(D), j, &u) ? (int64_t)many_units<D>(u) : 0;
+        });
+        const int64_t all = s.total, end = min(s.pos + s.each, all * kv);   // units of a kv head; the stretch's end
+        int64_t pos = s.pos, begin = s.before;
+        int i = s.item, kvh = all > 0 ? (int)(pos / all) : 0;
+        for (int part = 0; pos < end; ++part) {
+            const int64_t rel = pos - kvh * all;
+            if (rel >= all) {                           // the next kv head's first tile
+                ++kvh;
+                i = 0;
+                begin = 0;
+                --part;
+                continue;
+            }
+            const int n = tile_of(a, few_rows_of(D), i, &t) ? many_units<D>(t) : 0;
+            if (rel >= begin + n) {
+                begin += n;
+                ++i;
+                --part;
+                continue;
+            }
+            const int k0 = (int)(rel - begin), k1 = (int)min((int64_t)n, k0 + (end - pos));
+            many_stretch<D, E4M3>(a, t, kvh, k0, k1, k0 == 0 && k1 == n ? -1 : 2 * share + (part > 0));
+            pos += k1 - k0;
+        }
+    }
+}
+
+// Four rows a workgroup, a wave each: lines lie in few stretches.
+template <int D>
 __global__ __launch_bounds__(kThreads) void sp_attend_many_join_kernel(AttendArgs a)
 {
-    constexpr int kKeys = Stage<D, E4M3>::kKeys;
-    const int x = blockIdx.x / kManyRows, r = blockIdx.x % kManyRows, kvh = blockIdx.y, G = a.c.group;
+    const int x = blockIdx.x / (kManyRows / kWaves), r = blockIdx.x % (kManyRows / kWaves) * kWaves + (threadIdx.x >> 6), kvh = blockIdx.y, G = a.c.group;
+    const int64_t before = a.many_before[x], n = a.many_before[x + 1] - before, total = a.many_before[a.tiles];
+    int64_t each = (total * a.c.n_kv_heads + a.many_shares - 1) / a.many_shares;
+    each = each < kManyLeastTiles ? kManyLeastTiles : each;
+    const int64_t begin = kvh * total + before, end = begin + n;
+    if (n == 0 || begin / each == (end - 1) / each) return;
     Tile t;
-    if (!tile_of(a, x, &t) || r >= t.rows) return;
-    const int64_t span = t.hi - t.lo / kKeys * kKeys;
-    int count = (int)((span + a.many_keys - 1) / a.many_keys);
-    count = count < 1 ? 1 : (count > a.many_splits ? a.many_splits : count);
-    const int64_t at = ((int64_t)x * a.c.n_kv_heads + kvh) * kManyRows + r, step = (int64_t)a.tiles * a.c.n_kv_heads * kManyRows;
-    join_row<D>(a, a.many_ml, a.many_o, at, step, count, (a.off[t.b] + (t.row0 + r) / G) * a.c.n_q_heads + kvh * G + (t.row0 + r) % G);
+    if (!tile_of(a, few_rows_of(D), x, &t) || r >= t.rows) return;
+    join_row<D, 1>(a, a.many_ml, a.many_o, kManyRows, r, begin, end, each, (a.off[t.b] + (t.row0 + r) / G) * a.c.n_q_heads + kvh * G + (t.row0 + r) % G);
 }
 
-// How a call is laid out: which kernels run, and the splits of each.
+// How a call is laid out: which kernels run, and on how many workgroups.
 struct Plan {
-    int64_t total, most_few;            // rows in all; rows of a kv head of the largest request that has few
+    int64_t total, most_few;            // query tokens in all; rows of a kv head of the largest request that has few
     bool few, many;
-    int32_t few_rows, splits, split_blocks;
-    int32_t tiles, many_splits, many_count, many_b[kManyList], many_tile[kManyList];
-    int64_t many_keys;
-    size_t part_o, many_ml, many_o, bytes;      // where the workspace's parts begin (part_ml at 0)
+    int32_t few_rows, few_shares, tiles, many_shares, many_count, many_b[kManyList], many_tile[kManyList];
+    size_t few_o, few_before, many_ml, many_o, many_before, bytes;      // where the workspace's parts begin (few_ml at 0)
 };
 
-constexpr int64_t kFewTarget = 1024;    // workgroups that keep the device busy: four on each of 256 compute units
-constexpr int64_t kMinSplit = 8;        // blocks of a split: two for each wave
-constexpr int64_t kManyTarget = 256;    // one workgroup of eight waves on each compute unit
-constexpr int64_t kManyMinKeys = 1024;  // keys of a split that are worth writing 256 rows of partial results
+constexpr int64_t kMaxLen = int64_t(1) << 30, kMaxTokens = int64_t(1) << 26;     // key indices and rows fit 32 bits
+constexpr int64_t kUnits = 256;         // compute units
+constexpr int64_t kFewWhole = 17;       // blocks of contexts that are not worth a joining launch
+constexpr int64_t kFewRounds = 1;
+constexpr int64_t kManyPerUnit64 = 1;   // workgroups of sp_attend_many_kernel on a compute unit at head_dim 64
+constexpr int64_t kManyWhole = 1;       // lines for each of those that make up for their different lengths
 
-// Splits of `span` units for `lines` lines of work: about `target` workgroups in all, `least` units each, at most `most` splits.
-void split_of(int64_t span, int64_t lines, int64_t target, int64_t least, int64_t most, int64_t *splits, int64_t *each)
-{
-    *each = sp::ceil_div(span * lines, target);
-    if (*each < least) *each = least;
-    if (sp::ceil_div(span, *each) > most) *each = sp::ceil_div(span, most);
-    *splits = sp::ceil_div(span, *each);
-}
-
-sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64_t max_len, int64_t window, Plan *p)
+sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64_t max_len, Plan *p)
 {
     if (sp_status rc = sp::check_cache(d)) return rc;
     int64_t longest;
     if (sp_status rc = sp::check_ragged(off, B, &p->total, &longest)) return rc;
-    if (max_len < 0 || max_len >= (int64_t(1) << 31))
-        return sp::fail(SP_ERR_INVALID_ARG, "max_len = %lld outside 0..2^31-1", (long long)max_len);
-    const int64_t G = d->n_q_heads / d->n_kv_heads, kv = d->n_kv_heads;
+    if (max_len < 0 || max_len > kMaxLen)
+        return sp::fail(SP_ERR_INVALID_ARG, "max_len = %lld outside 0..2^30", (long long)max_len);
+    if (p->total > kMaxTokens) return sp::fail(SP_ERR_UNSUPPORTED, "%lld query tokens exceed 2^26", (long long)p->total);
+    const int64_t G = d->n_q_heads / d->n_kv_heads, kv = d->n_kv_heads, D = d->head_dim;
     int64_t used = 0, requests = 0;     // tiles and requests with many rows
     p->most_few = 0;
     p->few = p->many = false;
     for (int32_t b = 0; b < B; ++b) {
         const int64_t rows = (off[b + 1] - off[b]) * G;
-        if (rows > kFewRows) {
+        if (rows > few_rows_of(d->head_dim)) {
             p->many = true;
             if (requests < kManyList) {
                 p->many_b[requests] = b;
@@ -845,56 +1136,64 @@ sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64
         }
     }
     p->few_rows = p->most_few <= 16 ? 16 : (p->most_few <= 32 ? 32 : 64);
-    const int64_t tile = 8192 / d->head_dim, tiles = requests <= kManyList ? used : p->total * G / kManyRows + B;
+    const int64_t tiles = requests <= kManyList ? used : p->total * G / kManyRows + B;
     if (tiles * kv >= (int64_t(1) << 31))
         return sp::fail(SP_ERR_UNSUPPORTED, "%lld query rows are more than a launch holds", (long long)(p->total * d->n_q_heads));
     p->tiles = (int32_t)tiles;
     p->many_count = requests <= kManyList ? (int32_t)requests : 0;
 
-    // The workspace is sized without a window, which shortens what rows see and never takes more splits than the whole contexts would.
-    int64_t splits, each, many_splits, many_each;
-    split_of(sp::ceil_div(max_len, kBlock) + 1, B * kv, kFewTarget, kMinSplit, INT64_MAX, &splits, &each);
-    split_of(sp::ceil_div(max_len, tile) + 1, tiles * kv > 0 ? tiles * kv : 1, kManyTarget, kManyMinKeys / tile, INT64_MAX, &many_splits, &many_each);
-    const size_t few = p->few && splits > 1 ? (size_t)splits * B * kv * p->few_rows : 0;
-    const size_t many = p->many && many_splits > 1 ? (size_t)many_splits * tiles * kv * kManyRows : 0;
-    p->part_o = sp::align_up(few * sizeof(f32x2), 256);
-    p->many_ml = p->part_o + sp::align_up(few * d->head_dim * sizeof(float), 256);
+    // Few rows: as many workgroups as are resident at once (by the registers of each variant), unless contexts are so short that a
+    // line is best taken whole.
+    const int64_t blocks = sp::ceil_div(max_len, kBlock) + 1;
+    const int64_t resident = kUnits * (D == 64 ? (p->few_rows == 16 ? 4 : p->few_rows == 32 ? 3 : 2) : (p->few_rows == 16 ? 2 : 1));
+    const int64_t most = sp::ceil_div(blocks * B * kv, kFewLeast);
+    p->few_shares = !p->few || blocks <= kFewWhole ? 0 : (int32_t)(resident * kFewRounds < most ? resident * kFewRounds : most);
+    // Many rows: where there are so few tiles that compute units would be left over or finish far apart.
+    const int64_t tile = 8192 / D, spans = sp::ceil_div(max_len, tile) + 1, most_many = sp::ceil_div(spans * tiles * kv, kManyLeastTiles);
+    const int64_t want = kUnits * (D == 64 ? kManyPerUnit64 : 1);
+    p->many_shares = 0;
+    if (p->many && p->many_count && spans > kManyLeastTiles && tiles * kv < kManyWhole * want) p->many_shares = (int32_t)(want < most_many ? want : most_many);
+
+    const size_t few = (size_t)2 * p->few_shares * p->few_rows, many = (size_t)2 * p->many_shares * kManyRows;
+    p->few_o = sp::align_up(few * sizeof(f32x2), 256);
+    p->few_before = p->few_o + sp::align_up(few * D * sizeof(float), 256);
+    p->many_ml = p->few_before + (few ? sp::align_up((size_t)(B + 1) * sizeof(int64_t), 256) : 0);
     p->many_o = p->many_ml + sp::align_up(many * sizeof(f32x2), 256);
-    p->bytes = p->many_o + sp::align_up(many * d->head_dim * sizeof(float), 256);
-    const int64_t few_seen = window + kFewRows, many_seen = window + kManyRows;     // of a long context
-    if (window > 0 && window < max_len && few_seen < max_len)
-        split_of(sp::ceil_div(few_seen, kBlock) + 1, B * kv, kFewTarget, kMinSplit, splits, &splits, &each);
-    if (window > 0 && window < max_len && many_seen < max_len)
-        split_of(sp::ceil_div(many_seen, tile) + 1, tiles * kv > 0 ? tiles * kv : 1, kManyTarget, kManyMinKeys / tile, many_splits, &many_splits, &many_each);
-    p->splits = (int32_t)splits;
-    p->split_blocks = (int32_t)each;
-    p->many_splits = (int32_t)many_splits;
-    p->many_keys = many_each * tile;
+    p->many_before = p->many_o + sp::align_up(many * D * sizeof(float), 256);
+    p->bytes = p->many_before + (many ? sp::align_up((size_t)(tiles + 1) * sizeof(int64_t), 256) : 0);
     return SP_OK;
+}
+
+template <int D, bool E4M3, int MT>
+void few(const AttendArgs &a, dim3 grid, hipStream_t st)
+{
+    if (a.few_shares) hipLaunchKernelGGL((sp_attend_few_kernel<D, E4M3, MT, true>), grid, dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL((sp_attend_few_kernel<D, E4M3, MT, false>), grid, dim3(kThreads), 0, st, a);
 }
 
 template <int D, bool E4M3>
 sp_status run(const AttendArgs &a, const Plan &p, hipStream_t st)
 {
+    const unsigned kv = (unsigned)a.c.n_kv_heads;
     if (p.few) {
-        const dim3 grid((unsigned)p.splits, (unsigned)a.c.n_kv_heads, (unsigned)a.B);
-        if (p.few_rows == 16) hipLaunchKernelGGL((sp_attend_few_kernel<D, E4M3, 1>), grid, dim3(kThreads), 0, st, a);
-        else if (p.few_rows == 32) hipLaunchKernelGGL((sp_attend_few_kernel<D, E4M3, 2>), grid, dim3(kThreads), 0, st, a);
-        else hipLaunchKernelGGL((sp_attend_few_kernel<D, E4M3, 4>), grid, dim3(kThreads), 0, st, a);
+        const dim3 grid(p.few_shares ? (unsigned)p.few_shares : (unsigned)a.B * kv);
+        if (p.few_rows == 16) few<D, E4M3, 1>(a, grid, st);
+        else if (p.few_rows == 32) few<D, E4M3, 2>(a, grid, st);
+        else if constexpr (few_rows_of(D) > 32) few<D, E4M3, 4>(a, grid, st);
         SP_HIP_CHECK(hipGetLastError());
-        if (p.splits > 1) {
-            const dim3 rows((unsigned)p.most_few, (unsigned)a.c.n_kv_heads, (unsigned)a.B);
-            hipLaunchKernelGGL((sp_attend_join_kernel<D>), rows, dim3(kThreads), 0, st, a);
+        if (p.few_shares) {
+            hipLaunchKernelGGL((sp_attend_few_join_kernel<D>), dim3((unsigned)p.most_few, kv, (unsigned)a.B), dim3(kThreads), 0, st, a);
             SP_HIP_CHECK(hipGetLastError());
         }
     }
     if (p.many) {
-        const dim3 grid((unsigned)((int64_t)p.tiles * a.c.n_kv_heads * p.many_splits));
-        hipLaunchKernelGGL((sp_attend_many_kernel<D, E4M3>), grid, dim3(kManyThreads), 0, st, a);
+        const dim3 grid(p.many_shares ? (unsigned)p.many_shares : (unsigned)p.tiles * kv);
+        if (p.many_shares) hipLaunchKernelGGL((sp_attend_many_kernel<D, E4M3, true>), grid, dim3(kManyThreads), 0, st, a);
+        else hipLaunchKernelGGL((sp_attend_many_kernel<D, E4M3, false>), grid, dim3(kManyThreads), 0, st, a);
         SP_HIP_CHECK(hipGetLastError());
-        if (p.many_splits > 1) {
-            const dim3 rows((unsigned)((int64_t)p.tiles * kManyRows), (unsigned)a.c.n_kv_heads);
-            hipLaunchKernelGGL((sp_attend_many_join_kernel<D, E4M3>), rows, dim3(kThreads), 0, st, a);
+        if (p.many_shares) {
+            const dim3 rows((unsigned)(p.tiles * (kManyRows / kWaves)), kv);
+            hipLaunchKernelGGL((sp_attend_many_join_kernel<D>), rows, dim3(kThreads), 0, st, a);
             SP_HIP_CHECK(hipGetLastError());
         }
     }
@@ -908,7 +1207,7 @@ extern "C" sp_status sp_attend_workspace(const sp_cache_desc *desc, const int64_
 {
     if (!bytes) return sp::fail(SP_ERR_INVALID_ARG, "bytes is null");
     Plan p;
-    if (sp_status rc = make_plan(desc, offsets_host, B, max_len, 0, &p)) return rc;
+    if (sp_status rc = make_plan(desc, offsets_host, B, max_len, &p)) return rc;
     *bytes = p.bytes;
     return SP_OK;
 }
@@ -921,7 +1220,7 @@ extern "C" sp_status sp_attend(const sp_cache_desc *desc, const void *q_dev, con
                                size_t ws_bytes, void *hip_stream)
 {
     Plan p;
-    if (sp_status rc = make_plan(desc, offsets_host, B, max_len, window, &p)) return rc;
+    if (sp_status rc = make_plan(desc, offsets_host, B, max_len, &p)) return rc;
     if (!(scale > 0.f) || scale > 3.0e38f) return sp::fail(SP_ERR_INVALID_ARG, "scale must be finite and > 0");
     if (causal != 0 && causal != 1) return sp::fail(SP_ERR_INVALID_ARG, "causal = %d is neither 0 nor 1", causal);
     if (window < 0 || (window > 0 && !causal))
@@ -945,27 +1244,28 @@ extern "C" sp_status sp_attend(const sp_cache_desc *desc, const void *q_dev, con
 
     AttendArgs a{sp::view_of(*desc, block_table_dev, table_stride), static_cast<const uint16_t *>(q_dev), offsets_dev,
                  lens_dev, static_cast<const uint8_t *>(k_pool_dev), static_cast<const uint8_t *>(v_pool_dev),
-                 k_scale_dev, v_scale_dev, static_cast<uint16_t *>(out_dev), lse_dev, max_len, window, B, causal, scale};
+                 k_scale_dev, v_scale_dev, static_cast<uint16_t *>(out_dev), lse_dev, (int32_t)max_len,
+                 window < max_len ? (int32_t)window : 0, B, causal, scale};      // a longer window takes no key from a row
     a.page_blocks = (int32_t)(desc->page_tokens / kBlock);
     a.page_shift = -1;
     for (int s = 0; s < 24; ++s)
         if (a.page_blocks == 1 << s) a.page_shift = s;
-    a.splits = p.splits;
-    a.split_blocks = p.split_blocks;
-    a.few_rows = p.few_rows;
     a.tiles = p.tiles;
-    a.many_splits = p.many_splits;
-    a.many_keys = p.many_keys;
     a.many_count = p.many_count;
     for (int i = 0; i < p.many_count; ++i) {
         a.many_b[i] = p.many_b[i];
         a.many_tile[i] = p.many_tile[i];
     }
     uint8_t *ws = static_cast<uint8_t *>(ws_dev);
-    a.part_ml = reinterpret_cast<f32x2 *>(ws);
-    a.part_o = reinterpret_cast<float *>(ws + p.part_o);
+    a.few_shares = p.few_shares;
+    a.few_rows = p.few_rows;
+    a.few_ml = reinterpret_cast<f32x2 *>(ws);
+    a.few_o = reinterpret_cast<float *>(ws + p.few_o);
+    a.few_before = reinterpret_cast<int64_t *>(ws + p.few_before);
+    a.many_shares = p.many_shares;
     a.many_ml = reinterpret_cast<f32x2 *>(ws + p.many_ml);
     a.many_o = reinterpret_cast<float *>(ws + p.many_o);
+    a.many_before = reinterpret_cast<int64_t *>(ws + p.many_before);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const bool e4m3 = sp::cache_is_e4m3(*desc);
     if (desc->head_dim == 64) return e4m3 ? run<64, true>(a, p, st) : run<64, false>(a, p, st);
