@@ -385,7 +385,7 @@ template <int D, bool E4M3, int MT>
 __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh, int k0, int k1, int slot)
 {
     constexpr int kSteps = D / 32, kTiles = D / 16;
-    __shared__ float merge_o[2][16 * MT][D];
+    __shared__ float merge_o[2][16 * MT][D + 4];       // padded: sixteen rows are written side by side
     __shared__ f32x2 merge_ml[2][16 * MT];
     const int G = a.c.group;
     const Range rg = range_of(a, b);
@@ -595,11 +595,21 @@ __device__ __forceinline__ void join_row(const AttendArgs &a, const f32x2 *ml, c
             l += x[1] * w;
         }
         const int n = min(64, count - s0);
-        for (int s = part_wave; s < n; s += WAVES) {
-            const float f = __shfl(w, s);
-            const float *src = po + at(s0 + s) * D + lane;
+        constexpr int kAhead = 8;                           // partial results under way
+        for (int s = part_wave; s < n; s += WAVES * kAhead) {
+            float x[kAhead][D / 64];
 #pragma unroll
-            for (int i = 0; i < D / 64; ++i) acc[i] += src[64 * i] * f;
+            for (int k = 0; k < kAhead; ++k) {
+                const float *src = po + at(s0 + min(s + WAVES * k, n - 1)) * D + lane;
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) x[k][i] = src[64 * i];
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const float f = s + WAVES * k < n ? __shfl(w, (s + WAVES * k) & 63) : 0.f;
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) acc[i] += x[k][i] * f;
+            }
         }
     }
 #pragma unroll
