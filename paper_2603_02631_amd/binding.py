@@ -462,6 +462,15 @@ def _offsets(values):
 def _rows(t, what: str, rows: int, width: int, stride: Optional[int], elem: int):
     """(address, row stride in elements) of `rows` rows of `width` contiguous elements: a tensor whose first dimension
     counts rows and whose others are dense, or an address with its stride."""
+    # two dimensions, the second dense: what a projection's output and its parts are. Few attribute reads, as in _ptr
+    try:
+        st = t.stride()
+        if t.is_cuda and len(st) == 2 and st[1] == 1 and stride is None and t.element_size() == elem:
+            n, w = t.shape
+            if n >= rows and w >= width:
+                return t.data_ptr(), st[0] if rows > 1 else (width + 7) & ~7      # the stride of a single row means nothing
+    except AttributeError:
+        pass
     if t is None:
         return None, 0
     if isinstance(t, int):
@@ -480,8 +489,7 @@ def _rows(t, what: str, rows: int, width: int, stride: Optional[int], elem: int)
         raise SpError(1, f"{what} has {dense} elements a row, the call needs {width}")
     if stride is not None and stride != strides[0] and rows > 1:
         raise SpError(1, f"{what} has a row stride of {strides[0]}, the call says {stride}")
-    # the stride of a single row means nothing
-    return t.data_ptr(), (strides[0] if rows > 1 else max(width, 8))
+    return t.data_ptr(), (strides[0] if rows > 1 else (width + 7) & ~7)
 
 
 def _table(block_table, B: int, table_stride: Optional[int]):
@@ -495,14 +503,11 @@ def _table(block_table, B: int, table_stride: Optional[int]):
     return _ptr(block_table, "block_table", 4 * B * table_stride), table_stride
 
 
-def _pool_bytes(desc: CacheDesc) -> int:
-    elem = 1 if desc.cache_type == SP_CACHE_E4M3 else 2
-    return ((desc.n_pages - 1) * desc.page_stride + (desc.n_kv_heads - 1) * desc.stride_head
-            + (desc.page_tokens - 1) * desc.stride_token + desc.head_dim) * elem
-
-
-def _scale_bytes(desc: CacheDesc) -> int:
-    return 4 * desc.n_pages * desc.n_kv_heads * (desc.page_tokens // SP_CACHE_BLOCK)
+def _cache_bytes(desc: CacheDesc):
+    """Query heads, kv heads, head_dim, and the bytes that a pool and its scales have to hold."""
+    kv, d, pages, page = desc.n_kv_heads, desc.head_dim, desc.n_pages, desc.page_tokens
+    pool = (pages - 1) * desc.page_stride + (kv - 1) * desc.stride_head + (page - 1) * desc.stride_token + d
+    return desc.n_q_heads, kv, d, pool if desc.cache_type == SP_CACHE_E4M3 else 2 * pool, 4 * pages * kv * (page // SP_CACHE_BLOCK)
 
 
 def sp_cache_append(desc: CacheDesc, k, v, offsets_host, offsets_dev, start, block_table, k_pool, v_pool, k_scale=None,
@@ -513,14 +518,15 @@ def sp_cache_append(desc: CacheDesc, k, v, offsets_host, offsets_dev, start, blo
     off = _offsets(offsets_host)
     B = len(off) - 1
     T = max(off[B], 0) if B >= 0 else 0
-    kw, qw = desc.n_kv_heads * desc.head_dim, desc.n_q_heads * desc.head_dim
+    H, kv, d, pool, scales = _cache_bytes(desc)
+    kw, qw = kv * d, H * d
     kp, ks = _rows(k, "k", T, kw, k_stride, 2)
     vp, vs = _rows(v, "v", T, kw, v_stride, 2)
     qp, qs = _rows(q, "q", T, qw, q_stride, 2)
     tab, width = _table(block_table, B, table_stride)
     if n_pos is None:
         n_pos = 0 if cos is None or isinstance(cos, int) else cos.shape[0]
-    pool, scales, trig = _pool_bytes(desc), _scale_bytes(desc), 2 * n_pos * rot_dim
+    trig = 2 * n_pos * rot_dim
     _check(load_library().sp_cache_append(
         ctypes.byref(desc), kp, ks, vp, vs, qp, qs, _ptr(q_out, "q_out", 2 * T * qw), off,
         _ptr(offsets_dev, "offsets_dev", 8 * (B + 1)), B, _ptr(start, "start", 4 * B),
@@ -547,12 +553,13 @@ def sp_attend(desc: CacheDesc, q, offsets_host, offsets_dev, lens, max_len: int,
     B = len(off) - 1
     T = max(off[B], 0) if B >= 0 else 0
     tab, width = _table(block_table, B, table_stride)
-    rows, pool, scales = T * desc.n_q_heads, _pool_bytes(desc), _scale_bytes(desc)
+    H, _, d, pool, scales = _cache_bytes(desc)
+    rows = T * H
     _check(load_library().sp_attend(
-        ctypes.byref(desc), _ptr(q, "q", 2 * rows * desc.head_dim), off, _ptr(offsets_dev, "offsets_dev", 8 * (B + 1)), B,
+        ctypes.byref(desc), _ptr(q, "q", 2 * rows * d), off, _ptr(offsets_dev, "offsets_dev", 8 * (B + 1)), B,
         _ptr(lens, "lens", 4 * B), max_len, tab, width, _ptr(k_pool, "k_pool", pool), _ptr(v_pool, "v_pool", pool),
         _ptr(k_scale, "k_scale", scales), _ptr(v_scale, "v_scale", scales), scale, causal, window,
-        _ptr(out, "out", 2 * rows * desc.head_dim), _ptr(lse, "lse", 4 * rows), _ptr(ws, "ws"), _ws_bytes(ws, ws_bytes),
+        _ptr(out, "out", 2 * rows * d), _ptr(lse, "lse", 4 * rows), _ptr(ws, "ws"), _ws_bytes(ws, ws_bytes),
         _stream(stream)))
 
 
@@ -574,6 +581,6 @@ def sp_logprobs(logits, n_rows: int, vocab: int, targets, n_top: int, logprob, e
     x, stride = _rows(logits, "logits", n_rows, vocab, row_stride, 4 if dtype == SP_LOGITS_F32 else 2)
     n, k = max(n_rows, 0), max(n_top, 0)
     _check(load_library().sp_logprobs(
-        x, dtype, n_rows, vocab, max(stride, vocab) if n_rows <= 1 else stride, _ptr(targets, "targets", 4 * n), n_top,
+        x, dtype, n_rows, vocab, stride or row_stride or vocab, _ptr(targets, "targets", 4 * n), n_top,
         _ptr(logprob, "logprob", 4 * n), _ptr(entropy, "entropy", 4 * n), _ptr(top_ids, "top_ids", 4 * n * k),
         _ptr(top_logprobs, "top_logprobs", 4 * n * k), _ptr(ws, "ws"), _ws_bytes(ws, ws_bytes), _stream(stream)))

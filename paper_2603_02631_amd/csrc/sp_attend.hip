@@ -570,18 +570,30 @@ __global__ __launch_bounds__(kThreads, D == 128 && MT > 1 ? 1 : 2) void sp_atten
     }
 }
 
-// Joins the partial results of one row: units [begin, end) of the work, `each` to a workgroup, `rows` rows in a partial result. WAVES waves
-// share them out; their weights exp2(m_s - m) come first, then the weighted sum.
+// The partial results of a line of work, units [begin, end), `each` to a workgroup: workgroups first_share .. first_share + count - 1. A
+// line that begins inside a workgroup's stretch is that workgroup's second partial result.
+struct Parts {
+    int first_share, count;
+    bool second;
+
+    __device__ __forceinline__ Parts(int64_t begin, int64_t end, int64_t each)
+    {
+        first_share = (int)(begin / each);
+        count = (int)((end - 1) / each) - first_share + 1;
+        second = begin != first_share * each;
+    }
+
+    __device__ __forceinline__ int slot(int s) const { return s == 0 ? 2 * first_share + second : 2 * (first_share + s); }
+};
+
+// Joins the partial results of one row, `rows` rows in each. WAVES waves share them out; their weights exp2(m_s - m) come first, then the
+// weighted sum.
 template <int D, int WAVES>
-__device__ __forceinline__ void join_row(const AttendArgs &a, const f32x2 *ml, const float *po, int rows, int r, int64_t begin, int64_t end,
-                                         int64_t each, int64_t row)
+__device__ __forceinline__ void join_row(const AttendArgs &a, const f32x2 *ml, const float *po, int rows, int r, const Parts &parts, int64_t row)
 {
     __shared__ float part[kWaves][D];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, part_wave = wave % WAVES;
-    const int i0 = (int)(begin / each), i1 = (int)((end - 1) / each), count = i1 - i0 + 1;
-    // a line that begins inside a workgroup's stretch is that workgroup's second partial result
-    const int first = 2 * i0 + (begin != i0 * each);
-    const auto at = [&](int s) { return (int64_t)(s == 0 ? first : 2 * (i0 + s)) * rows + r; };
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, part_wave = wave % WAVES, count = parts.count;
+    const auto at = [&](int s) { return (int64_t)parts.slot(s) * rows + r; };
     float m = neg_inf();
     for (int s = lane; s < count; s += 64) m = fmaxf(m, ml[at(s)][0]);
 #pragma unroll
@@ -641,9 +653,10 @@ __global__ __launch_bounds__(kThreads) void sp_attend_few_join_kernel(AttendArgs
     if (n == 0 || r >= rows) return;
     int64_t each = (total + a.few_shares - 1) / a.few_shares;
     each = each < kFewLeast ? kFewLeast : each;
-    const int64_t begin = before + (int64_t)kvh * n, end = begin + n;
-    if (begin / each == (end - 1) / each) return;
-    join_row<D, kWaves>(a, a.few_ml, a.few_o, a.few_rows, r, begin, end, each, (a.off[b] + r / G) * a.c.n_q_heads + kvh * G + r % G);
+    const int64_t begin = before + (int64_t)kvh * n;
+    const Parts parts(begin, begin + n, each);
+    if (parts.count == 1) return;
+    join_row<D, kWaves>(a, a.few_ml, a.few_o, a.few_rows, r, parts, (a.off[b] + r / G) * a.c.n_q_heads + kvh * G + r % G);
 }
 
 // ---- many rows: prompt chunks -----------------------------------------------------------------------------------------
@@ -1088,19 +1101,22 @@ __global__ __launch_bounds__(kManyThreads) void sp_attend_many_kernel(AttendArgs
     }
 }
 
-// Four rows a workgroup, a wave each: lines lie in few stretches.
+constexpr int kJoinRows = 2;            // of a wave: finding a line's few parts takes longer than joining a row, but more rows wait for each other
+
 template <int D>
 __global__ __launch_bounds__(kThreads) void sp_attend_many_join_kernel(AttendArgs a)
 {
-    const int x = blockIdx.x / (kManyRows / kWaves), r = blockIdx.x % (kManyRows / kWaves) * kWaves + (threadIdx.x >> 6), kvh = blockIdx.y, G = a.c.group;
+    constexpr int kBlocksOfTile = kManyRows / (kWaves * kJoinRows);
+    const int x = blockIdx.x / kBlocksOfTile, r0 = (blockIdx.x % kBlocksOfTile * kWaves + (threadIdx.x >> 6)) * kJoinRows, kvh = blockIdx.y, G = a.c.group;
     const int64_t before = a.many_before[x], n = a.many_before[x + 1] - before, total = a.many_before[a.tiles];
     int64_t each = (total * a.c.n_kv_heads + a.many_shares - 1) / a.many_shares;
     each = each < kManyLeastTiles ? kManyLeastTiles : each;
-    const int64_t begin = kvh * total + before, end = begin + n;
-    if (n == 0 || begin / each == (end - 1) / each) return;
+    if (n == 0) return;
+    const Parts parts(kvh * total + before, kvh * total + before + n, each);
     Tile t;
-    if (!tile_of(a, few_rows_of(D), x, &t) || r >= t.rows) return;
-    join_row<D, 1>(a, a.many_ml, a.many_o, kManyRows, r, begin, end, each, (a.off[t.b] + (t.row0 + r) / G) * a.c.n_q_heads + kvh * G + (t.row0 + r) % G);
+    if (parts.count == 1 || !tile_of(a, few_rows_of(D), x, &t)) return;
+    for (int r = r0; r < min(r0 + kJoinRows, t.rows); ++r)
+        join_row<D, 1>(a, a.many_ml, a.many_o, kManyRows, r, parts, (a.off[t.b] + (t.row0 + r) / G) * a.c.n_q_heads + kvh * G + (t.row0 + r) % G);
 }
 
 // How a call is laid out: which kernels run, and on how many workgroups.
@@ -1202,7 +1218,7 @@ sp_status run(const AttendArgs &a, const Plan &p, hipStream_t st)
         else hipLaunchKernelGGL((sp_attend_many_kernel<D, E4M3, false>), grid, dim3(kManyThreads), 0, st, a);
         SP_HIP_CHECK(hipGetLastError());
         if (p.many_shares) {
-            const dim3 rows((unsigned)(p.tiles * (kManyRows / kWaves)), kv);
+            const dim3 rows((unsigned)(p.tiles * (kManyRows / (kWaves * kJoinRows))), kv);
             hipLaunchKernelGGL((sp_attend_many_join_kernel<D>), rows, dim3(kThreads), 0, st, a);
             SP_HIP_CHECK(hipGetLastError());
         }
