@@ -36,11 +36,13 @@ int main()
                                 }
                         }
     sp_cache_desc ok{8, 2, 64, SP_CACHE_E4M3, 4, 64, 8192, 4096, 64};
-    const int64_t two[] = {0, 3}, huge[] = {0, INT64_MAX}, big[] = {0, INT32_MAX}, down[] = {0, INT64_MIN};
+    const int64_t two[] = {0, 3}, huge[] = {0, INT64_MAX}, big[] = {0, 1 << 26}, over[] = {0, (1 << 26) + 1}, down[] = {0, INT64_MIN};
     size_t n = 0;
     EXPECT(sp_attend_workspace(&ok, huge, 1, 64, &n) == SP_ERR_INVALID_ARG);
     EXPECT(sp_attend_workspace(&ok, down, 1, 64, &n) == SP_ERR_INVALID_ARG);
-    EXPECT(sp_attend_workspace(&ok, big, 1, INT32_MAX, &n) == SP_OK && n % 256 == 0);
+    EXPECT(sp_attend_workspace(&ok, big, 1, 1 << 30, &n) == SP_OK && n % 256 == 0);
+    EXPECT(sp_attend_workspace(&ok, big, 1, (1 << 30) + 1, &n) == SP_ERR_INVALID_ARG);
+    EXPECT(sp_attend_workspace(&ok, over, 1, 64, &n) == SP_ERR_UNSUPPORTED);
     for (int64_t s : extremes)
         for (int64_t t : extremes)
             for (int64_t np : extremes)
