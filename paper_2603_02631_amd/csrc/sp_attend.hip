@@ -907,7 +907,7 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
     const int G = a.c.group, r = 32 * wave + c;                 // this lane's row of the tile
     const int token = (t.row0 + r) / G, head = kvh * G + (t.row0 + r) % G;
     const int64_t row = (a.off[t.b] + token) * a.c.n_q_heads + head;
-    int last = t.rg.len;                    // this lane's row sees keys [last - window or 0, last)
+    int last = t.rg.len;                    // this lane's row sees keys [first, last)
     // keys that every row of this wave sees: [all_lo, all_hi); that some row sees: [any_lo, any_hi)
     int all_lo = 0, all_hi = t.rg.len, any_hi = t.rg.len, any_lo = 0;
     if (a.causal) {
@@ -920,6 +920,8 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
             any_lo = all_hi - a.window;
         }
     }
+    const int first = a.causal && a.window > 0 && last > a.window ? last - a.window : 0;
+    const uint32_t seen = last > first ? last - first : 0;      // keys of this lane's row
     const bool busy = 32 * wave < t.rows;
 
     bf16x8 q[kSteps];
@@ -972,10 +974,8 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
 #pragma unroll
                         for (int w = 0; w < 2; ++w)
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                const int key = key0 + 32 * (u + w) + 8 * (e >> 2) + 4 * h + (e & 3);
-                                if (key >= last || (a.window > 0 && key < last - a.window)) x[w][e] = neg_inf();
-                            }
+                            for (int e = 0; e < 16; ++e)
+                                if ((uint32_t)(key0 + 4 * h - first + 32 * (u + w) + 8 * (e >> 2) + (e & 3)) >= seen) x[w][e] = neg_inf();
                     float sc[2], vexp[2], vinv[2], top = neg_inf();
 #pragma unroll
                     for (int w = 0; w < 2; ++w) {
@@ -984,7 +984,7 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
                         vinv[w] = 1.f;
                         // blocks that no row of the tile sees may have any scale: they are masked, and take none
                         if (E4M3 && (whole || (key0 + 32 * (u + w) < t.hi && key0 + 32 * (u + w) + 32 > t.lo))) {
-                            const float vs = scales[buf][kBlocks + u + w];
+                            const float vs = fmaxf(scales[buf][kBlocks + u + w], 1.17549435e-38f);     // 0, of a block of zeros, has no logarithm
                             sc[w] *= scales[buf][u + w];
                             vexp[w] = log2_(vs);
                             vinv[w] = 1.f / vs;
