@@ -900,6 +900,7 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
     using S = Stage<D, E4M3>;
     constexpr int kKeys = S::kKeys, kBlocks = S::kBlocks, kSteps = D / 16, kOut = D / 32;
     constexpr float kSlack = 8.f;
+    constexpr int kVectorOnly = 0x406;      // what may cross a scheduling barrier: vector, scalar and transcendental operations
     __shared__ u32x4 keys[2][1024], values[2][1024];            // 16 KB each
     __shared__ float scales[2][2 * kBlocks];
     const int from = (t.lo / kKeys + k0) * kKeys, to = min((t.lo / kKeys + k1) * kKeys, t.hi);
@@ -957,25 +958,51 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
             if (n + 2 <= last_tile) st.load(a, t.b, kvh, last_page, cur, fresh);
             if (busy && key0 < any_hi && key0 + kKeys > any_lo) {
                 const bool whole = key0 >= all_lo && key0 + kKeys <= all_hi;
-                // two blocks at a time: two independent chains of the first product, one look at the reference
+                // Two blocks at a time: two independent chains of the first product, one look at the reference. Operands are read from LDS a group of
+                // products ahead; the scheduling barriers keep the reads (not vector operations) from being moved behind the products (2048 rows
+                // after 32K tokens 605 -> 570 us). At head_dim 64 they gain nothing: 347 with, 344 without on a whole prompt of 8192.
 #pragma unroll
                 for (int u = 0; u < kBlocks; u += 2) {
+                    constexpr int kGroup = 2;                       // steps of the first product read at a time
+                    bf16x8 kf[2][kGroup][2];
+                    const auto read_keys = [&](int to, int s0) {
+#pragma unroll
+                        for (int s = 0; s < kGroup; ++s)
+#pragma unroll
+                            for (int w = 0; w < 2; ++w) kf[to][s][w] = __builtin_bit_cast(bf16x8, keys[buf][S::key_slot(32 * (u + w) + c, 2 * (s0 + s) + h)]);
+                        if constexpr (D == 128) __builtin_amdgcn_sched_barrier(kVectorOnly);
+                    };
                     f32x16 x[2];
 #pragma unroll
                     for (int w = 0; w < 2; ++w)
 #pragma unroll
                         for (int e = 0; e < 16; ++e) x[w][e] = 0.f;
+                    read_keys(0, 0);
 #pragma unroll
-                    for (int s = 0; s < kSteps; ++s)
+                    for (int s0 = 0; s0 < kSteps; s0 += kGroup) {
+                        if (s0 + kGroup < kSteps) read_keys(s0 / kGroup + 1 & 1, s0 + kGroup);
 #pragma unroll
-                        for (int w = 0; w < 2; ++w)
-                            x[w] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, keys[buf][S::key_slot(32 * (u + w) + c, 2 * s + h)]), q[s], x[w], 0, 0, 0);
-                    if (!whole)
+                        for (int s = 0; s < kGroup; ++s)
+#pragma unroll
+                            for (int w = 0; w < 2; ++w) x[w] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s0 / kGroup & 1][s][w], q[s0 + s], x[w], 0, 0, 0);
+                        if constexpr (D == 128) __builtin_amdgcn_sched_barrier(kVectorOnly);
+                    }
+                    bf16x8 vf[2][kOut];
+                    const auto read_values = [&](int to, int part) {        // part: 16 keys
+#pragma unroll
+                        for (int i = 0; i < kOut; ++i) vf[to][i] = __builtin_bit_cast(bf16x8, values[buf][S::value_slot(32 * i + c, 4 * u + 2 * part + h)]);
+                        if constexpr (D == 128) __builtin_amdgcn_sched_barrier(kVectorOnly);
+                    };
+                    read_values(0, 0);
+                    if (!whole) {
+                        int at = key0 + 32 * u + 4 * h - first;
+                        if constexpr (D == 128) asm volatile("" : "+v"(at));        // no register for each element: they are short
 #pragma unroll
                         for (int w = 0; w < 2; ++w)
 #pragma unroll
                             for (int e = 0; e < 16; ++e)
-                                if ((uint32_t)(key0 + 4 * h - first + 32 * (u + w) + 8 * (e >> 2) + (e & 3)) >= seen) x[w][e] = neg_inf();
+                                if ((uint32_t)(at + 32 * w + 8 * (e >> 2) + (e & 3)) >= seen) x[w][e] = neg_inf();
+                    }
                     float sc[2], vexp[2], vinv[2], top = neg_inf();
 #pragma unroll
                     for (int w = 0; w < 2; ++w) {
@@ -1002,27 +1029,25 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
                         for (int i = 0; i < kOut; ++i) o[i] *= f;
                         m = mx;
                     }
+                    float sum[2] = {0.f, 0.f};
 #pragma unroll
-                    for (int w = 0; w < 2; ++w) {
+                    for (int part = 0; part < 4; ++part) {
+                        const int w = part >> 1, k = part & 1;
                         const float ref = (m == neg_inf() ? 0.f : m) - vexp[w];
-                        float sum[2] = {0.f, 0.f};
+                        u32x4 p;
+                        if (k == 0) sum[0] = sum[1] = 0.f;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) x[w][e] = exp2_(x[w][e] * sc[w] - ref);
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            u32x4 p;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                p[e] = pack2(x[w][8 * k + 2 * e], x[w][8 * k + 2 * e + 1]);
-                                sum[0] += x[w][8 * k + 2 * e];
-                                sum[1] += x[w][8 * k + 2 * e + 1];
-                            }
-#pragma unroll
-                            for (int i = 0; i < kOut; ++i)
-                                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values[buf][S::value_slot(32 * i + c, 4 * (u + w) + 2 * k + h)]),
-                                                                              __builtin_bit_cast(bf16x8, p), o[i], 0, 0, 0);
+                        for (int e = 0; e < 4; ++e) {
+                            const float a0 = exp2_(x[w][8 * k + 2 * e] * sc[w] - ref), a1 = exp2_(x[w][8 * k + 2 * e + 1] * sc[w] - ref);
+                            p[e] = pack2(a0, a1);
+                            sum[0] += a0;
+                            sum[1] += a1;
                         }
-                        l += (sum[0] + sum[1]) * vinv[w];
+                        if (part < 3) read_values(part + 1 & 1, part + 1);
+#pragma unroll
+                        for (int i = 0; i < kOut; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[part & 1][i], __builtin_bit_cast(bf16x8, p), o[i], 0, 0, 0);
+                        if constexpr (D == 128) __builtin_amdgcn_sched_barrier(kVectorOnly);
+                        if (k == 1) l += (sum[0] + sum[1]) * vinv[w];
                     }
                 }
             }
