@@ -478,7 +478,7 @@ typedef enum { SP_ROTATE_HALF = 0, SP_ROTATE_PAIRS = 1 } sp_rotate_style;
  * (optionally) queries to their positions on the way. Request b brings tokens
  * [offsets[b], offsets[b+1]) of the packed inputs (offsets in host and in device
  * memory, the same B+1 non-decreasing values, offsets[0] == 0; 0 <= B <= 4096,
- * requests without new tokens are allowed, fewer than 2^31 new tokens in all).
+ * requests without new tokens are allowed, at most 2^28 new tokens in all).
  * Its i-th new token becomes token start_dev[b] + i of its cache.
  *  - k_dev, v_dev: bf16, token t at t * k_stride (v_stride), n_kv_heads * head_dim
  *    contiguous elements each; strides in elements, multiples of 8 (so keys, values and
@@ -532,6 +532,9 @@ sp_status sp_attend_workspace(const sp_cache_desc *desc, const int64_t *offsets_
  * logarithm of the softmax's denominator. A row that sees no key gets zeros and an lse
  * of minus infinity. Slots that no row of the request sees (those of a last page past the
  * context among them) may hold anything, NaN included.
+ * What a row sees should be finite: logits below 2^120, values below 2^90 in magnitude, scales
+ * finite and not negative (a value scale below 2^-64 may count as 2^-64: zero is in order for a block
+ * of zeros). A row that sees a NaN becomes NaN, and other rows of its request may.
  * At most 2^26 query tokens and contexts of at most 2^30 tokens.
  * max_len bounds the contexts from the host's side (a longer lens[b] counts as
  * max_len, a negative one as 0) and must not exceed table_stride * page_tokens; the call reads the table entries

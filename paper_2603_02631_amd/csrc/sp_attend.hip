@@ -70,6 +70,12 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
     return __builtin_bit_cast(uint32_t, r);
 }
 
+// What a row's result is multiplied by, and its logarithm of the denominator (m in units of log 2). A row that saw no key has a sum of exactly
+// zero; looked at as bits, since the sum of a row that saw a NaN is NaN and must get out.
+__device__ __forceinline__ bool saw_nothing(float l) { return __float_as_uint(l) == 0u; }
+__device__ __forceinline__ float inverse(float l) { return saw_nothing(l) ? 0.f : 1.f / l; }
+__device__ __forceinline__ float lse_of(float m, float l) { return saw_nothing(l) ? neg_inf() : (m + log2_(l)) * kLn2; }
+
 // ---- a few rows: single tokens, lookahead rows -----------------------------------------------------------------------
 
 // What a request's rows see: row r (token r / G) keys [first(r), last(r)), all rows together [lo, hi). Key indices fit 32 bits:
@@ -523,14 +529,14 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
                 for (int i = 0; i < kTiles; i += 4)
                     *reinterpret_cast<f32x4 *>(dst + j * kTiles + i) = f32x4{acc.o[t][i][j], acc.o[t][i + 1][j], acc.o[t][i + 2][j], acc.o[t][i + 3][j]};
         } else {
-            const float inv = acc.l[t] > 0.f ? 1.f / acc.l[t] : 0.f;
+            const float inv = inverse(acc.l[t]);
             const int64_t row = (a.off[b] + r / G) * a.c.n_q_heads + kvh * G + r % G;
             uint32_t *dst = reinterpret_cast<uint32_t *>(a.out + row * D + 4 * g * kTiles);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int i = 0; i < kTiles; i += 2) dst[(j * kTiles + i) / 2] = pack2(acc.o[t][i][j] * inv, acc.o[t][i + 1][j] * inv);
-            if (a.lse && g == 0) a.lse[row] = acc.l[t] > 0.f ? (acc.m[t] + log2_(acc.l[t])) * kLn2 : neg_inf();
+            if (a.lse && g == 0) a.lse[row] = lse_of(acc.m[t], acc.l[t]);
         }
     }
 }
@@ -626,7 +632,7 @@ __device__ __forceinline__ void join_row(const AttendArgs &a, const f32x2 *ml, c
     }
 #pragma unroll
     for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o);
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = inverse(l);
     if (WAVES > 1) {
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) part[wave][lane + 64 * i] = acc[i];
@@ -640,7 +646,7 @@ __device__ __forceinline__ void join_row(const AttendArgs &a, const f32x2 *ml, c
     }
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) a.out[row * D + lane + 64 * i] = __builtin_bit_cast(uint16_t, (__bf16)(acc[i] * inv));
-    if (a.lse && lane == 0) a.lse[row] = l > 0.f ? (m + log2_(l)) * kLn2 : neg_inf();
+    if (a.lse && lane == 0) a.lse[row] = lse_of(m, l);
 }
 
 // Row r of every kv head and request whose line lies in more than one stretch.
@@ -705,6 +711,9 @@ __device__ __forceinline__ bool tile_of(const AttendArgs &a, int few_rows, int x
 // lane holds its probabilities, so these are the second product's operand as they are. Tiles are double-buffered, one barrier a
 // tile; the next tile's loads are under way during the products.
 // A block's key scale goes into its logits' factor, its value scale into the exponent (and out of the sum again): no operation for an element.
+// The factor stays above zero, so that masked logits stay minus infinity; the value scale above 2^-64, so that exponents keep their range.
+constexpr float kLeastScale = 5.42101086e-20f, kLeastFactor = 1.17549435e-38f;
+
 template <int D, bool E4M3>
 struct Stage {
     static constexpr int kKeys = 8192 / D, kBlocks = kKeys / kBlock;
@@ -1011,8 +1020,8 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
                         vinv[w] = 1.f;
                         // blocks that no row of the tile sees may have any scale: they are masked, and take none
                         if (E4M3 && (whole || (key0 + 32 * (u + w) < t.hi && key0 + 32 * (u + w) + 32 > t.lo))) {
-                            const float vs = fmaxf(scales[buf][kBlocks + u + w], 1.17549435e-38f);     // 0, of a block of zeros, has no logarithm
-                            sc[w] *= scales[buf][u + w];
+                            const float vs = fmaxf(scales[buf][kBlocks + u + w], kLeastScale);
+                            sc[w] = fmaxf(sc[w] * scales[buf][u + w], kLeastFactor);
                             vexp[w] = log2_(vs);
                             vinv[w] = 1.f / vs;
                         }
@@ -1071,14 +1080,14 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
                 *reinterpret_cast<f32x4 *>(a.many_o + at * D + 32 * i + 2 * e + 4 * h) = f32x4{o[i][e], o[i][e + 1], o[i][e + 2], o[i][e + 3]};
         return;
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = inverse(l);
 #pragma unroll
     for (int i = 0; i < kOut; ++i)
 #pragma unroll
         for (int e = 0; e < 16; e += 4)
             *reinterpret_cast<u32x2 *>(a.out + row * D + 32 * i + 2 * e + 4 * h) =
                 u32x2{pack2(o[i][e] * inv, o[i][e + 1] * inv), pack2(o[i][e + 2] * inv, o[i][e + 3] * inv)};
-    if (a.lse && h == 0) a.lse[row] = l > 0.f ? (m + log2_(l)) * kLn2 : neg_inf();
+    if (a.lse && h == 0) a.lse[row] = lse_of(m, l);
 }
 
 constexpr int kManyLeastTiles = 16;     // tiles of keys of a stretch: worth writing 256 rows of partial results
@@ -1154,10 +1163,8 @@ struct Plan {
 
 constexpr int64_t kMaxLen = int64_t(1) << 30, kMaxTokens = int64_t(1) << 26;     // key indices and rows fit 32 bits
 constexpr int64_t kUnits = 256;         // compute units
+constexpr int64_t kMaxGroups = int64_t(1) << 23;                // a launch's threads fit 32 bits
 constexpr int64_t kFewWhole = 17;       // blocks of contexts that are not worth a joining launch
-constexpr int64_t kFewRounds = 1;
-constexpr int64_t kManyPerUnit64 = 1;   // workgroups of sp_attend_many_kernel on a compute unit at head_dim 64
-constexpr int64_t kManyWhole = 1;       // lines for each of those that make up for their different lengths
 
 sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64_t max_len, Plan *p)
 {
@@ -1188,8 +1195,8 @@ sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64
     }
     p->few_rows = p->most_few <= 16 ? 16 : (p->most_few <= 32 ? 32 : 64);
     const int64_t tiles = requests <= kManyList ? used : p->total * G / kManyRows + B;
-    if (tiles * kv >= (int64_t(1) << 31))
-        return sp::fail(SP_ERR_UNSUPPORTED, "%lld query rows are more than a launch holds", (long long)(p->total * d->n_q_heads));
+    if (tiles * kv >= kMaxGroups || B * kv >= kMaxGroups)
+        return sp::fail(SP_ERR_UNSUPPORTED, "%lld query rows of %d requests are more than a launch holds", (long long)(p->total * d->n_q_heads), B);
     p->tiles = (int32_t)tiles;
     p->many_count = requests <= kManyList ? (int32_t)requests : 0;
 
@@ -1198,12 +1205,12 @@ sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64
     const int64_t blocks = sp::ceil_div(max_len, kBlock) + 1;
     const int64_t resident = kUnits * (D == 64 ? (p->few_rows == 16 ? 4 : p->few_rows == 32 ? 3 : 2) : (p->few_rows == 16 ? 2 : 1));
     const int64_t most = sp::ceil_div(blocks * B * kv, kFewLeast);
-    p->few_shares = !p->few || blocks <= kFewWhole ? 0 : (int32_t)(resident * kFewRounds < most ? resident * kFewRounds : most);
+    p->few_shares = !p->few || blocks <= kFewWhole ? 0 : (int32_t)(resident < most ? resident : most);
     // Many rows: where there are so few tiles that compute units would be left over or finish far apart.
-    const int64_t tile = 8192 / D, spans = sp::ceil_div(max_len, tile) + 1, most_many = sp::ceil_div(spans * tiles * kv, kManyLeastTiles);
-    const int64_t want = kUnits * (D == 64 ? kManyPerUnit64 : 1);
+    const int64_t spans = sp::ceil_div(max_len, 8192 / D) + 1, most_many = sp::ceil_div(spans * tiles * kv, kManyLeastTiles);
     p->many_shares = 0;
-    if (p->many && p->many_count && spans > kManyLeastTiles && tiles * kv < kManyWhole * want) p->many_shares = (int32_t)(want < most_many ? want : most_many);
+    if (p->many && p->many_count && spans > kManyLeastTiles && tiles * kv < kUnits)
+        p->many_shares = (int32_t)(kUnits < most_many ? kUnits : most_many);
 
     const size_t few = (size_t)2 * p->few_shares * p->few_rows, many = (size_t)2 * p->many_shares * kManyRows;
     p->few_o = sp::align_up(few * sizeof(f32x2), 256);

@@ -20,6 +20,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kBlock = sp::kCacheBlock;
 constexpr float kFloorExp = -64;        // log2 of the smallest scale
+constexpr int64_t kMaxTokens = int64_t(1) << 28;    // a launch's threads fit 32 bits
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
@@ -313,6 +314,7 @@ extern "C" sp_status sp_cache_append(const sp_cache_desc *desc, const void *k_de
         return sp::fail(SP_ERR_INVALID_ARG, "rot_style = %d is neither SP_ROTATE_HALF nor SP_ROTATE_PAIRS", rot_style);
     if (table_stride < 1 || table_stride > (int64_t(1) << 31))
         return sp::fail(SP_ERR_INVALID_ARG, "table_stride = %lld outside 1..2^31", (long long)table_stride);
+    if (total > kMaxTokens) return sp::fail(SP_ERR_UNSUPPORTED, "%lld new tokens exceed 2^28", (long long)total);
     if (total == 0) return SP_OK;
     if (!k_dev || !v_dev) return sp::fail(SP_ERR_INVALID_ARG, "k_dev or v_dev is null");
     if (!q_dev != !q_out_dev) return sp::fail(SP_ERR_INVALID_ARG, "q_dev and q_out_dev come together or not at all");

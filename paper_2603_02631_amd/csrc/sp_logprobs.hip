@@ -70,16 +70,6 @@ struct Sums {
         s *= f;
         m = to;
     }
-
-    __device__ __forceinline__ void join(float m2, float s2, float u2)
-    {
-        const float to = fmaxf(m, m2);
-        Sums o{m2, s2, u2};
-        move(to);
-        o.move(to);
-        s += o.s;
-        u += o.u;
-    }
 };
 
 __device__ __forceinline__ float wave_max(float x)

@@ -237,3 +237,65 @@ def test_pages_beyond_32_bit_offsets(news):
     C.d = d
     verify(C, 1, [held], np.array([0, news]), q, [L], 0.125, 1, 0, ou.bits_to_f64(out.cpu().numpy().view(np.uint16)),
            lse.cpu().numpy().astype(np.float64))
+
+
+@pytest.mark.parametrize("e4m3", [True, False])
+def test_more_requests_than_lanes(e4m3):
+    """Work is shared out over more requests than a wave has lanes, empty ones and ones without queries among them."""
+    rng = np.random.default_rng(9)
+    news, lens = rng.integers(0, 4, 70), rng.integers(0, 200, 70)
+    lens[[3, 66]] = 590, 600
+    check(4, 1, 64, news.tolist(), lens.tolist(), 64, e4m3, max_len=600)
+    check(3, 1, 128, news.tolist(), lens.tolist(), 64, e4m3, max_len=600)
+
+
+@pytest.mark.parametrize("e4m3", [True, False])
+def test_more_prompt_chunks_than_the_list_of_a_launch(e4m3):
+    rng = np.random.default_rng(10)
+    news = rng.integers(4, 8, 67)
+    news[[5, 40]] = 1, 50
+    check(16, 1, 64, news.tolist(), (news + rng.integers(0, 60, 67)).tolist(), 32, e4m3)
+
+
+@pytest.mark.parametrize("e4m3", [True, False])
+@pytest.mark.parametrize("H,kv,d,page,news,lens,window", [
+    (16, 1, 64, 96, [1130], [2300], 0),         # 71 tiles of query rows
+    (4, 2, 64, 32, [300, 150], [2200, 900], 0),
+    (6, 2, 128, 96, [200, 1, 90], [1500, 1100, 95], 0),
+    (4, 2, 128, 32, [300, 150], [2200, 900], 70)])
+def test_long_chunks_shared_out_over_kv_heads(e4m3, H, kv, d, page, news, lens, window):
+    check(H, kv, d, news, lens, page, e4m3, window=window, rows=set(range(0, sum(news), 17)) | {sum(news) - 1})
+
+
+@pytest.mark.parametrize("news", [[1, 3], [90, 70]])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scales_of_zero_where_a_block_is_zero(news, d):
+    c, held, off, q = build(4, 2, d, news, [300, 200], 32, True, "HND", 0, 12)
+    for b, L in enumerate([300, 200]):
+        for j0 in range(0, L, 96):
+            for h in range(2):
+                for j in range(j0, min(L, j0 + 32)):
+                    o = c.at(b, h, j)
+                    c.k[o:o + d] = c.v[o:o + d] = 0
+                    held[b][0][j, h] = held[b][1][j, h] = 0
+                c.ks[c.scale_at(b, h, j0)] = c.vs[c.scale_at(b, h, j0)] = 0
+    out, lse = call(c, 4, off, q, [300, 200], 300, 0.125, 1, 0)
+    verify(c, 4, held, off, q, [300, 200], 0.125, 1, 0, out, lse)
+
+
+@pytest.mark.parametrize("e4m3", [True, False])
+@pytest.mark.parametrize("news,lens", [([1, 3], [300, 200]), ([90, 70], [300, 200]), ([2, 1], [3000, 2500]), ([90, 70], [3000, 2500])])
+def test_a_nan_that_is_seen_gets_out(e4m3, news, lens):
+    """A NaN key makes a row and its lse NaN, a NaN value one element; the other kv head and the other request stay as they are."""
+    for which in ("k", "v"):
+        c, held, off, q = build(4, 2, 64, news, lens, 64, e4m3, "HND", 0, 13)
+        getattr(c, which)[c.at(0, 1, 57) + 5] = 0x7F if e4m3 else 0x7FC0
+        out, lse = call(c, 4, off, q, lens, max(lens), 0.125, 1, 0)
+        n = news[0]
+        if which == "k":
+            assert np.isnan(out[:n, 2:]).all() and np.isnan(lse[:n, 2:]).all()
+        else:
+            assert np.isnan(out[:n, 2:, 5]).all() and np.isfinite(lse[:n, 2:]).all()
+            assert np.isfinite(np.delete(out[:n, 2:], 5, axis=2)).all()
+        assert np.isfinite(out[:n, :2]).all() and np.isfinite(lse[:n, :2]).all()
+        assert np.isfinite(out[n:]).all() and np.isfinite(lse[n:]).all()
