@@ -48,7 +48,7 @@ struct AttendArgs {
     float scale;
     int32_t page_blocks, page_shift;    // blocks of 32 tokens in a page; their logarithm, or -1
     // sp_attend_few_kernel: workgroups that share the work (0: one for each request and kv head), rows of a partial result
-    int32_t few_shares, few_rows;
+    int32_t few_shares, few_rows, few_least;    // the last: blocks of a share
     f32x2 *few_ml;                      // [2 few_shares][few_rows]: reference (in units of log 2), sum
     float *few_o;                       // [2 few_shares][few_rows][head_dim]
     int64_t *few_before;                // [B + 1]: units of work before each request
@@ -541,8 +541,6 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
     }
 }
 
-constexpr int kFewLeast = 16;       // blocks of a stretch: four for each wave
-
 template <int D, bool E4M3, int MT, bool SHARED>
 __global__ __launch_bounds__(kThreads, D == 128 && MT > 1 ? 1 : 2) void sp_attend_few_kernel(AttendArgs a)
 {
@@ -555,7 +553,7 @@ __global__ __launch_bounds__(kThreads, D == 128 && MT > 1 ? 1 : 2) void sp_atten
         pos = (int64_t)(share % kv) * n;
         end = pos + n;
     } else {
-        const Start s = start_of<kThreads>(share, a.few_shares, a.B, 1, kFewLeast, a.few_before, [&](int i) { return (int64_t)few_blocks<D>(a, i) * kv; });
+        const Start s = start_of<kThreads>(share, a.few_shares, a.B, 1, a.few_least, a.few_before, [&](int i) { return (int64_t)few_blocks<D>(a, i) * kv; });
         b = s.item;
         begin = s.before;
         pos = s.pos;
@@ -592,42 +590,43 @@ struct Parts {
     __device__ __forceinline__ int slot(int s) const { return s == 0 ? 2 * first_share + second : 2 * (first_share + s); }
 };
 
-// Joins the partial results of one row, `rows` rows in each. WAVES waves share them out; their weights exp2(m_s - m) come first, then the
-// weighted sum.
+// Joins the partial results of one row, `rows` rows in each. WAVES waves share them out. The outputs are requested before the statistics
+// have come, whose weights exp2(m_s - m) they wait for.
 template <int D, int WAVES>
 __device__ __forceinline__ void join_row(const AttendArgs &a, const f32x2 *ml, const float *po, int rows, int r, const Parts &parts, int64_t row)
 {
     __shared__ float part[kWaves][D];
+    constexpr int kAhead = 8;                               // partial results under way
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, part_wave = wave % WAVES, count = parts.count;
     const auto at = [&](int s) { return (int64_t)parts.slot(s) * rows + r; };
-    float m = neg_inf();
-    for (int s = lane; s < count; s += 64) m = fmaxf(m, ml[at(s)][0]);
+    float x[kAhead][D / 64], acc[D / 64] = {}, m = neg_inf(), l = 0.f;
+    const auto load = [&](int s) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const float *src = po + at(min(s + WAVES * k, count - 1)) * D + lane;
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) x[k][i] = src[64 * i];
+        }
+    };
+    f32x2 mine = ml[at(min(lane, count - 1))];
+    load(part_wave);
+    if (lane < count) m = mine[0];
+    for (int s = lane + 64; s < count; s += 64) m = fmaxf(m, ml[at(s)][0]);
 #pragma unroll
     for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    float l = 0.f, acc[D / 64] = {};
     for (int s0 = 0; s0 < count; s0 += 64) {
-        float w = 0.f;
-        if (s0 + lane < count) {
-            const f32x2 x = ml[at(s0 + lane)];
-            w = x[0] == neg_inf() ? 0.f : exp2_(x[0] - m);
-            l += x[1] * w;
-        }
-        const int n = min(64, count - s0);
-        constexpr int kAhead = 8;                           // partial results under way
-        for (int s = part_wave; s < n; s += WAVES * kAhead) {
-            float x[kAhead][D / 64];
+        if (s0 > 0) mine = ml[at(min(s0 + lane, count - 1))];
+        const float w = s0 + lane >= count || mine[0] == neg_inf() ? 0.f : exp2_(mine[0] - m);
+        if (s0 + lane < count) l += mine[1] * w;
+        const int end = min(s0 + 64, count);
+        for (int s = s0 + part_wave; s < end; s += WAVES * kAhead) {
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
-                const float *src = po + at(s0 + min(s + WAVES * k, n - 1)) * D + lane;
-#pragma unroll
-                for (int i = 0; i < D / 64; ++i) x[k][i] = src[64 * i];
-            }
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                const float f = s + WAVES * k < n ? __shfl(w, (s + WAVES * k) & 63) : 0.f;
+                const float f = s + WAVES * k < end ? __shfl(w, s + WAVES * k - s0 & 63) : 0.f;
 #pragma unroll
                 for (int i = 0; i < D / 64; ++i) acc[i] += x[k][i] * f;
             }
+            if (s + WAVES * kAhead < count) load(s + WAVES * kAhead);
         }
     }
 #pragma unroll
@@ -649,20 +648,20 @@ __device__ __forceinline__ void join_row(const AttendArgs &a, const f32x2 *ml, c
     if (a.lse && lane == 0) a.lse[row] = lse_of(m, l);
 }
 
-// Row r of every kv head and request whose line lies in more than one stretch.
-template <int D>
+// Every row of the kv heads and requests whose line lies in more than one stretch, WAVES waves a row.
+template <int D, int WAVES>
 __global__ __launch_bounds__(kThreads) void sp_attend_few_join_kernel(AttendArgs a)
 {
-    const int b = blockIdx.z, kvh = blockIdx.y, r = blockIdx.x, G = a.c.group;
+    const int b = blockIdx.z, kvh = blockIdx.y, r = (blockIdx.x * kWaves + (threadIdx.x >> 6)) / WAVES, G = a.c.group;
     const int64_t before = a.few_before[b], total = a.few_before[a.B];
     const int n = (int)((a.few_before[b + 1] - before) / a.c.n_kv_heads), rows = (int)min((int64_t)few_rows_of(D) + 1, a.off[b + 1] - a.off[b]) * G;
     if (n == 0 || r >= rows) return;
     int64_t each = (total + a.few_shares - 1) / a.few_shares;
-    each = each < kFewLeast ? kFewLeast : each;
+    each = each < a.few_least ? a.few_least : each;
     const int64_t begin = before + (int64_t)kvh * n;
     const Parts parts(begin, begin + n, each);
     if (parts.count == 1) return;
-    join_row<D, kWaves>(a, a.few_ml, a.few_o, a.few_rows, r, parts, (a.off[b] + r / G) * a.c.n_q_heads + kvh * G + r % G);
+    join_row<D, WAVES>(a, a.few_ml, a.few_o, a.few_rows, r, parts, (a.off[b] + r / G) * a.c.n_q_heads + kvh * G + r % G);
 }
 
 // ---- many rows: prompt chunks -----------------------------------------------------------------------------------------
@@ -1090,8 +1089,6 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
     if (a.lse && h == 0) a.lse[row] = lse_of(m, l);
 }
 
-constexpr int kManyLeastTiles = 16;     // tiles of keys of a stretch: worth writing 256 rows of partial results
-
 template <int D, bool E4M3, bool SHARED>
 __global__ __launch_bounds__(kManyThreads) void sp_attend_many_kernel(AttendArgs a)
 {
@@ -1105,7 +1102,7 @@ __global__ __launch_bounds__(kManyThreads) void sp_attend_many_kernel(AttendArgs
         // stretches of one kv head lie on one die, as far as they divide
         const int per_die = a.many_shares / 8, x = blockIdx.x;
         const int share = x < 8 * per_die ? x % 8 * per_die + x / 8 : x;
-        const Start s = start_of<kManyThreads>(share, a.many_shares, a.tiles, kv, kManyLeastTiles, a.many_before, [&](int j) {
+        const Start s = start_of<kManyThreads>(share, a.many_shares, a.tiles, kv, 1, a.many_before, [&](int j) {
             Tile u;
             return tile_of(a, few_rows_of(D), j, &u) ? (int64_t)many_units<D>(u) : 0;
         });
@@ -1143,8 +1140,7 @@ __global__ __launch_bounds__(kThreads) void sp_attend_many_join_kernel(AttendArg
     constexpr int kBlocksOfTile = kManyRows / (kWaves * kJoinRows);
     const int x = blockIdx.x / kBlocksOfTile, r0 = (blockIdx.x % kBlocksOfTile * kWaves + (threadIdx.x >> 6)) * kJoinRows, kvh = blockIdx.y, G = a.c.group;
     const int64_t before = a.many_before[x], n = a.many_before[x + 1] - before, total = a.many_before[a.tiles];
-    int64_t each = (total * a.c.n_kv_heads + a.many_shares - 1) / a.many_shares;
-    each = each < kManyLeastTiles ? kManyLeastTiles : each;
+    const int64_t each = (total * a.c.n_kv_heads + a.many_shares - 1) / a.many_shares;
     if (n == 0) return;
     const Parts parts(kvh * total + before, kvh * total + before + n, each);
     Tile t;
@@ -1157,14 +1153,13 @@ __global__ __launch_bounds__(kThreads) void sp_attend_many_join_kernel(AttendArg
 struct Plan {
     int64_t total, most_few;            // query tokens in all; rows of a kv head of the largest request that has few
     bool few, many;
-    int32_t few_rows, few_shares, tiles, many_shares, many_count, many_b[kManyList], many_tile[kManyList];
+    int32_t few_rows, few_shares, few_least, tiles, many_shares, many_count, many_b[kManyList], many_tile[kManyList];
     size_t few_o, few_before, many_ml, many_o, many_before, bytes;      // where the workspace's parts begin (few_ml at 0)
 };
 
 constexpr int64_t kMaxLen = int64_t(1) << 30, kMaxTokens = int64_t(1) << 26;     // key indices and rows fit 32 bits
 constexpr int64_t kUnits = 256;         // compute units
 constexpr int64_t kMaxGroups = int64_t(1) << 23;                // a launch's threads fit 32 bits
-constexpr int64_t kFewWhole = 17;       // blocks of contexts that are not worth a joining launch
 
 sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64_t max_len, Plan *p)
 {
@@ -1201,16 +1196,23 @@ sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64
     p->many_count = requests <= kManyList ? (int32_t)requests : 0;
 
     // Few rows: as many workgroups as are resident at once (by the registers of each variant), unless contexts are so short that a
-    // line is best taken whole.
-    const int64_t blocks = sp::ceil_div(max_len, kBlock) + 1;
+    // line is best taken whole: a block of a line takes 0.2 us (0.3 at head_dim 128), sharing out about 5 for its second launch, and more with the number of lines.
+    // Single tokens over 8 kv heads of 64, whole and shared: 8 contexts of 1000 tokens 9.5 and 11.4 us, of up to 4000 15.5 and 13.0; 64 of 1000 15.2 and 20.4, of
+    // up to 4000 28.8 and 28.2. At most 128 blocks, since one long line among many short ones would then be what takes the time.
+    const int64_t blocks = sp::ceil_div(max_len, kBlock) + 1, lines = B * kv;
     const int64_t resident = kUnits * (D == 64 ? (p->few_rows == 16 ? 4 : p->few_rows == 32 ? 3 : 2) : (p->few_rows == 16 ? 2 : 1));
-    const int64_t most = sp::ceil_div(blocks * B * kv, kFewLeast);
-    p->few_shares = !p->few || blocks <= kFewWhole ? 0 : (int32_t)(resident < most ? resident : most);
-    // Many rows: where there are so few tiles that compute units would be left over or finish far apart.
-    const int64_t spans = sp::ceil_div(max_len, 8192 / D) + 1, most_many = sp::ceil_div(spans * tiles * kv, kManyLeastTiles);
+    const int64_t whole = (lines < 320 ? 48 + lines / 4 : 128) * 64 / D;
+    // Joining takes longer with more parts of a line, its stretches with fewer: the best size grows with the root of the length (one context of 2000
+    // tokens: at least 4 or 16 blocks 12.1 and 14.2 us; of 32768: 8 or 16 blocks 17.8 and 15.4).
+    p->few_least = 4;
+    while (8 * p->few_least * p->few_least < blocks) p->few_least *= 2;
+    const int64_t most = sp::ceil_div(blocks * lines, p->few_least);
+    p->few_shares = !p->few || blocks <= whole ? 0 : (int32_t)(resident < most ? resident : most);
+    // Many rows: where compute units would be left over, unless lines are short. Whole and shared, 8 kv heads: 512 rows of head_dim 64 over 512 tokens (five
+    // tiles of keys) 17 and 26 us, 128 rows of head_dim 128 over 500 (nine) 24 and 23, over 1500 56 and 25; but 6000 over 6000 (384 lines) 197 and 253.
+    const int64_t spans = sp::ceil_div(max_len, 8192 / D) + 1, most_many = spans * tiles * kv;
     p->many_shares = 0;
-    if (p->many && p->many_count && spans > kManyLeastTiles && tiles * kv < kUnits)
-        p->many_shares = (int32_t)(kUnits < most_many ? kUnits : most_many);
+    if (p->many && p->many_count && spans > 8 && tiles * kv < kUnits) p->many_shares = (int32_t)(kUnits < most_many ? kUnits : most_many);
 
     const size_t few = (size_t)2 * p->few_shares * p->few_rows, many = (size_t)2 * p->many_shares * kManyRows;
     p->few_o = sp::align_up(few * sizeof(f32x2), 256);
@@ -1240,7 +1242,11 @@ sp_status run(const AttendArgs &a, const Plan &p, hipStream_t st)
         else if constexpr (few_rows_of(D) > 32) few<D, E4M3, 4>(a, grid, st);
         SP_HIP_CHECK(hipGetLastError());
         if (p.few_shares) {
-            hipLaunchKernelGGL((sp_attend_few_join_kernel<D>), dim3((unsigned)p.most_few, kv, (unsigned)a.B), dim3(kThreads), 0, st, a);
+            // four waves a row where a line has many parts
+            if (p.few_shares > 8 * a.B * (int64_t)kv)
+                hipLaunchKernelGGL((sp_attend_few_join_kernel<D, kWaves>), dim3((unsigned)p.most_few, kv, (unsigned)a.B), dim3(kThreads), 0, st, a);
+            else
+                hipLaunchKernelGGL((sp_attend_few_join_kernel<D, 1>), dim3((unsigned)sp::ceil_div(p.most_few, kWaves), kv, (unsigned)a.B), dim3(kThreads), 0, st, a);
             SP_HIP_CHECK(hipGetLastError());
         }
     }
@@ -1317,6 +1323,7 @@ extern "C" sp_status sp_attend(const sp_cache_desc *desc, const void *q_dev, con
     uint8_t *ws = static_cast<uint8_t *>(ws_dev);
     a.few_shares = p.few_shares;
     a.few_rows = p.few_rows;
+    a.few_least = p.few_least;
     a.few_ml = reinterpret_cast<f32x2 *>(ws);
     a.few_o = reinterpret_cast<float *>(ws + p.few_o);
     a.few_before = reinterpret_cast<int64_t *>(ws + p.few_before);
