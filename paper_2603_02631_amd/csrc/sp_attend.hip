@@ -34,6 +34,10 @@ constexpr int kBlock = sp::kCacheBlock;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+// A block's key scale goes into its logits' factor, its value scale into the exponent (and out of the sum again): no operation for an element.
+// The factor stays above zero, so that masked logits stay minus infinity; the value scale above 2^-64, so that exponents keep their range.
+constexpr float kLeastScale = 5.42101086e-20f, kLeastFactor = 1.17549435e-38f;
+
 struct AttendArgs {
     sp::CacheView c;
     const uint16_t *q;
@@ -112,8 +116,6 @@ __device__ __forceinline__ int page_entry(const AttendArgs &a, int b, uint32_t i
     return page >= (int)a.c.n_pages ? (int)a.c.n_pages - 1 : page;
 }
 
-__device__ __forceinline__ int page_at(const AttendArgs &a, int b, uint32_t blk) { return page_entry(a, b, page_of_block(a, blk)); }
-
 // Eight E4M3 codes as eight bf16, exactly: the upper halves of their float images.
 __device__ __forceinline__ bf16x8 widen8(uint32_t c0, uint32_t c1)
 {
@@ -128,6 +130,75 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t c0, uint32_t c1)
     return __builtin_bit_cast(bf16x8, r);
 }
 
+// A scalar address that moves, and loads at a lane's 32-bit offset from it: a load takes both as they are. What the compiler does not know to stay
+// the same in a loop (asm) it does not add up beforehand, which would cost two vector operations for each load.
+struct Moving {
+    uint64_t p;
+
+    __device__ __forceinline__ explicit Moving(const uint8_t *at) : p(reinterpret_cast<uint64_t>(at)) { asm("" : "+s"(p)); }
+
+    __device__ __forceinline__ void advance(int64_t bytes)
+    {
+        p += (uint64_t)bytes;
+        asm("" : "+s"(p));
+    }
+
+    template <class T>
+    __device__ __forceinline__ T load(uint32_t lane) const
+    {
+        typedef const __attribute__((address_space(1))) uint8_t *Bytes;
+        return *reinterpret_cast<const __attribute__((address_space(1))) T *>(reinterpret_cast<Bytes>(p) + lane);
+    }
+};
+
+__device__ __forceinline__ uint32_t opaque(uint32_t lane)
+{
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
+// A request's cache of one kv head, and where a block of it lies: bytes from k and v, floats from ks and vs.
+struct Line {
+    const uint8_t *k, *v;
+    const float *ks, *vs;
+    int64_t page_bytes;
+    uint32_t row_bytes, page_scales;
+
+    __device__ __forceinline__ Line(const AttendArgs &a, int kvh, int es)
+    {
+        k = a.k_pool + kvh * a.c.stride_head * es;
+        v = a.v_pool + kvh * a.c.stride_head * es;
+        ks = a.k_scale + (int64_t)kvh * a.page_blocks;
+        vs = a.v_scale + (int64_t)kvh * a.page_blocks;
+        page_bytes = a.c.page_stride * es;
+        row_bytes = (uint32_t)a.c.stride_token * es;
+        page_scales = (uint32_t)a.c.n_kv_heads * (uint32_t)a.page_blocks;
+    }
+};
+
+struct Place {
+    int64_t off, scale;
+};
+
+// Block blk of request b as the block table has it: requested here, looked at in place(), as scalars, so that loads take a scalar base.
+struct Entry {
+    int page;
+    uint32_t in_page;
+
+    __device__ __forceinline__ Entry(const AttendArgs &a, int b, int blk)
+    {
+        const uint32_t i = page_of_block(a, (uint32_t)blk);
+        page = a.c.table[b * a.c.table_stride + i];
+        in_page = (uint32_t)blk - i * (uint32_t)a.page_blocks;
+    }
+
+    __device__ __forceinline__ Place place(const AttendArgs &a, const Line &l) const
+    {
+        const int p = min(max(__builtin_amdgcn_readfirstlane(page), 0), (int)a.c.n_pages - 1);      // never outside the pools
+        return {p * l.page_bytes + (int64_t)((uint64_t)in_page * (kBlock * l.row_bytes)), (int64_t)((uint64_t)(uint32_t)p * l.page_scales) + in_page};
+    }
+};
+
 // One block of 32 tokens as a wave loads it, straight into the registers that the matrix instructions take it from.
 // Lane l = 16 g + c. Keys: row c of 16-key tile t, the contraction's elements in an order that makes a lane's share of a row contiguous
 // (queries are loaded in the same order). Values: elements [c D/16, (c+1) D/16) of the eight keys 4g + j and 16 + 4g + j, j < 4: the
@@ -139,47 +210,40 @@ struct Block {
     uint32_t v[8][kLoads];
     float ks, vs;
 
-    static constexpr int ES = E4M3 ? 1 : 2;
-
-    __device__ __forceinline__ static int64_t base_of(const AttendArgs &a, int kvh, int page, uint32_t in_page)
+    __device__ __forceinline__ void load_keys(const Line &l, const Place &at, uint32_t lane)
     {
-        return (page * a.c.page_stride + kvh * a.c.stride_head + (int64_t)(in_page * kBlock) * a.c.stride_token) * ES;
-    }
-
-    __device__ __forceinline__ void load_keys(const AttendArgs &a, int kvh, int page, uint32_t blk, uint32_t lane)
-    {
-        const uint32_t in_page = blk - page_of_block(a, blk) * (uint32_t)a.page_blocks;
-        const uint8_t *p = a.k_pool + base_of(a, kvh, page, in_page);
-        const int64_t half = 16 * a.c.stride_token * ES;
+        lane = opaque(lane);
+        Moving p(l.k + at.off);
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) k[t][i] = *reinterpret_cast<const u32x4 *>(p + t * half + i * 64 + lane);
+            for (int i = 0; i < kLoads; ++i) k[t][i] = p.load<u32x4>(lane + 64 * i);
+            p.advance(16 * (int64_t)l.row_bytes);
+        }
         ks = 1.f;
-        if (E4M3) ks = a.k_scale[((int64_t)page * a.c.n_kv_heads + kvh) * a.page_blocks + in_page];
+        if (E4M3) ks = l.ks[at.scale];
     }
 
-    __device__ __forceinline__ void load_values(const AttendArgs &a, int kvh, int page, uint32_t blk, uint32_t lane)
+    __device__ __forceinline__ void load_values(const Line &l, const Place &at, uint32_t lane)
     {
-        const uint32_t in_page = blk - page_of_block(a, blk) * (uint32_t)a.page_blocks;
-        const uint8_t *p = a.v_pool + base_of(a, kvh, page, in_page);
-        const int64_t row = a.c.stride_token * ES;
+        lane = opaque(lane);
+        Moving p(l.v + at.off);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const uint8_t *x = p + ((j & 3) + (j >> 2) * 16) * row + lane;
-            if constexpr (kLoads == 1) v[j][0] = *reinterpret_cast<const uint32_t *>(x);
+            if constexpr (kLoads == 1) v[j][0] = p.load<uint32_t>(lane);
             else if constexpr (kLoads == 2) {
-                const u32x2 w = *reinterpret_cast<const u32x2 *>(x);
+                const u32x2 w = p.load<u32x2>(lane);
                 v[j][0] = w[0];
                 v[j][1] = w[1];
             } else {
-                const u32x4 w = *reinterpret_cast<const u32x4 *>(x);
+                const u32x4 w = p.load<u32x4>(lane);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[j][i] = w[i];
             }
+            p.advance((j == 3 ? 13 : 1) * (int64_t)l.row_bytes);
         }
         vs = 1.f;
-        if (E4M3) vs = a.v_scale[((int64_t)page * a.c.n_kv_heads + kvh) * a.page_blocks + in_page];
+        if (E4M3) vs = l.vs[at.scale];
     }
 
     // Elements of step s of tile t's rows.
@@ -261,10 +325,11 @@ struct Rows {
         }
     }
 
-    // x: logits of this lane's eight keys in units of log 2. Returns their probabilities' bits times vs.
-    __device__ __forceinline__ bf16x8 weigh(int t, const float (&x)[8], float vs)
+    // x: products <q, k> of this lane's eight keys, factor: what makes logits in units of log 2 of them. Returns 2^vexp times the probabilities as bf16;
+    // vinv = 2^-vexp.
+    __device__ __forceinline__ bf16x8 weigh(int t, const float (&x)[8], float factor, float vexp, float vinv)
     {
-        float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+        const float top = factor * fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
         if (__any(top > m[t] + kSlack)) {
             const float mx = fmaxf(m[t], row_max(top));
             const float f = m[t] == neg_inf() ? 0.f : exp2_(m[t] - mx);
@@ -273,14 +338,14 @@ struct Rows {
             for (int i = 0; i < D / 16; ++i) o[t][i] *= f;
             m[t] = mx;
         }
-        const float ref = m[t] == neg_inf() ? 0.f : m[t];
+        const float ref = (m[t] == neg_inf() ? 0.f : m[t]) - vexp;
         float p[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = exp2_(x[i] - ref);
-        l[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+        for (int i = 0; i < 8; ++i) p[i] = exp2_(x[i] * factor - ref);
+        l[t] += (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]))) * vinv;
         u32x4 r;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = pack2(p[2 * i] * vs, p[2 * i + 1] * vs);
+        for (int i = 0; i < 4; ++i) r[i] = pack2(p[2 * i], p[2 * i + 1]);
         return __builtin_bit_cast(bf16x8, r);
     }
 };
@@ -421,20 +486,21 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
 
     Rows<D, MT> acc;
     acc.clear();
-    const uint32_t row_bytes = (uint32_t)a.c.stride_token * (E4M3 ? 1 : 2);
-    const uint32_t k_lane = c * row_bytes + 16 * g, v_lane = 4 * g * row_bytes + c * (D / 16) * (E4M3 ? 1 : 2);
-    // The next block's keys are loaded once this one's are in the first product, its values once these are in operand form.
+    const Line line(a, kvh, E4M3 ? 1 : 2);
+    const uint32_t k_lane = c * line.row_bytes + 16 * g, v_lane = 4 * g * line.row_bytes + c * (D / 16) * (E4M3 ? 1 : 2);
+    // The next block's keys are loaded once this one's are in the first product, its values once these are in operand form. Block table entries
+    // are requested two blocks ahead.
     Block<D, E4M3> kv;
     int blk = from + wave;
     if (blk < to) {
         const auto next = [&](int x) { return x + kWaves < to ? x + kWaves : x; };
-        int page = page_at(a, b, (uint32_t)blk);
-        kv.load_keys(a, kvh, page, (uint32_t)blk, k_lane);
-        kv.load_values(a, kvh, page, (uint32_t)blk, v_lane);
-        page = page_at(a, b, (uint32_t)next(blk));
+        const Place here = Entry(a, b, blk).place(a, line);
+        Entry soon(a, b, next(blk));
+        kv.load_keys(line, here, k_lane);
+        kv.load_values(line, here, v_lane);
         for (;;) {
             const int ahead = next(blk), key0 = blk * kBlock;
-            const int page2 = page_at(a, b, (uint32_t)next(ahead));
+            const Entry later(a, b, next(ahead));
             const bool whole = key0 >= all_lo && key0 + kBlock <= all_hi;
             f32x4 s0[MT], s1[MT];
             {
@@ -453,20 +519,27 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
                     }
                 }
             }
-            const float sc = scale2 * kv.ks, vs = kv.vs;
-            kv.load_keys(a, kvh, page, (uint32_t)ahead, k_lane);
+            const Place there = soon.place(a, line);
+            float factor = scale2, vexp = 0.f, vinv = 1.f;
+            if (E4M3) {
+                const float vs = fmaxf(kv.vs, kLeastScale);
+                factor = fmaxf(scale2 * kv.ks, kLeastFactor);
+                vexp = log2_(vs);
+                vinv = __builtin_amdgcn_rcpf(vs);
+            }
+            kv.load_keys(line, there, k_lane);
             bf16x8 vf[kTiles];
             if (!whole) kv.clear_values(g, key0, rg.lo, rg.hi);
             kv.values(vf);
-            kv.load_values(a, kvh, page, (uint32_t)ahead, v_lane);
-            page = page2;
+            kv.load_values(line, there, v_lane);
+            soon = later;
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
                 float x[8];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    x[j] = s0[t][j] * sc;
-                    x[4 + j] = s1[t][j] * sc;
+                    x[j] = s0[t][j];
+                    x[4 + j] = s1[t][j];
                 }
                 if (!whole)
 #pragma unroll
@@ -474,7 +547,7 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
                         const int key = key0 + 4 * g + (j & 3) + (j >> 2) * 16;
                         if (key >= last[t] || (a.window > 0 && key < last[t] - a.window)) x[j] = neg_inf();
                     }
-                const bf16x8 p = acc.weigh(t, x, vs);
+                const bf16x8 p = acc.weigh(t, x, factor, vexp, vinv);
 #pragma unroll
                 for (int i = 0; i < kTiles; ++i) acc.o[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], p, acc.o[t][i], 0, 0, 0);
             }
@@ -709,10 +782,6 @@ __device__ __forceinline__ bool tile_of(const AttendArgs &a, int few_rows, int x
 // LDS. The transposed logits put a row into a lane column; the order of keys in a row of transposed values is the one in which a
 // lane holds its probabilities, so these are the second product's operand as they are. Tiles are double-buffered, one barrier a
 // tile; the next tile's loads are under way during the products.
-// A block's key scale goes into its logits' factor, its value scale into the exponent (and out of the sum again): no operation for an element.
-// The factor stays above zero, so that masked logits stay minus infinity; the value scale above 2^-64, so that exponents keep their range.
-constexpr float kLeastScale = 5.42101086e-20f, kLeastFactor = 1.17549435e-38f;
-
 template <int D, bool E4M3>
 struct Stage {
     static constexpr int kKeys = 8192 / D, kBlocks = kKeys / kBlock;
