@@ -143,11 +143,13 @@ struct Moving {
         asm("" : "+s"(p));
     }
 
-    template <class T>
+    template <class T, bool STREAM = false>
     __device__ __forceinline__ T load(uint32_t lane) const
     {
         typedef const __attribute__((address_space(1))) uint8_t *Bytes;
-        return *reinterpret_cast<const __attribute__((address_space(1))) T *>(reinterpret_cast<Bytes>(p) + lane);
+        const auto *x = reinterpret_cast<const __attribute__((address_space(1))) T *>(reinterpret_cast<Bytes>(p) + lane);
+        if constexpr (STREAM) return __builtin_nontemporal_load(x);
+        else return *x;
     }
 };
 
@@ -203,7 +205,10 @@ struct Entry {
 // Lane l = 16 g + c. Keys: row c of 16-key tile t, the contraction's elements in an order that makes a lane's share of a row contiguous
 // (queries are loaded in the same order). Values: elements [c D/16, (c+1) D/16) of the eight keys 4g + j and 16 + 4g + j, j < 4: the
 // keys whose logits the lane holds after the first product.
-template <int D, bool E4M3>
+// Loads that take whole lines of 128 bytes pass the caches by: values, unless their rows have 64 bytes, and keys whose rows do. 32 requests of bf16, head_dim
+// 128, 172 us without and 159 with (but 168 with it for keys, whose lines take two or four loads); 48 of E4M3, head_dim 64, 156 and 143. The latter only
+// for contexts that no cache would hold until the next call: 64 of up to 2000 tokens, called again and again, take 21 us without and 25 with.
+template <int D, bool E4M3, bool STREAM>
 struct Block {
     static constexpr int kLoads = E4M3 ? D / 64 : D / 32;           // 16-byte loads of a key's row share; dwords of a value's
     u32x4 k[2][kLoads];
@@ -217,7 +222,7 @@ struct Block {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) k[t][i] = p.load<u32x4>(lane + 64 * i);
+            for (int i = 0; i < kLoads; ++i) k[t][i] = p.load<u32x4, STREAM && kLoads == 1>(lane + 64 * i);
             p.advance(16 * (int64_t)l.row_bytes);
         }
         ks = 1.f;
@@ -232,11 +237,11 @@ struct Block {
         for (int j = 0; j < 8; ++j) {
             if constexpr (kLoads == 1) v[j][0] = p.load<uint32_t>(lane);
             else if constexpr (kLoads == 2) {
-                const u32x2 w = p.load<u32x2>(lane);
+                const u32x2 w = p.load<u32x2, true>(lane);
                 v[j][0] = w[0];
                 v[j][1] = w[1];
             } else {
-                const u32x4 w = p.load<u32x4>(lane);
+                const u32x4 w = p.load<u32x4, true>(lane);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[j][i] = w[i];
             }
@@ -452,7 +457,7 @@ __device__ __forceinline__ int few_blocks(const AttendArgs &a, int b)
 // Bound by the bytes of the cache. Four waves take every fourth block of 32 tokens of a stretch; a wave holds its rows'
 // statistics and output by itself and loads a block ahead, the four meet in LDS at the end.
 // Blocks [k0, k1) of request b and kv head kvh; `slot` of the partial results, or -1 if that is all of them.
-template <int D, bool E4M3, int MT>
+template <int D, bool E4M3, int MT, bool STREAM>
 __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh, int k0, int k1, int slot)
 {
     constexpr int kSteps = D / 32, kTiles = D / 16;
@@ -490,7 +495,7 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
     const uint32_t k_lane = c * line.row_bytes + 16 * g, v_lane = 4 * g * line.row_bytes + c * (D / 16) * (E4M3 ? 1 : 2);
     // The next block's keys are loaded once this one's are in the first product, its values once these are in operand form. Block table entries
     // are requested two blocks ahead.
-    Block<D, E4M3> kv;
+    Block<D, E4M3, STREAM> kv;
     int blk = from + wave;
     if (blk < to) {
         const auto next = [&](int x) { return x + kWaves < to ? x + kWaves : x; };
@@ -614,7 +619,7 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
     }
 }
 
-template <int D, bool E4M3, int MT, bool SHARED>
+template <int D, bool E4M3, int MT, bool SHARED, bool STREAM>
 __global__ __launch_bounds__(kThreads, D == 128 && MT > 1 ? 1 : 2) void sp_attend_few_kernel(AttendArgs a)
 {
     const int kv = a.c.n_kv_heads, share = blockIdx.x;
@@ -641,7 +646,7 @@ __global__ __launch_bounds__(kThreads, D == 128 && MT > 1 ? 1 : 2) void sp_atten
             continue;
         }
         const int rel = (int)(pos - begin), kvh = rel / n, k0 = rel % n, k1 = (int)min((int64_t)n, k0 + (end - pos));
-        few_stretch<D, E4M3, MT>(a, b, kvh, k0, k1, k0 == 0 && k1 == n ? -1 : 2 * share + (part > 0));
+        few_stretch<D, E4M3, MT, STREAM>(a, b, kvh, k0, k1, k0 == 0 && k1 == n ? -1 : 2 * share + (part > 0));
         pos += k1 - k0;
         __syncthreads();                    // the merge's LDS is used again
     }
@@ -1221,13 +1226,14 @@ __global__ __launch_bounds__(kThreads) void sp_attend_many_join_kernel(AttendArg
 // How a call is laid out: which kernels run, and on how many workgroups.
 struct Plan {
     int64_t total, most_few;            // query tokens in all; rows of a kv head of the largest request that has few
-    bool few, many;
+    bool few, many, stream;             // stream: contexts that no cache holds until the next call
     int32_t few_rows, few_shares, few_least, tiles, many_shares, many_count, many_b[kManyList], many_tile[kManyList];
     size_t few_o, few_before, many_ml, many_o, many_before, bytes;      // where the workspace's parts begin (few_ml at 0)
 };
 
 constexpr int64_t kMaxLen = int64_t(1) << 30, kMaxTokens = int64_t(1) << 26;     // key indices and rows fit 32 bits
 constexpr int64_t kUnits = 256;         // compute units
+constexpr int64_t kStream = int64_t(1) << 28;                   // bytes that the last cache before memory holds
 constexpr int64_t kMaxGroups = int64_t(1) << 23;                // a launch's threads fit 32 bits
 
 sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64_t max_len, Plan *p)
@@ -1273,6 +1279,7 @@ sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64
     const int64_t whole = (lines < 320 ? 48 + lines / 4 : 128) * 64 / D;
     // Joining takes longer with more parts of a line, its stretches with fewer: the best size grows with the root of the length (one context of 2000
     // tokens: at least 4 or 16 blocks 12.1 and 14.2 us; of 32768: 8 or 16 blocks 17.8 and 15.4).
+    p->stream = 2 * max_len * B * kv * D * (sp::cache_is_e4m3(*d) ? 1 : 2) > kStream;
     p->few_least = 4;
     while (8 * p->few_least * p->few_least < blocks) p->few_least *= 2;
     const int64_t most = sp::ceil_div(blocks * lines, p->few_least);
@@ -1293,11 +1300,19 @@ sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64
     return SP_OK;
 }
 
-template <int D, bool E4M3, int MT>
-void few(const AttendArgs &a, dim3 grid, hipStream_t st)
+template <int D, bool E4M3, int MT, bool STREAM>
+void few_of(const AttendArgs &a, dim3 grid, hipStream_t st)
 {
-    if (a.few_shares) hipLaunchKernelGGL((sp_attend_few_kernel<D, E4M3, MT, true>), grid, dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL((sp_attend_few_kernel<D, E4M3, MT, false>), grid, dim3(kThreads), 0, st, a);
+    if (a.few_shares) hipLaunchKernelGGL((sp_attend_few_kernel<D, E4M3, MT, true, STREAM>), grid, dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL((sp_attend_few_kernel<D, E4M3, MT, false, STREAM>), grid, dim3(kThreads), 0, st, a);
+}
+
+template <int D, bool E4M3, int MT>
+void few(const AttendArgs &a, bool stream, dim3 grid, hipStream_t st)
+{
+    if constexpr (D == 64 && E4M3)              // keys of 64 bytes: as they stand the only loads that the answer changes
+        if (stream) return few_of<D, E4M3, MT, true>(a, grid, st);
+    few_of<D, E4M3, MT, false>(a, grid, st);
 }
 
 template <int D, bool E4M3>
@@ -1306,9 +1321,9 @@ sp_status run(const AttendArgs &a, const Plan &p, hipStream_t st)
     const unsigned kv = (unsigned)a.c.n_kv_heads;
     if (p.few) {
         const dim3 grid(p.few_shares ? (unsigned)p.few_shares : (unsigned)a.B * kv);
-        if (p.few_rows == 16) few<D, E4M3, 1>(a, grid, st);
-        else if (p.few_rows == 32) few<D, E4M3, 2>(a, grid, st);
-        else if constexpr (few_rows_of(D) > 32) few<D, E4M3, 4>(a, grid, st);
+        if (p.few_rows == 16) few<D, E4M3, 1>(a, p.stream, grid, st);
+        else if (p.few_rows == 32) few<D, E4M3, 2>(a, p.stream, grid, st);
+        else if constexpr (few_rows_of(D) > 32) few<D, E4M3, 4>(a, p.stream, grid, st);
         SP_HIP_CHECK(hipGetLastError());
         if (p.few_shares) {
             // four waves a row where a line has many parts
