@@ -116,24 +116,34 @@ __device__ __forceinline__ int page_entry(const AttendArgs &a, int b, uint32_t i
     return page >= (int)a.c.n_pages ? (int)a.c.n_pages - 1 : page;
 }
 
-// Eight E4M3 codes as eight bf16, exactly: the upper halves of their float images.
+// Two E4M3 codes of a word (the lower or the upper two) as bf16, exactly.
+template <bool UPPER>
+__device__ __forceinline__ uint32_t widen2(uint32_t w)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.f, UPPER));
+}
+
 __device__ __forceinline__ bf16x8 widen8(uint32_t c0, uint32_t c1)
 {
-    u32x4 r;
-    const uint32_t w[2] = {c0, c1};
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
-        r[2 * i] = __builtin_amdgcn_perm(__float_as_uint(lo.y), __float_as_uint(lo.x), 0x07060302u);
-        r[2 * i + 1] = __builtin_amdgcn_perm(__float_as_uint(hi.y), __float_as_uint(hi.x), 0x07060302u);
-    }
-    return __builtin_bit_cast(bf16x8, r);
+    return __builtin_bit_cast(bf16x8, u32x4{widen2<false>(c0), widen2<true>(c0), widen2<false>(c1), widen2<true>(c1)});
+}
+
+// Four codes each of two keys: element i's pair of them as bf16.
+__device__ __forceinline__ void widen_pairs(uint32_t x, uint32_t y, uint32_t (&pair)[4])
+{
+    const uint32_t lo = __builtin_amdgcn_perm(y, x, 0x05010400u), hi = __builtin_amdgcn_perm(y, x, 0x07030602u);
+    pair[0] = widen2<false>(lo);
+    pair[1] = widen2<true>(lo);
+    pair[2] = widen2<false>(hi);
+    pair[3] = widen2<true>(hi);
 }
 
 // A scalar address that moves, and loads at a lane's 32-bit offset from it: a load takes both as they are. What the compiler does not know to stay
 // the same in a loop (asm) it does not add up beforehand, which would cost two vector operations for each load.
 struct Moving {
     uint64_t p;
+
+    Moving() = default;
 
     __device__ __forceinline__ explicit Moving(const uint8_t *at) : p(reinterpret_cast<uint64_t>(at)) { asm("" : "+s"(p)); }
 
@@ -166,8 +176,11 @@ struct Line {
     int64_t page_bytes;
     uint32_t row_bytes, page_scales;
 
-    __device__ __forceinline__ Line(const AttendArgs &a, int kvh, int es)
+    const int32_t *table;
+
+    __device__ __forceinline__ Line(const AttendArgs &a, int b, int kvh, int es)
     {
+        table = a.c.table + b * a.c.table_stride;
         k = a.k_pool + kvh * a.c.stride_head * es;
         v = a.v_pool + kvh * a.c.stride_head * es;
         ks = a.k_scale + (int64_t)kvh * a.page_blocks;
@@ -187,10 +200,10 @@ struct Entry {
     int page;
     uint32_t in_page;
 
-    __device__ __forceinline__ Entry(const AttendArgs &a, int b, int blk)
+    __device__ __forceinline__ Entry(const AttendArgs &a, const Line &l, int blk)
     {
         const uint32_t i = page_of_block(a, (uint32_t)blk);
-        page = a.c.table[b * a.c.table_stride + i];
+        page = l.table[i];
         in_page = (uint32_t)blk - i * (uint32_t)a.page_blocks;
     }
 
@@ -267,14 +280,10 @@ struct Block {
 #pragma unroll
             for (int p = 0; p < 4; ++p) {                           // keys 2p and 2p + 1
                 if (E4M3) {
+                    uint32_t pair[4];
+                    widen_pairs(v[2 * p][i], v[2 * p + 1][i], pair);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const f32x2 x = h ? __builtin_amdgcn_cvt_pk_f32_fp8((int)v[2 * p][i], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)v[2 * p][i], false);
-                        const f32x2 y = h ? __builtin_amdgcn_cvt_pk_f32_fp8((int)v[2 * p + 1][i], true)
-                                          : __builtin_amdgcn_cvt_pk_f32_fp8((int)v[2 * p + 1][i], false);
-                        r[4 * i + 2 * h][p] = __builtin_amdgcn_perm(__float_as_uint(y.x), __float_as_uint(x.x), 0x07060302u);
-                        r[4 * i + 2 * h + 1][p] = __builtin_amdgcn_perm(__float_as_uint(y.y), __float_as_uint(x.y), 0x07060302u);
-                    }
+                    for (int e = 0; e < 4; ++e) r[4 * i + e][p] = pair[e];
                 } else {
                     r[2 * i][p] = __builtin_amdgcn_perm(v[2 * p + 1][i], v[2 * p][i], 0x05040100u);
                     r[2 * i + 1][p] = __builtin_amdgcn_perm(v[2 * p + 1][i], v[2 * p][i], 0x07060302u);
@@ -491,7 +500,7 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
 
     Rows<D, MT> acc;
     acc.clear();
-    const Line line(a, kvh, E4M3 ? 1 : 2);
+    const Line line(a, b, kvh, E4M3 ? 1 : 2);
     const uint32_t k_lane = c * line.row_bytes + 16 * g, v_lane = 4 * g * line.row_bytes + c * (D / 16) * (E4M3 ? 1 : 2);
     // The next block's keys are loaded once this one's are in the first product, its values once these are in operand form. Block table entries
     // are requested two blocks ahead.
@@ -499,13 +508,13 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
     int blk = from + wave;
     if (blk < to) {
         const auto next = [&](int x) { return x + kWaves < to ? x + kWaves : x; };
-        const Place here = Entry(a, b, blk).place(a, line);
-        Entry soon(a, b, next(blk));
+        const Place here = Entry(a, line, blk).place(a, line);
+        Entry soon(a, line, next(blk));
         kv.load_keys(line, here, k_lane);
         kv.load_values(line, here, v_lane);
         for (;;) {
             const int ahead = next(blk), key0 = blk * kBlock;
-            const Entry later(a, b, next(ahead));
+            const Entry later(a, line, next(ahead));
             const bool whole = key0 >= all_lo && key0 + kBlock <= all_hi;
             f32x4 s0[MT], s1[MT];
             {
@@ -813,19 +822,14 @@ struct Stage {
         value_key = 32 * (value_octet >> 2) + 16 * ((value_octet >> 1) & 1) + 4 * (value_octet & 1) + 8 * value_half;
     }
 
-    // Where a wave loads from, tile after tile: a pointer that moves along a page and is looked up again at its end. Behind the last
-    // page it stays where it is: what is loaded there is masked.
+    // Where a wave loads from, tile after tile. At a page's end the next table entry is requested, which the next tile's loads look at. Behind
+    // the last page it goes back to that page's beginning: what is loaded there is masked.
     struct Cursor {
-        const uint8_t *p;
+        int entry;
         uint32_t in, page;                                      // block of the page; place in the block table
     };
 
-    __device__ __forceinline__ static const uint8_t *place(const AttendArgs &a, const uint8_t *pool, int b, int kvh, const Cursor &c)
-    {
-        return pool + (page_entry(a, b, c.page) * a.c.page_stride + kvh * a.c.stride_head + (int64_t)(c.in * kBlock) * a.c.stride_token) * ES;
-    }
-
-    __device__ __forceinline__ static Cursor cursor(const AttendArgs &a, const uint8_t *pool, int b, int kvh, uint32_t blk, uint32_t last_page)
+    __device__ __forceinline__ static Cursor cursor(const AttendArgs &a, const int32_t *table, uint32_t blk, uint32_t last_page)
     {
         Cursor c;
         c.page = page_of_block(a, blk);
@@ -834,25 +838,28 @@ struct Stage {
             c.page = last_page;
             c.in = 0;
         }
-        c.p = place(a, pool, b, kvh, c);
+        c.entry = table[c.page];
         return c;
     }
 
-    __device__ __forceinline__ static void advance(const AttendArgs &a, const uint8_t *pool, int b, int kvh, uint32_t last_page, Cursor &c)
+    // The address of the cursor's block; moves it to the next tile's.
+    __device__ __forceinline__ static Moving next(const AttendArgs &a, const Line &l, const uint8_t *pool, uint32_t last_page, Cursor &c)
     {
+        const int p = min(max(__builtin_amdgcn_readfirstlane(c.entry), 0), (int)a.c.n_pages - 1);       // never outside the pools
+        const Moving at(pool + p * l.page_bytes + (int64_t)((uint64_t)c.in * (kBlock * l.row_bytes)));
         c.in += kBlocks;
-        if (c.in < (uint32_t)a.page_blocks) {
-            c.p += (int64_t)kKeys * a.c.stride_token * ES;
-            return;
+        if (c.in >= (uint32_t)a.page_blocks) {
+            do {
+                c.in -= a.page_blocks;
+                ++c.page;
+            } while (c.in >= (uint32_t)a.page_blocks);
+            if (c.page > last_page) {
+                c.page = last_page;
+                c.in = 0;
+            }
+            c.entry = l.table[c.page];
         }
-        uint32_t page = c.page;
-        do {
-            c.in -= a.page_blocks;
-            ++page;
-        } while (c.in >= (uint32_t)a.page_blocks);
-        if (page > last_page) return;
-        c.page = page;
-        c.p = place(a, pool, b, kvh, c);
+        return at;
     }
 
     struct Cursors {
@@ -867,13 +874,13 @@ struct Stage {
         return scales + ((int64_t)page_entry(a, b, c.scale_page) * a.c.n_kv_heads + kvh) * a.page_blocks + c.scale_in;
     }
 
-    __device__ __forceinline__ Cursors cursors(const AttendArgs &a, int b, int kvh, uint32_t blk, uint32_t last_page) const
+    __device__ __forceinline__ Cursors cursors(const AttendArgs &a, const Line &l, int b, int kvh, uint32_t blk, uint32_t last_page) const
     {
         Cursors c;
 #pragma unroll
         for (int i = 0; i < kKeyLoads; ++i)
-            c.key[i] = cursor(a, a.k_pool, b, kvh, blk + __builtin_amdgcn_readfirstlane((key_row + i * (kManyThreads / kKeyLanes)) / kBlock), last_page);
-        c.value = cursor(a, a.v_pool, b, kvh, blk + __builtin_amdgcn_readfirstlane(value_octet >> 2), last_page);
+            c.key[i] = cursor(a, l.table, blk + __builtin_amdgcn_readfirstlane((key_row + i * (kManyThreads / kKeyLanes)) / kBlock), last_page);
+        c.value = cursor(a, l.table, blk + __builtin_amdgcn_readfirstlane(value_octet >> 2), last_page);
         if (E4M3) {
             const uint32_t mine = blk + threadIdx.x % kBlocks;
             c.scale_page = min(page_of_block(a, mine), last_page);
@@ -884,26 +891,26 @@ struct Stage {
     }
 
     // Loads the tile at the cursors and moves them to the next.
-    __device__ __forceinline__ void load(const AttendArgs &a, int b, int kvh, uint32_t last_page, Cursors &c, Raw &w) const
+    __device__ __forceinline__ void load(const AttendArgs &a, const Line &l, int b, int kvh, uint32_t last_page, Cursors &c, Raw &w) const
     {
-        const int64_t row = a.c.stride_token * ES;
+        Moving k[kKeyLoads];
 #pragma unroll
-        for (int i = 0; i < kKeyLoads; ++i) {
-            const uint32_t lane = (key_row + i * (kManyThreads / kKeyLanes)) % kBlock * (uint32_t)row + key_col * 16;
-            w.k[i] = *reinterpret_cast<const u32x4 *>(c.key[i].p + lane);
-            advance(a, a.k_pool, b, kvh, last_page, c.key[i]);
-        }
-        const uint32_t lane = value_key % kBlock * (uint32_t)row + value_col * 4 * ES;
+        for (int i = 0; i < kKeyLoads; ++i) k[i] = next(a, l, l.k, last_page, c.key[i]);
+        Moving v = next(a, l, l.v, last_page, c.value);
+#pragma unroll
+        for (int i = 0; i < kKeyLoads; ++i)
+            w.k[i] = k[i].template load<u32x4>(opaque((key_row + i * (kManyThreads / kKeyLanes)) % kBlock * l.row_bytes + key_col * 16));
+        const uint32_t lane = opaque(value_key % kBlock * l.row_bytes + value_col * 4 * ES);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if constexpr (E4M3) w.v[j][0] = *reinterpret_cast<const uint32_t *>(c.value.p + j * row + lane);
+            if constexpr (E4M3) w.v[j][0] = v.template load<uint32_t>(lane);
             else {
-                const u32x2 x = *reinterpret_cast<const u32x2 *>(c.value.p + j * row + lane);
+                const u32x2 x = v.template load<u32x2>(lane);
                 w.v[j][0] = x[0];
                 w.v[j][1] = x[1];
             }
+            v.advance(l.row_bytes);
         }
-        advance(a, a.v_pool, b, kvh, last_page, c.value);
         if (E4M3 && threadIdx.x < 2 * kBlocks) {
             w.scale = *c.scale;
             c.scale += kBlocks;
@@ -948,12 +955,10 @@ struct Stage {
 #pragma unroll
         for (int p = 0; p < 2; ++p)
             if constexpr (E4M3) {
-                const f32x2 x0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)v[2 * p][0], false), x1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)v[2 * p][0], true);
-                const f32x2 y0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)v[2 * p + 1][0], false), y1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)v[2 * p + 1][0], true);
-                r[0][p] = __builtin_amdgcn_perm(__float_as_uint(y0.x), __float_as_uint(x0.x), 0x07060302u);
-                r[1][p] = __builtin_amdgcn_perm(__float_as_uint(y0.y), __float_as_uint(x0.y), 0x07060302u);
-                r[2][p] = __builtin_amdgcn_perm(__float_as_uint(y1.x), __float_as_uint(x1.x), 0x07060302u);
-                r[3][p] = __builtin_amdgcn_perm(__float_as_uint(y1.y), __float_as_uint(x1.y), 0x07060302u);
+                uint32_t pair[4];
+                widen_pairs(v[2 * p][0], v[2 * p + 1][0], pair);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) r[e][p] = pair[e];
             } else
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
@@ -1028,16 +1033,17 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
         const uint32_t last_page = page_of_block(a, last_blk);
         const int last_tile = (to - from + kKeys - 1) / kKeys - 1;
         typename S::Raw ra, rb;
-        typename S::Cursors cur = st.cursors(a, t.b, kvh, (uint32_t)(from / kBlock), last_page);
-        st.load(a, t.b, kvh, last_page, cur, ra);
-        st.load(a, t.b, kvh, last_page, cur, rb);
+        const Line line(a, t.b, kvh, S::ES);
+        typename S::Cursors cur = st.cursors(a, line, t.b, kvh, (uint32_t)(from / kBlock), last_page);
+        st.load(a, line, t.b, kvh, last_page, cur, ra);
+        st.load(a, line, t.b, kvh, last_page, cur, rb);
         st.store(ra, keys[0], values[0], scales[0], from, t.lo, t.hi);
         __syncthreads();
         // Tile n is taken from buffer n % 2, while tile n + 1 lies in `ready`, loaded or under way, and tile n + 2 is requested into `fresh`.
         const auto take = [&](int n, int buf, typename S::Raw &ready, typename S::Raw &fresh) {
             const int key0 = from + n * kKeys;
             const bool more = n < last_tile;
-            if (n + 2 <= last_tile) st.load(a, t.b, kvh, last_page, cur, fresh);
+            if (n + 2 <= last_tile) st.load(a, line, t.b, kvh, last_page, cur, fresh);
             if (busy && key0 < any_hi && key0 + kKeys > any_lo) {
                 const bool whole = key0 >= all_lo && key0 + kKeys <= all_hi;
                 // Two blocks at a time: two independent chains of the first product, one look at the reference. Operands are read from LDS a group of
@@ -1096,7 +1102,7 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
                             const float vs = fmaxf(scales[buf][kBlocks + u + w], kLeastScale);
                             sc[w] = fmaxf(sc[w] * scales[buf][u + w], kLeastFactor);
                             vexp[w] = log2_(vs);
-                            vinv[w] = 1.f / vs;
+                            vinv[w] = __builtin_amdgcn_rcpf(vs);
                         }
                         float y = x[w][0];
 #pragma unroll
