@@ -478,7 +478,7 @@ typedef enum { SP_ROTATE_HALF = 0, SP_ROTATE_PAIRS = 1 } sp_rotate_style;
  * (optionally) queries to their positions on the way. Request b brings tokens
  * [offsets[b], offsets[b+1]) of the packed inputs (offsets in host and in device
  * memory, the same B+1 non-decreasing values, offsets[0] == 0; 0 <= B <= 4096,
- * requests without new tokens are allowed, at most 2^28 new tokens in all).
+ * requests without new tokens are allowed; (new tokens / 32 + 2 B) * n_kv_heads < 2^24).
  * Its i-th new token becomes token start_dev[b] + i of its cache.
  *  - k_dev, v_dev: bf16, token t at t * k_stride (v_stride), n_kv_heads * head_dim
  *    contiguous elements each; strides in elements, multiples of 8 (so keys, values and

@@ -20,7 +20,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kBlock = sp::kCacheBlock;
 constexpr float kFloorExp = -64;        // log2 of the smallest scale
-constexpr int64_t kMaxTokens = int64_t(1) << 28;    // a launch's threads fit 32 bits
+constexpr int64_t kMaxGroups = int64_t(1) << 24;    // a launch's threads fit 32 bits
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
@@ -38,7 +38,7 @@ struct AppendArgs {
     uint8_t *k_pool, *v_pool;
     float *k_scale, *v_scale;
     int32_t B, rot;
-    bool single;        // no request brings more than one token: workgroup x belongs to request x
+    bool single;        // no request brings more than one token: item x belongs to request x
 };
 
 __device__ __forceinline__ void unpack(u32x4 w, float (&x)[8])
@@ -144,7 +144,7 @@ __device__ __forceinline__ u32x2 rescale(u32x2 c, float ratio)
     return r;
 }
 
-// Which request workgroup x works for, and which of its blocks of slots. Request b's workgroups begin at
+// Which request item x (a block of slots) belongs to, and which of its blocks that is. Request b's items begin at
 // off[b] / 32 + 2 b: enough, since n tokens from any slot touch at most n / 32 + 2 blocks (rounded down).
 __device__ __forceinline__ int find_request(const AppendArgs &a, int x, int64_t *first)
 {
@@ -168,14 +168,16 @@ __global__ __launch_bounds__(kThreads) void sp_cache_append_kernel(AppendArgs a)
     constexpr int kParts = kThreads / (kBlock * kVecs); // 2 at head_dim 64: half the threads take keys, half values
     __shared__ uint32_t wave_max[2][kThreads / 64];
 
+    // the kv heads of the same tokens side by side: their parts of a token's row are neighbours in memory
+    const uint32_t x = blockIdx.x / (uint32_t)a.c.n_kv_heads;
     int64_t first;
-    const int b = find_request(a, blockIdx.x, &first);
+    const int b = find_request(a, (int)x, &first);
     const int64_t t0 = a.off[b], n = a.off[b + 1] - t0;
     const int64_t start = a.start[b] > 0 ? a.start[b] : 0, end = start + n;
-    const int64_t slot0 = (start / kBlock + (blockIdx.x - first)) * kBlock;
+    const int64_t slot0 = (start / kBlock + ((int64_t)x - first)) * kBlock;
     if (n == 0 || slot0 >= end) return;
 
-    const int kvh = blockIdx.y, tid = threadIdx.x;
+    const int kvh = blockIdx.x % (uint32_t)a.c.n_kv_heads, tid = threadIdx.x;
     const int part = kParts == 2 ? tid / (kThreads / 2) : 0, slot = tid / kVecs % kBlock, vec = tid % kVecs;
     const int64_t at = slot0 + slot;
     const bool fresh = at >= start && at < end, older = at < start;
@@ -314,7 +316,6 @@ extern "C" sp_status sp_cache_append(const sp_cache_desc *desc, const void *k_de
         return sp::fail(SP_ERR_INVALID_ARG, "rot_style = %d is neither SP_ROTATE_HALF nor SP_ROTATE_PAIRS", rot_style);
     if (table_stride < 1 || table_stride > (int64_t(1) << 31))
         return sp::fail(SP_ERR_INVALID_ARG, "table_stride = %lld outside 1..2^31", (long long)table_stride);
-    if (total > kMaxTokens) return sp::fail(SP_ERR_UNSUPPORTED, "%lld new tokens exceed 2^28", (long long)total);
     if (total == 0) return SP_OK;
     if (!k_dev || !v_dev) return sp::fail(SP_ERR_INVALID_ARG, "k_dev or v_dev is null");
     if (!q_dev != !q_out_dev) return sp::fail(SP_ERR_INVALID_ARG, "q_dev and q_out_dev come together or not at all");
@@ -333,13 +334,18 @@ extern "C" sp_status sp_cache_append(const sp_cache_desc *desc, const void *k_de
         return sp::fail(SP_ERR_INVALID_ARG, "keys, values and queries must be 16-byte aligned");
     if (sp_status rc = sp::check_pools(*desc, k_pool_dev, v_pool_dev, k_scale_dev, v_scale_dev)) return rc;
 
+    const bool single = longest <= 1;
+    const int64_t groups = (single ? B : total / kBlock + 2 * (int64_t)B) * desc->n_kv_heads;
+    if (groups >= kMaxGroups)
+        return sp::fail(SP_ERR_UNSUPPORTED, "%lld new tokens of %d kv heads are more than a launch holds", (long long)total, desc->n_kv_heads);
+
     AppendArgs a{sp::view_of(*desc, block_table_dev, table_stride),
                  static_cast<const uint16_t *>(k_dev), static_cast<const uint16_t *>(v_dev),
                  static_cast<const uint16_t *>(q_dev), static_cast<uint16_t *>(q_out_dev),
                  k_stride, v_stride, q_stride, offsets_dev, start_dev, positions_dev, cos_dev, sin_dev, n_pos,
                  static_cast<uint8_t *>(k_pool_dev), static_cast<uint8_t *>(v_pool_dev), k_scale_dev, v_scale_dev,
-                 B, rot_dim, longest <= 1};
-    const dim3 grid((unsigned)(a.single ? B : total / kBlock + 2 * (int64_t)B), (unsigned)desc->n_kv_heads);
+                 B, rot_dim, single};
+    const dim3 grid((unsigned)groups);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const bool pairs = rot_style == SP_ROTATE_PAIRS;
     if (desc->head_dim == 64)
