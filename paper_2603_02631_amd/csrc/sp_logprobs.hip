@@ -116,11 +116,15 @@ struct Row {
 
     __device__ __forceinline__ bool whole(uint32_t c) const { return index(c, 0) >= 0 && index(c, E) <= vocab; }
 
-    // Logits of a chunk; -inf in the places that are not the row's, which are not read.
+    // Logits of a chunk; -inf in the places that are not the row's, which are not read. ONCE: they pass the caches by.
+    template <bool ONCE = false>
     __device__ __forceinline__ void load(uint32_t c, float (&x)[E]) const
     {
         if (whole(c)) {
-            const u32x4 w = *reinterpret_cast<const u32x4 *>(base + (int64_t)c * 16);
+            const u32x4 *p = reinterpret_cast<const u32x4 *>(base + (int64_t)c * 16);
+            u32x4 w;
+            if constexpr (ONCE) w = __builtin_nontemporal_load(p);
+            else w = *p;
 #pragma unroll
             for (int e = 0; e < E; ++e)
                 x[e] = BF16 ? __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16) : __uint_as_float(w[e % 4]);
@@ -175,7 +179,7 @@ struct Shared {
     uint32_t bound, last, columns, found;
 };
 
-template <bool BF16, int kThreads>
+template <bool BF16, int kThreads, bool ONCE>
 __global__ __launch_bounds__(kThreads) void sp_logprobs_kernel(Args a)
 {
     __shared__ Shared<kThreads> sh;
@@ -195,7 +199,7 @@ __global__ __launch_bounds__(kThreads) void sp_logprobs_kernel(Args a)
 #pragma unroll
         for (int i = 0; i < kUnroll; ++i) {
             const uint32_t c = c0 + i * kThreads;
-            if (c < to) row.load(c, x[i]);
+            if (c < to) row.template load<ONCE>(c, x[i]);
             else
 #pragma unroll
                 for (int e = 0; e < E; ++e) x[i][e] = neg_inf();
@@ -414,6 +418,10 @@ __global__ __launch_bounds__(kJoinThreads) void sp_logprobs_join_kernel(Args a)
 // threads and 26 with 512, 300 rows of 128000 bf16 ones 48 and 33.
 constexpr int64_t kShort = 2048;
 
+// Long rows are read past the caches where they are fp32 (1000 rows of 50000 40.4 us without, 37.8 with), and of bf16 where they are more bytes than the
+// last cache holds: 4096 rows of 128000 195 and 190, but 600 42.7 and 43.1, 300 called again and again 32.5 and 37.6.
+constexpr int64_t kOnce = int64_t(1) << 28;
+
 // Segments of a row: as many as keep the device busy (two workgroups of 512 threads on each of 256 compute units), each worth its launch.
 int splits_of(int64_t n_rows, int64_t vocab)
 {
@@ -446,8 +454,9 @@ sp_status run(const Args &a, int64_t n_rows, hipStream_t st)
             b.top_logprobs += r0 * a.n_top;
         }
         const dim3 grid((unsigned)a.splits, (unsigned)n);
-        if (a.vocab <= kShort * (BF16 ? 8 : 4)) hipLaunchKernelGGL((sp_logprobs_kernel<BF16, 256>), grid, dim3(256), 0, st, b);
-        else hipLaunchKernelGGL((sp_logprobs_kernel<BF16, 512>), grid, dim3(512), 0, st, b);
+        if (a.vocab <= kShort * (BF16 ? 8 : 4)) hipLaunchKernelGGL((sp_logprobs_kernel<BF16, 256, false>), grid, dim3(256), 0, st, b);
+        else if (!BF16 || n_rows * a.vocab * 2 > kOnce) hipLaunchKernelGGL((sp_logprobs_kernel<BF16, 512, true>), grid, dim3(512), 0, st, b);
+        else hipLaunchKernelGGL((sp_logprobs_kernel<BF16, 512, false>), grid, dim3(512), 0, st, b);
         SP_HIP_CHECK(hipGetLastError());
     }
     if (a.splits > 1) {

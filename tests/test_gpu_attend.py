@@ -299,3 +299,10 @@ def test_a_nan_that_is_seen_gets_out(e4m3, news, lens):
             assert np.isfinite(np.delete(out[:n, 2:], 5, axis=2)).all()
         assert np.isfinite(out[:n, :2]).all() and np.isfinite(lse[:n, :2]).all()
         assert np.isfinite(out[n:]).all() and np.isfinite(lse[n:]).all()
+
+
+@pytest.mark.parametrize("news", [[1, 3], [30, 8], [60, 64]])
+def test_contexts_that_may_be_larger_than_a_cache(news):
+    """A bound of 2^20 tokens a request: keys are read past the caches, work is shared out as for the longest lengths."""
+    check(4, 4, 64, news, [700, 65], 512, True, max_len=1 << 20)
+    check(2, 2, 128, news, [700, 65], 512, False, max_len=1 << 20)

@@ -188,3 +188,21 @@ def test_logprobs_with_the_best_thousands_in_a_few_places(bf16, width, rows):
     np.testing.assert_allclose(got[3][0], lps, atol=1e-4)
     for a in got:
         assert (a == a[:1]).all()
+
+
+def test_more_logits_than_a_cache_holds():
+    """Rows of bf16 that are read past the caches; three of them against the definition."""
+    rows, vocab, n_top = 1100, 130001, 4
+    torch.manual_seed(3)
+    t = (torch.randn(rows, vocab, device=DEV) * 3).to(torch.bfloat16)
+    targets = np.arange(rows) * 7
+    got = call(t, rows, vocab, targets, n_top)
+    rel = (vocab / 64 + 20) * 2.0 ** -24 + 2.0 ** -17
+    for r in (0, 517, 1099):
+        x = t[r].float().cpu().numpy()
+        lp, h, ids, lps, mean = ou.logprobs(x, int(targets[r]), n_top)
+        assert got[2][r].tolist() == ids
+        big = np.abs(x).max()
+        assert close(got[0][r], lp, rel + 2.0 ** -22 * (abs(lp) + big))
+        assert close(got[1][r], h, 2 * rel * (1 + mean) + 2.0 ** -22 * h)
+        assert all(close(a, b, rel + 2.0 ** -22 * (abs(b) + big)) for a, b in zip(got[3][r], lps))
