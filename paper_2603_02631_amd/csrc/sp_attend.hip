@@ -1046,6 +1046,8 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
             if (n + 2 <= last_tile) st.load(a, line, t.b, kvh, last_page, cur, fresh);
             if (busy && key0 < any_hi && key0 + kKeys > any_lo) {
                 const bool whole = key0 >= all_lo && key0 + kKeys <= all_hi;
+                // Of the two waves of a SIMD the one in its softmax goes first, then one that stores a tile, then one in the first product, so that products run beside
+                // vector operations (four chunks of 512 rows over 8192 tokens at head_dim 64 171 -> 168 us, a prompt of 8192 at 128 282 -> 280).
                 // Two blocks at a time: two independent chains of the first product, one look at the reference. Operands are read from LDS a group of
                 // products ahead; the scheduling barriers keep the reads (not vector operations) from being moved behind the products (2048 rows
                 // after 32K tokens 605 -> 570 us). At head_dim 64 they gain nothing: 347 with, 344 without on a whole prompt of 8192.
@@ -1065,6 +1067,7 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
                     for (int w = 0; w < 2; ++w)
 #pragma unroll
                         for (int e = 0; e < 16; ++e) x[w][e] = 0.f;
+                    __builtin_amdgcn_s_setprio(0);
                     read_keys(0, 0);
 #pragma unroll
                     for (int s0 = 0; s0 < kSteps; s0 += kGroup) {
@@ -1075,6 +1078,7 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
                             for (int w = 0; w < 2; ++w) x[w] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s0 / kGroup & 1][s][w], q[s0 + s], x[w], 0, 0, 0);
                         if constexpr (D == 128) __builtin_amdgcn_sched_barrier(kVectorOnly);
                     }
+                    __builtin_amdgcn_s_setprio(3);
                     bf16x8 vf[2][kOut];
                     const auto read_values = [&](int to, int part) {        // part: 16 keys
 #pragma unroll
@@ -1139,6 +1143,7 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
                     }
                 }
             }
+            __builtin_amdgcn_s_setprio(1);
             if (more) st.store(ready, keys[buf ^ 1], values[buf ^ 1], scales[buf ^ 1], key0 + kKeys, t.lo, t.hi);
             __syncthreads();
         };
@@ -1276,12 +1281,13 @@ sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64
     p->tiles = (int32_t)tiles;
     p->many_count = requests <= kManyList ? (int32_t)requests : 0;
 
-    // Few rows: as many workgroups as are resident at once (by the registers of each variant), unless contexts are so short that a
-    // line is best taken whole: a block of a line takes 0.2 us (0.3 at head_dim 128), sharing out about 5 for its second launch, and more with the number of lines.
+    // Few rows: shared out unless contexts are so short that a line is best taken whole: a block of a line takes 0.2 us (0.3 at head_dim 128), sharing out about 5 for its second launch, and more with the number of lines.
     // Single tokens over 8 kv heads of 64, whole and shared: 8 contexts of 1000 tokens 9.5 and 11.4 us, of up to 4000 15.5 and 13.0; 64 of 1000 15.2 and 20.4, of
     // up to 4000 28.8 and 28.2. At most 128 blocks, since one long line among many short ones would then be what takes the time.
     const int64_t blocks = sp::ceil_div(max_len, kBlock) + 1, lines = B * kv;
-    const int64_t resident = kUnits * (D == 64 ? (p->few_rows == 16 ? 4 : p->few_rows == 32 ? 3 : 2) : (p->few_rows == 16 ? 2 : 1));
+    // On each compute unit: four, three and two would be resident at head_dim 64 with 16, 32 and 64 rows, two and one at 128; one less reads as fast and leaves
+    // fewer parts to join (8 tokens over 131072 40.9 and 36.5 us, 32 requests of bf16 at 128 160 and 154), but for 64 rows (61 and 72).
+    const int64_t spread = kUnits * (D == 64 ? (p->few_rows == 16 ? 3 : 2) : 1);
     const int64_t whole = (lines < 320 ? 48 + lines / 4 : 128) * 64 / D;
     // Joining takes longer with more parts of a line, its stretches with fewer: the best size grows with the root of the length (one context of 2000
     // tokens: at least 4 or 16 blocks 12.1 and 14.2 us; of 32768: 8 or 16 blocks 17.8 and 15.4).
@@ -1289,7 +1295,7 @@ sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64
     p->few_least = 4;
     while (8 * p->few_least * p->few_least < blocks) p->few_least *= 2;
     const int64_t most = sp::ceil_div(blocks * lines, p->few_least);
-    p->few_shares = !p->few || blocks <= whole ? 0 : (int32_t)(resident < most ? resident : most);
+    p->few_shares = !p->few || blocks <= whole ? 0 : (int32_t)(spread < most ? spread : most);
     // Many rows: where compute units would be left over, unless lines are short. Whole and shared, 8 kv heads: 512 rows of head_dim 64 over 512 tokens (five
     // tiles of keys) 17 and 26 us, 128 rows of head_dim 128 over 500 (nine) 24 and 23, over 1500 56 and 25; but 6000 over 6000 (384 lines) 197 and 253.
     const int64_t spans = sp::ceil_div(max_len, 8192 / D) + 1, most_many = spans * tiles * kv;
