@@ -683,7 +683,7 @@ template <int D, int WAVES>
 __device__ __forceinline__ void join_row(const AttendArgs &a, const f32x2 *ml, const float *po, int rows, int r, const Parts &parts, int64_t row)
 {
     __shared__ float part[kWaves][D];
-    constexpr int kAhead = 8;                               // partial results under way
+    constexpr int kAhead = WAVES == 1 ? 4 : 8;              // partial results under way
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, part_wave = wave % WAVES, count = parts.count;
     const auto at = [&](int s) { return (int64_t)parts.slot(s) * rows + r; };
     float x[kAhead][D / 64], acc[D / 64] = {}, m = neg_inf(), l = 0.f;
@@ -1217,21 +1217,24 @@ __global__ __launch_bounds__(kManyThreads) void sp_attend_many_kernel(AttendArgs
     }
 }
 
-constexpr int kJoinRows = 2;            // of a wave: finding a line's few parts takes longer than joining a row, but more rows wait for each other
+constexpr int join_rows(bool many_parts) { return many_parts ? 1 : 2 * kWaves; }      // of a workgroup
 
-template <int D>
+// Every row of the tiles whose line lies in more than one stretch: four waves a row where a line has many parts, else a wave for two rows (finding the
+// parts takes longer than joining them).
+template <int D, bool MANY_PARTS>
 __global__ __launch_bounds__(kThreads) void sp_attend_many_join_kernel(AttendArgs a)
 {
-    constexpr int kBlocksOfTile = kManyRows / (kWaves * kJoinRows);
-    const int x = blockIdx.x / kBlocksOfTile, r0 = (blockIdx.x % kBlocksOfTile * kWaves + (threadIdx.x >> 6)) * kJoinRows, kvh = blockIdx.y, G = a.c.group;
+    constexpr int kRows = MANY_PARTS ? 1 : 2, kBlocksOfTile = kManyRows / join_rows(MANY_PARTS);
+    const int x = blockIdx.x / kBlocksOfTile, kvh = blockIdx.y, G = a.c.group;
+    const int r0 = blockIdx.x % kBlocksOfTile * join_rows(MANY_PARTS) + (MANY_PARTS ? 0 : (threadIdx.x >> 6) * kRows);
     const int64_t before = a.many_before[x], n = a.many_before[x + 1] - before, total = a.many_before[a.tiles];
     const int64_t each = (total * a.c.n_kv_heads + a.many_shares - 1) / a.many_shares;
     if (n == 0) return;
     const Parts parts(kvh * total + before, kvh * total + before + n, each);
     Tile t;
     if (parts.count == 1 || !tile_of(a, few_rows_of(D), x, &t)) return;
-    for (int r = r0; r < min(r0 + kJoinRows, t.rows); ++r)
-        join_row<D, 1>(a, a.many_ml, a.many_o, kManyRows, r, parts, (a.off[t.b] + (t.row0 + r) / G) * a.c.n_q_heads + kvh * G + (t.row0 + r) % G);
+    for (int r = r0; r < min(r0 + kRows, t.rows); ++r)
+        join_row<D, MANY_PARTS ? kWaves : 1>(a, a.many_ml, a.many_o, kManyRows, r, parts, (a.off[t.b] + (t.row0 + r) / G) * a.c.n_q_heads + kvh * G + (t.row0 + r) % G);
 }
 
 // How a call is laid out: which kernels run, and on how many workgroups.
@@ -1281,14 +1284,16 @@ sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64
     p->tiles = (int32_t)tiles;
     p->many_count = requests <= kManyList ? (int32_t)requests : 0;
 
-    // Few rows: shared out unless contexts are so short that a line is best taken whole: a block of a line takes 0.2 us (0.3 at head_dim 128), sharing out about 5 for its second launch, and more with the number of lines.
-    // Single tokens over 8 kv heads of 64, whole and shared: 8 contexts of 1000 tokens 9.5 and 11.4 us, of up to 4000 15.5 and 13.0; 64 of 1000 15.2 and 20.4, of
-    // up to 4000 28.8 and 28.2. At most 128 blocks, since one long line among many short ones would then be what takes the time.
-    const int64_t blocks = sp::ceil_div(max_len, kBlock) + 1, lines = B * kv;
-    // On each compute unit: four, three and two would be resident at head_dim 64 with 16, 32 and 64 rows, two and one at 128; one less reads as fast and leaves
-    // fewer parts to join (8 tokens over 131072 40.9 and 36.5 us, 32 requests of bf16 at 128 160 and 154), but for 64 rows (61 and 72).
-    const int64_t spread = kUnits * (D == 64 ? (p->few_rows == 16 ? 3 : 2) : 1);
-    const int64_t whole = (lines < 320 ? 48 + lines / 4 : 128) * 64 / D;
+    // Few rows: shared out unless contexts are so short that a line is best taken whole. A block of a line takes 0.2 us (0.3 at head_dim 128), sharing out about
+    // five for its second launch, and more with the number of lines. Single tokens over 8 kv heads of 64, whole and shared: 8 contexts of 1000 tokens 9.5 and
+    // 11.4 us, of up to 4000 15.5 and 13.0; 64 of 1000 15.2 and 20.4, 200 of up to 4000 59.6 and 73. Of 128: 8 of 2000 22.7 and 18.0, 128 of up to 4000 77 and 90.
+    // At most 128 blocks, since one long line among many short ones would then be what takes the time.
+    const int64_t blocks = sp::ceil_div(max_len, kBlock) + 1, lines = B * kv, limit = 48 * 64 / D + lines / 4, whole = limit < 128 ? limit : 128;
+    // Workgroups of a compute unit: with as many lines as units what is resident (by registers), so that one reads while another changes lines (32 requests of up to
+    // 16000 tokens of E4M3, head_dim 128, 80 us with one, 74 with two); with fewer one less, which leaves fewer parts to join (8 tokens over 131072, head_dim 64,
+    // 40.9 us with three, 36.5 with two), but for 64 rows (72 with one, 61 with two).
+    const bool fill = lines >= kUnits || p->few_rows == 64;
+    const int64_t spread = kUnits * ((D == 64 ? (p->few_rows == 16 ? 4 : p->few_rows == 32 ? 3 : 2) : p->few_rows == 16 ? 2 : 1) - (fill || (D == 128 && p->few_rows > 16) ? 0 : 1));
     // Joining takes longer with more parts of a line, its stretches with fewer: the best size grows with the root of the length (one context of 2000
     // tokens: at least 4 or 16 blocks 12.1 and 14.2 us; of 32768: 8 or 16 blocks 17.8 and 15.4).
     p->stream = 2 * max_len * B * kv * D * (sp::cache_is_e4m3(*d) ? 1 : 2) > kStream;
@@ -1352,8 +1357,10 @@ sp_status run(const AttendArgs &a, const Plan &p, hipStream_t st)
         else hipLaunchKernelGGL((sp_attend_many_kernel<D, E4M3, false>), grid, dim3(kManyThreads), 0, st, a);
         SP_HIP_CHECK(hipGetLastError());
         if (p.many_shares) {
-            const dim3 rows((unsigned)(p.tiles * (kManyRows / (kWaves * kJoinRows))), kv);
-            hipLaunchKernelGGL((sp_attend_many_join_kernel<D>), rows, dim3(kThreads), 0, st, a);
+            const bool parts = p.many_shares > 8 * p.tiles * (int64_t)kv;
+            const dim3 rows((unsigned)(p.tiles * (kManyRows / join_rows(parts))), kv);
+            if (parts) hipLaunchKernelGGL((sp_attend_many_join_kernel<D, true>), rows, dim3(kThreads), 0, st, a);
+            else hipLaunchKernelGGL((sp_attend_many_join_kernel<D, false>), rows, dim3(kThreads), 0, st, a);
             SP_HIP_CHECK(hipGetLastError());
         }
     }
