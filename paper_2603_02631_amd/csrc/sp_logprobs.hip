@@ -422,10 +422,14 @@ constexpr int64_t kShort = 2048;
 // last cache holds: 4096 rows of 128000 195 and 190, but 600 42.7 and 43.1, 300 called again and again 32.5 and 37.6.
 constexpr int64_t kOnce = int64_t(1) << 28;
 
-// Segments of a row: as many as keep the device busy (two workgroups of 512 threads on each of 256 compute units), each worth its launch.
-int splits_of(int64_t n_rows, int64_t vocab)
+// Segments of a row: as many as keep the device busy (two workgroups of 512 threads on each of 256 compute units; one row of 131072 of bf16 20 us whole, 12.3 in
+// 32 segments), unless the row is read in less time than the second launch takes: whole and split, 8 rows of 32000 of bf16 8.7 and 10.5 us, 64 of 50021 11.8 and 12.6,
+// but one of 50000 of fp32 13.9 and 10.2.
+constexpr int64_t kWholeBytes = 7168 * 16;
+
+int splits_of(int64_t n_rows, int64_t vocab, int bytes)
 {
-    const int64_t want = n_rows > 0 ? 512 / n_rows : 1, most = vocab / kMinSplit;
+    const int64_t want = n_rows > 0 && vocab * bytes > kWholeBytes ? 512 / n_rows : 1, most = vocab / kMinSplit;
     const int64_t s = want < most ? want : most;
     return (int)(s < 1 ? 1 : (s > kMaxSplits ? kMaxSplits : s));
 }
@@ -477,7 +481,7 @@ extern "C" sp_status sp_logprobs_workspace(int64_t n_rows, int64_t vocab, int32_
         return sp::fail(SP_ERR_INVALID_ARG, "vocab = %lld outside 1..2^31-1", (long long)vocab);
     if (n_top < 0 || n_top > SP_LOGPROBS_MAX_TOP || n_top > vocab)
         return sp::fail(SP_ERR_INVALID_ARG, "n_top = %d outside 0..min(%d, vocab)", n_top, SP_LOGPROBS_MAX_TOP);
-    *bytes = workspace_need(n_rows, splits_of(n_rows, vocab), n_top);
+    *bytes = workspace_need(n_rows, splits_of(n_rows, vocab, 4), n_top);      // for both types
     return SP_OK;
 }
 
@@ -506,7 +510,7 @@ extern "C" sp_status sp_logprobs(const void *logits_dev, int32_t dtype, int64_t 
         if (ws_bytes < need) return sp::fail(SP_ERR_WORKSPACE, "workspace too small: %zu < %zu", ws_bytes, need);
     }
     Args a{static_cast<const uint8_t *>(logits_dev), vocab, row_stride, targets_dev, logprob_dev, entropy_dev, top_ids_dev,
-           top_logprobs_dev, n_top, splits_of(n_rows, vocab), static_cast<float *>(ws_dev), nullptr};
+           top_logprobs_dev, n_top, splits_of(n_rows, vocab, dtype == SP_LOGITS_F32 ? 4 : 2), static_cast<float *>(ws_dev), nullptr};
     a.part_keys = reinterpret_cast<uint64_t *>(static_cast<uint8_t *>(ws_dev) + keys_at(n_rows, a.splits));
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     return dtype == SP_LOGITS_BF16 ? run<true>(a, n_rows, st) : run<false>(a, n_rows, st);
