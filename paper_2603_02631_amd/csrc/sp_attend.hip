@@ -61,8 +61,12 @@ struct AttendArgs {
     f32x2 *many_ml;                     // as above, kManyRows rows
     float *many_o;
     int64_t *many_before;               // [tiles + 1]
-    // the requests with many rows and their first tiles, if there are at most kManyList of them (else many_count is 0)
-    int32_t many_count, many_b[kManyList], many_tile[kManyList];
+};
+
+// The requests with many rows and their first tiles, if there are at most kManyList of them (else count is 0). An argument of its own: the kernels for
+// few rows, whose calls are short, need not be given it.
+struct ManyList {
+    int32_t count, b[kManyList], tile[kManyList];
 };
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_huge_valf(); }
@@ -768,18 +772,18 @@ struct Tile {
     int lo, hi;
 };
 
-__device__ __forceinline__ bool tile_of(const AttendArgs &a, int few_rows, int x, Tile *t)
+__device__ __forceinline__ bool tile_of(const AttendArgs &a, const ManyList &list, int few_rows, int x, Tile *t)
 {
     const int G = a.c.group;
-    int lo = 0, hi = a.many_count ? a.many_count : a.B;
+    int lo = 0, hi = list.count ? list.count : a.B;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        const int64_t begin = a.many_count ? a.many_tile[mid] : a.off[mid] * G / kManyRows + mid;
+        const int64_t begin = list.count ? list.tile[mid] : a.off[mid] * G / kManyRows + mid;
         if (begin <= x) lo = mid; else hi = mid;
     }
-    t->b = a.many_count ? a.many_b[lo] : lo;
+    t->b = list.count ? list.b[lo] : lo;
     t->rg = range_of(a, t->b);
-    const int64_t row0 = (x - (a.many_count ? a.many_tile[lo] : a.off[lo] * G / kManyRows + lo)) * kManyRows, rows = (int64_t)t->rg.n * G - row0;
+    const int64_t row0 = (x - (list.count ? list.tile[lo] : a.off[lo] * G / kManyRows + lo)) * kManyRows, rows = (int64_t)t->rg.n * G - row0;
     if (t->rg.n <= few_rows / G || rows <= 0) return false;
     t->row0 = (int)row0;
     t->rows = (int)(rows < kManyRows ? rows : kManyRows);
@@ -1180,21 +1184,21 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
 }
 
 template <int D, bool E4M3, bool SHARED>
-__global__ __launch_bounds__(kManyThreads) void sp_attend_many_kernel(AttendArgs a)
+__global__ __launch_bounds__(kManyThreads) void sp_attend_many_kernel(AttendArgs a, ManyList list)
 {
     const int kv = a.c.n_kv_heads;
     Tile t;
     if constexpr (!SHARED) {
         // A line each. Neighbouring workgroups take different kv heads: with eight of them, each die's L2 holds one head's cache. Later
         // tiles of a prompt see more: they go first
-        if (tile_of(a, few_rows_of(D), a.tiles - 1 - blockIdx.x / kv, &t)) many_stretch<D, E4M3>(a, t, blockIdx.x % kv, 0, many_units<D>(t), -1);
+        if (tile_of(a, list, few_rows_of(D), a.tiles - 1 - blockIdx.x / kv, &t)) many_stretch<D, E4M3>(a, t, blockIdx.x % kv, 0, many_units<D>(t), -1);
     } else {
         // stretches of one kv head lie on one die, as far as they divide
         const int per_die = a.many_shares / 8, x = blockIdx.x;
         const int share = x < 8 * per_die ? x % 8 * per_die + x / 8 : x;
         const Start s = start_of<kManyThreads>(share, a.many_shares, a.tiles, kv, 1, a.many_before, [&](int j) {
             Tile u;
-            return tile_of(a, few_rows_of(D), j, &u) ? (int64_t)many_units<D>(u) : 0;
+            return tile_of(a, list, few_rows_of(D), j, &u) ? (int64_t)many_units<D>(u) : 0;
         });
         const int64_t all = s.total, end = min(s.pos + s.each, all * kv);   // units of a kv head; the stretch's end
         int64_t pos = s.pos, begin = s.before;
@@ -1208,7 +1212,7 @@ __global__ __launch_bounds__(kManyThreads) void sp_attend_many_kernel(AttendArgs
                 --part;
                 continue;
             }
-            const int n = tile_of(a, few_rows_of(D), i, &t) ? many_units<D>(t) : 0;
+            const int n = tile_of(a, list, few_rows_of(D), i, &t) ? many_units<D>(t) : 0;
             if (rel >= begin + n) {
                 begin += n;
                 ++i;
@@ -1227,7 +1231,7 @@ constexpr int join_rows(bool many_parts) { return many_parts ? 1 : 2 * kWaves; }
 // Every row of the tiles whose line lies in more than one stretch: four waves a row where a line has many parts, else a wave for two rows (finding the
 // parts takes longer than joining them).
 template <int D, bool MANY_PARTS>
-__global__ __launch_bounds__(kThreads) void sp_attend_many_join_kernel(AttendArgs a)
+__global__ __launch_bounds__(kThreads) void sp_attend_many_join_kernel(AttendArgs a, ManyList list)
 {
     constexpr int kRows = MANY_PARTS ? 1 : 2, kBlocksOfTile = kManyRows / join_rows(MANY_PARTS);
     const int x = blockIdx.x / kBlocksOfTile, kvh = blockIdx.y, G = a.c.group;
@@ -1237,7 +1241,7 @@ __global__ __launch_bounds__(kThreads) void sp_attend_many_join_kernel(AttendArg
     if (n == 0) return;
     const Parts parts(kvh * total + before, kvh * total + before + n, each);
     Tile t;
-    if (parts.count == 1 || !tile_of(a, few_rows_of(D), x, &t)) return;
+    if (parts.count == 1 || !tile_of(a, list, few_rows_of(D), x, &t)) return;
     for (int r = r0; r < min(r0 + kRows, t.rows); ++r)
         join_row<D, MANY_PARTS ? kWaves : 1>(a, a.many_ml, a.many_o, kManyRows, r, parts, (a.off[t.b] + (t.row0 + r) / G) * a.c.n_q_heads + kvh * G + (t.row0 + r) % G);
 }
@@ -1246,7 +1250,8 @@ __global__ __launch_bounds__(kThreads) void sp_attend_many_join_kernel(AttendArg
 struct Plan {
     int64_t total, most_few;            // query tokens in all; rows of a kv head of the largest request that has few
     bool few, many, stream;             // stream: contexts that no cache holds until the next call
-    int32_t few_rows, few_shares, few_least, tiles, many_shares, many_count, many_b[kManyList], many_tile[kManyList];
+    int32_t few_rows, few_shares, few_least, tiles, many_shares;
+    ManyList list;
     size_t few_o, few_before, many_ml, many_o, many_before, bytes;      // where the workspace's parts begin (few_ml at 0)
 };
 
@@ -1272,8 +1277,8 @@ sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64
         if (rows > few_rows_of(d->head_dim)) {
             p->many = true;
             if (requests < kManyList) {
-                p->many_b[requests] = b;
-                p->many_tile[requests] = (int32_t)used;
+                p->list.b[requests] = b;
+                p->list.tile[requests] = (int32_t)used;
             }
             ++requests;
             used += sp::ceil_div(rows, kManyRows);
@@ -1287,7 +1292,7 @@ sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64
     if (tiles * kv >= kMaxGroups || B * kv >= kMaxGroups)
         return sp::fail(SP_ERR_UNSUPPORTED, "%lld query rows of %d requests are more than a launch holds", (long long)(p->total * d->n_q_heads), B);
     p->tiles = (int32_t)tiles;
-    p->many_count = requests <= kManyList ? (int32_t)requests : 0;
+    p->list.count = requests <= kManyList ? (int32_t)requests : 0;
 
     // Few rows: shared out unless contexts are so short that a line is best taken whole. A block of a line takes 0.2 us (0.3 at head_dim 128), sharing out about
     // five for its second launch, and more with the number of lines. Single tokens over 8 kv heads of 64, whole and shared: 8 contexts of 1000 tokens 8.9 and
@@ -1310,7 +1315,7 @@ sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64
     // tiles of keys) 17 and 24 us, 128 rows of head_dim 128 over 500 (nine) 23 and 24, over 1500 51 and 25; but a prompt of 8192 (512 lines) 276 and 365.
     const int64_t spans = sp::ceil_div(max_len, 8192 / D) + 1, most_many = spans * tiles * kv;
     p->many_shares = 0;
-    if (p->many && p->many_count && spans > 8 && tiles * kv < kUnits) p->many_shares = (int32_t)(kUnits < most_many ? kUnits : most_many);
+    if (p->many && p->list.count && spans > 8 && tiles * kv < kUnits) p->many_shares = (int32_t)(kUnits < most_many ? kUnits : most_many);
 
     const size_t few = (size_t)2 * p->few_shares * p->few_rows, many = (size_t)2 * p->many_shares * kManyRows;
     p->few_o = sp::align_up(few * sizeof(f32x2), 256);
@@ -1358,14 +1363,14 @@ sp_status run(const AttendArgs &a, const Plan &p, hipStream_t st)
     }
     if (p.many) {
         const dim3 grid(p.many_shares ? (unsigned)p.many_shares : (unsigned)p.tiles * kv);
-        if (p.many_shares) hipLaunchKernelGGL((sp_attend_many_kernel<D, E4M3, true>), grid, dim3(kManyThreads), 0, st, a);
-        else hipLaunchKernelGGL((sp_attend_many_kernel<D, E4M3, false>), grid, dim3(kManyThreads), 0, st, a);
+        if (p.many_shares) hipLaunchKernelGGL((sp_attend_many_kernel<D, E4M3, true>), grid, dim3(kManyThreads), 0, st, a, p.list);
+        else hipLaunchKernelGGL((sp_attend_many_kernel<D, E4M3, false>), grid, dim3(kManyThreads), 0, st, a, p.list);
         SP_HIP_CHECK(hipGetLastError());
         if (p.many_shares) {
             const bool parts = p.many_shares > 8 * p.tiles * (int64_t)kv;
             const dim3 rows((unsigned)(p.tiles * (kManyRows / join_rows(parts))), kv);
-            if (parts) hipLaunchKernelGGL((sp_attend_many_join_kernel<D, true>), rows, dim3(kThreads), 0, st, a);
-            else hipLaunchKernelGGL((sp_attend_many_join_kernel<D, false>), rows, dim3(kThreads), 0, st, a);
+            if (parts) hipLaunchKernelGGL((sp_attend_many_join_kernel<D, true>), rows, dim3(kThreads), 0, st, a, p.list);
+            else hipLaunchKernelGGL((sp_attend_many_join_kernel<D, false>), rows, dim3(kThreads), 0, st, a, p.list);
             SP_HIP_CHECK(hipGetLastError());
         }
     }
@@ -1423,11 +1428,6 @@ extern "C" sp_status sp_attend(const sp_cache_desc *desc, const void *q_dev, con
     for (int s = 0; s < 24; ++s)
         if (a.page_blocks == 1 << s) a.page_shift = s;
     a.tiles = p.tiles;
-    a.many_count = p.many_count;
-    for (int i = 0; i < p.many_count; ++i) {
-        a.many_b[i] = p.many_b[i];
-        a.many_tile[i] = p.many_tile[i];
-    }
     uint8_t *ws = static_cast<uint8_t *>(ws_dev);
     a.few_shares = p.few_shares;
     a.few_rows = p.few_rows;
