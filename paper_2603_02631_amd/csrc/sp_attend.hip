@@ -513,14 +513,15 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
     Block<D, E4M3, STREAM> kv;
     int blk = from + wave;
     if (blk < to) {
-        const auto next = [&](int x) { return x + kWaves < to ? x + kWaves : x; };
-        const Place here = Entry(a, line, blk).place(a, line);
-        Entry soon(a, line, next(blk));
+        const int end = blk + (to - 1 - blk) / kWaves * kWaves;         // this wave's last block, loaded again behind it
+        const Entry now(a, line, blk);
+        Entry soon(a, line, min(blk + kWaves, end));
+        const Place here = now.place(a, line);
         kv.load_keys(line, here, k_lane);
         kv.load_values(line, here, v_lane);
         for (;;) {
-            const int ahead = next(blk), key0 = blk * kBlock;
-            const Entry later(a, line, next(ahead));
+            const int key0 = blk * kBlock;
+            const Entry later(a, line, min(blk + 2 * kWaves, end));
             const bool whole = key0 >= all_lo && key0 + kBlock <= all_hi;
             f32x4 s0[MT], s1[MT];
             {
@@ -571,8 +572,8 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
 #pragma unroll
                 for (int i = 0; i < kTiles; ++i) acc.o[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], p, acc.o[t][i], 0, 0, 0);
             }
-            if (ahead == blk) break;
-            blk = ahead;
+            if (blk == end) break;
+            blk += kWaves;
         }
     }
 #pragma unroll
