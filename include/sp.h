@@ -535,7 +535,8 @@ sp_status sp_attend_workspace(const sp_cache_desc *desc, const int64_t *offsets_
  * What a row sees should be finite: logits below 2^120, values below 2^90 in magnitude, scales
  * finite and not negative (a value scale below 2^-64 may count as 2^-64: zero is in order for a block
  * of zeros). A row that sees a NaN becomes NaN, and other rows of its request may.
- * At most 2^26 query tokens and contexts of at most 2^30 tokens.
+ * At most 2^26 query tokens and contexts of at most 2^30 tokens; requests times kv heads, and tiles of 256
+ * query rows times kv heads, below 2^23.
  * max_len bounds the contexts from the host's side (a longer lens[b] counts as
  * max_len, a negative one as 0) and must not exceed table_stride * page_tokens; the call reads the table entries
  * of the tokens below lens[b] only. The probabilities of the second product are rounded to bf16; sums and statistics are held in fp32. The
