@@ -515,7 +515,9 @@ sp_status sp_cache_append(const sp_cache_desc *desc, const void *k_dev, int64_t 
                           float *v_scale_dev, void *hip_stream);
 
 /* Bytes of workspace sp_attend needs for these queries and contexts of at most
- * max_len tokens (0 where it needs none). */
+ * max_len tokens (0 where it needs none). They are enough for every smaller max_len too, so
+ * a program asks once, for its longest context. The queries count as they are given: other
+ * offsets, with fewer rows or requests among them, may need more. */
 sp_status sp_attend_workspace(const sp_cache_desc *desc, const int64_t *offsets_host,
                               int32_t B, int64_t max_len, size_t *bytes);
 

@@ -1310,15 +1310,25 @@ sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64
     p->stream = 2 * max_len * B * kv * D * (sp::cache_is_e4m3(*d) ? 1 : 2) > kStream;
     p->few_least = 4;
     while (8 * p->few_least * p->few_least < blocks) p->few_least *= 2;
-    const int64_t most = sp::ceil_div(blocks * lines, p->few_least);
-    p->few_shares = !p->few || blocks <= whole ? 0 : (int32_t)(spread < most ? spread : most);
+    const auto shares_of = [&](int64_t n, int64_t least) {
+        const int64_t most = sp::ceil_div(n * lines, least);
+        return (int32_t)(!p->few || n <= whole ? 0 : spread < most ? spread : most);
+    };
+    p->few_shares = shares_of(blocks, p->few_least);
+    // Shorter contexts may be shared out over more workgroups, since their stretches are shorter: most of all at the lengths where few_least doubles. The
+    // workspace holds the partial results of any of them.
+    int32_t few_most = p->few_shares;
+    for (int64_t least = 4; least < p->few_least; least *= 2) {
+        const int32_t n = shares_of(8 * least * least, least);
+        few_most = n > few_most ? n : few_most;
+    }
     // Many rows: where compute units would be left over, unless lines are short. Whole and shared, 8 kv heads: 512 rows of head_dim 64 over 512 tokens (five
     // tiles of keys) 17 and 24 us, 128 rows of head_dim 128 over 500 (nine) 23 and 24, over 1500 51 and 25; but a prompt of 8192 (512 lines) 276 and 365.
     const int64_t spans = sp::ceil_div(max_len, 8192 / D) + 1, most_many = spans * tiles * kv;
     p->many_shares = 0;
     if (p->many && p->list.count && spans > 8 && tiles * kv < kUnits) p->many_shares = (int32_t)(kUnits < most_many ? kUnits : most_many);
 
-    const size_t few = (size_t)2 * p->few_shares * p->few_rows, many = (size_t)2 * p->many_shares * kManyRows;
+    const size_t few = (size_t)2 * few_most * p->few_rows, many = (size_t)2 * p->many_shares * kManyRows;
     p->few_o = sp::align_up(few * sizeof(f32x2), 256);
     p->few_before = p->few_o + sp::align_up(few * D * sizeof(float), 256);
     p->many_ml = p->few_before + (few ? sp::align_up((size_t)(B + 1) * sizeof(int64_t), 256) : 0);

@@ -164,3 +164,27 @@ def test_host_code_of_the_operators_under_sanitizers(tmp_path):
     run = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, env=env, timeout=300)
     assert run.returncode == 0, run.stdout[-4000:]
     assert "all checks passed" in run.stdout and "runtime error" not in run.stdout and "AddressSanitizer" not in run.stdout
+
+
+@pytest.mark.parametrize("H,kv,d,offsets", [
+    (32, 8, 64, [0, 1]), (32, 8, 64, [0, 8]), (32, 8, 64, [0, 16]), (16, 8, 128, [0, 1]), (16, 2, 128, [0, 3, 7]), (4, 4, 64, list(range(49))),
+    (32, 8, 64, [0, 1, 513, 514])])
+def test_attend_workspace_covers_shorter_contexts(H, kv, d, offsets):
+    """A program sizes its workspace once, for the longest context, and calls with the lengths that it has reached."""
+    desc = cache(n_q_heads=H, n_kv_heads=kv, head_dim=d, stride_token=d, stride_head=64 * d, page_stride=kv * 64 * d, n_pages=1 << 20)
+    B, most, widest = len(offsets) - 1, 0, 0
+    off = sp.host_offsets(offsets)
+    # every length up to 20000 tokens that changes the number of blocks, then those around where a share's least number of blocks doubles
+    lengths = list(range(1, 20000, 32)) + [32 * (8 << 2 * e) + 32 * s + 1 for e in range(5, 11) for s in (-3, -2, -1, 0, 1, 2)]
+    for n in lengths:
+        size = sp.sp_attend_workspace(desc, off, B, n)
+        assert size >= most, (n, size, most, widest)
+        if size > most:
+            most, widest = size, n
+    assert most > 0
+    # what a call asks for is what the query says for its own length, and no more
+    for n in (4064, 4065, 16346, 16384):
+        size = sp.sp_attend_workspace(desc, off, B, n)
+        kw = dict(offsets_host=offsets, max_len=n, table_stride=1 << 20)
+        if size:
+            refused(3, attend, desc, **kw, ws_bytes=size - 1)
