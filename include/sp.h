@@ -559,7 +559,9 @@ typedef enum { SP_LOGITS_F32 = 0, SP_LOGITS_BF16 = 1 } sp_logits_type;
 /* Largest number of alternatives sp_logprobs reports. */
 #define SP_LOGPROBS_MAX_TOP 32
 
-/* Bytes of workspace sp_logprobs needs (0 where it needs none). */
+/* Bytes of workspace that sp_logprobs needs at most for n_rows rows or fewer, of either type
+ * (0 where it needs none): a program asks once, for its most rows. A call that needs none
+ * itself (many rows, short rows) may go without. */
 sp_status sp_logprobs_workspace(int64_t n_rows, int64_t vocab, int32_t n_top, size_t *bytes);
 
 /*

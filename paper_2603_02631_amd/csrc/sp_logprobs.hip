@@ -425,11 +425,11 @@ constexpr int64_t kOnce = int64_t(1) << 28;
 // Segments of a row: as many as keep the device busy (two workgroups of 512 threads on each of 256 compute units; one row of 131072 of bf16 20 us whole, 12.3 in
 // 32 segments), unless the row is read in less time than the second launch takes: whole and split, 8 rows of 32000 of bf16 8.7 and 10.5 us, 64 of 50021 11.8 and 12.6,
 // but one of 50000 of fp32 13.9 and 10.2.
-constexpr int64_t kWholeBytes = 7168 * 16;
+constexpr int64_t kWholeBytes = 7168 * 16, kTarget = 512;
 
 int splits_of(int64_t n_rows, int64_t vocab, int bytes)
 {
-    const int64_t want = n_rows > 0 && vocab * bytes > kWholeBytes ? 512 / n_rows : 1, most = vocab / kMinSplit;
+    const int64_t want = n_rows > 0 && vocab * bytes > kWholeBytes ? kTarget / n_rows : 1, most = vocab / kMinSplit;
     const int64_t s = want < most ? want : most;
     return (int)(s < 1 ? 1 : (s > kMaxSplits ? kMaxSplits : s));
 }
@@ -440,6 +440,17 @@ size_t workspace_need(int64_t n_rows, int splits, int n_top)
 {
     if (splits <= 1) return 0;
     return keys_at(n_rows, splits) + sp::align_up((size_t)n_rows * splits * n_top * sizeof(uint64_t), 256);
+}
+
+sp_status check_sizes(int64_t n_rows, int64_t vocab, int32_t n_top)
+{
+    if (n_rows < 0 || n_rows >= (int64_t(1) << 31))
+        return sp::fail(SP_ERR_INVALID_ARG, "n_rows = %lld outside 0..2^31-1", (long long)n_rows);
+    if (vocab < 1 || vocab >= (int64_t(1) << 31))
+        return sp::fail(SP_ERR_INVALID_ARG, "vocab = %lld outside 1..2^31-1", (long long)vocab);
+    if (n_top < 0 || n_top > SP_LOGPROBS_MAX_TOP || n_top > vocab)
+        return sp::fail(SP_ERR_INVALID_ARG, "n_top = %d outside 0..min(%d, vocab)", n_top, SP_LOGPROBS_MAX_TOP);
+    return SP_OK;
 }
 
 template <bool BF16>
@@ -475,13 +486,13 @@ sp_status run(const Args &a, int64_t n_rows, hipStream_t st)
 extern "C" sp_status sp_logprobs_workspace(int64_t n_rows, int64_t vocab, int32_t n_top, size_t *bytes)
 {
     if (!bytes) return sp::fail(SP_ERR_INVALID_ARG, "bytes is null");
-    if (n_rows < 0 || n_rows >= (int64_t(1) << 31))
-        return sp::fail(SP_ERR_INVALID_ARG, "n_rows = %lld outside 0..2^31-1", (long long)n_rows);
-    if (vocab < 1 || vocab >= (int64_t(1) << 31))
-        return sp::fail(SP_ERR_INVALID_ARG, "vocab = %lld outside 1..2^31-1", (long long)vocab);
-    if (n_top < 0 || n_top > SP_LOGPROBS_MAX_TOP || n_top > vocab)
-        return sp::fail(SP_ERR_INVALID_ARG, "n_top = %d outside 0..min(%d, vocab)", n_top, SP_LOGPROBS_MAX_TOP);
-    *bytes = workspace_need(n_rows, splits_of(n_rows, vocab, 4), n_top);      // for both types
+    if (sp_status rc = check_sizes(n_rows, vocab, n_top)) return rc;
+    // for both types, and for fewer rows, which may be split more often: no row is split in more than kTarget / 2 of them
+    *bytes = 0;
+    for (int64_t n = 1; n <= n_rows && n <= kTarget / 2; ++n) {
+        const size_t need = workspace_need(n, splits_of(n, vocab, 4), n_top);
+        *bytes = need > *bytes ? need : *bytes;
+    }
     return SP_OK;
 }
 
@@ -490,8 +501,7 @@ extern "C" sp_status sp_logprobs(const void *logits_dev, int32_t dtype, int64_t 
                                  int32_t *top_ids_dev, float *top_logprobs_dev, void *ws_dev, size_t ws_bytes,
                                  void *hip_stream)
 {
-    size_t need;
-    if (sp_status rc = sp_logprobs_workspace(n_rows, vocab, n_top, &need)) return rc;
+    if (sp_status rc = check_sizes(n_rows, vocab, n_top)) return rc;
     if (dtype != SP_LOGITS_F32 && dtype != SP_LOGITS_BF16)
         return sp::fail(SP_ERR_INVALID_ARG, "dtype = %d is neither SP_LOGITS_F32 nor SP_LOGITS_BF16", dtype);
     if (row_stride < vocab || row_stride > (int64_t(1) << 40))
@@ -504,13 +514,15 @@ extern "C" sp_status sp_logprobs(const void *logits_dev, int32_t dtype, int64_t 
         return sp::fail(SP_ERR_INVALID_ARG, "logits_dev is not aligned to its elements");
     if (n_top > 0 && (!top_ids_dev || !top_logprobs_dev))
         return sp::fail(SP_ERR_INVALID_ARG, "top_ids_dev or top_logprobs_dev is null with n_top = %d", n_top);
+    const int splits = splits_of(n_rows, vocab, dtype == SP_LOGITS_F32 ? 4 : 2);
+    const size_t need = workspace_need(n_rows, splits, n_top);
     if (need > 0) {
         if (!ws_dev) return sp::fail(SP_ERR_WORKSPACE, "ws_dev is null (%zu bytes needed)", need);
         if ((uintptr_t)ws_dev % 256 != 0) return sp::fail(SP_ERR_WORKSPACE, "ws_dev is not 256-byte aligned");
         if (ws_bytes < need) return sp::fail(SP_ERR_WORKSPACE, "workspace too small: %zu < %zu", ws_bytes, need);
     }
     Args a{static_cast<const uint8_t *>(logits_dev), vocab, row_stride, targets_dev, logprob_dev, entropy_dev, top_ids_dev,
-           top_logprobs_dev, n_top, splits_of(n_rows, vocab, dtype == SP_LOGITS_F32 ? 4 : 2), static_cast<float *>(ws_dev), nullptr};
+           top_logprobs_dev, n_top, splits, static_cast<float *>(ws_dev), nullptr};
     a.part_keys = reinterpret_cast<uint64_t *>(static_cast<uint8_t *>(ws_dev) + keys_at(n_rows, a.splits));
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     return dtype == SP_LOGITS_BF16 ? run<true>(a, n_rows, st) : run<false>(a, n_rows, st);

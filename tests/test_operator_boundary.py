@@ -188,3 +188,14 @@ def test_attend_workspace_covers_shorter_contexts(H, kv, d, offsets):
         kw = dict(offsets_host=offsets, max_len=n, table_stride=1 << 20)
         if size:
             refused(3, attend, desc, **kw, ws_bytes=size - 1)
+
+
+@pytest.mark.parametrize("vocab", [4096, 32000, 50021, 128000, 262144])
+@pytest.mark.parametrize("n_top", [0, 1, 32])
+def test_logprobs_workspace_covers_fewer_rows(vocab, n_top):
+    """A program sizes its workspace once, for the most rows; a call that needs none itself goes without."""
+    sizes = [sp.sp_logprobs_workspace(n, vocab, n_top) for n in [*range(0, 600), 1000, 4096, (1 << 31) - 1]]
+    assert sizes == sorted(sizes)
+    if sizes[2]:
+        refused(3, logprobs, n_rows=1, vocab=vocab, row_stride=vocab, n_top=n_top, ws_bytes=sizes[1] - 1)
+        refused(3, logprobs, n_rows=2, vocab=vocab, row_stride=vocab, n_top=n_top, ws=None)
