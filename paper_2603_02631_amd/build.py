@@ -20,11 +20,12 @@ FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
 ]
-# device code never produces NaNs on purpose: lets fmaxf chains become v_max3_f32 without
+# device code that is given no NaNs and produces none on purpose: lets fmaxf chains become v_max3_f32 without
 # canonicalising moves (host-side argument checks keep full NaN semantics)
 NO_NANS = ["-Xarch_device", "-fno-honor-nans"]
-# ... but for the one that stores what it is given, NaN included
-HONOUR_NANS = {"sp_cache.hip"}
+# ... but for what may meet them and has to let them through: the cache stores what it is given, and attention makes
+# a row NaN that sees one. With the flag a NaN there would mean nothing to the compiler.
+HONOUR_NANS = {"sp_cache.hip", "sp_attend.hip"}
 
 
 def sources():

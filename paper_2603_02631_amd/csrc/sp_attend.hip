@@ -72,6 +72,9 @@ struct ManyList {
 __device__ __forceinline__ float neg_inf() { return -__builtin_huge_valf(); }
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
+// NaN if one of them is. One operation, as are two that are nested; fmaxf would take one more for each operand that may be a signalling NaN: this
+// file is compiled with NaNs honoured, since a row that sees one has to become NaN.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 __device__ __forceinline__ uint32_t pack2(float a, float b)
 {
     const bf16x2 r = {(__bf16)a, (__bf16)b};
@@ -79,8 +82,8 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
 }
 
 // What a row's result is multiplied by, and its logarithm of the denominator (m in units of log 2). A row that saw no key has a sum of exactly
-// zero; looked at as bits, since the sum of a row that saw a NaN is NaN and must get out.
-__device__ __forceinline__ bool saw_nothing(float l) { return __float_as_uint(l) == 0u; }
+// zero; that of a row that saw a NaN is NaN and gets out.
+__device__ __forceinline__ bool saw_nothing(float l) { return l == 0.f; }
 __device__ __forceinline__ float inverse(float l) { return saw_nothing(l) ? 0.f : 1.f / l; }
 __device__ __forceinline__ float lse_of(float m, float l) { return saw_nothing(l) ? neg_inf() : (m + log2_(l)) * kLn2; }
 
@@ -313,8 +316,8 @@ struct Block {
 // Maximum over the four lanes that hold a query row's logits.
 __device__ __forceinline__ float row_max(float x)
 {
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
+    x = larger(x, __shfl_xor(x, 16));
+    return larger(x, __shfl_xor(x, 32));
 }
 
 __device__ __forceinline__ float row_sum(float x)
@@ -347,9 +350,9 @@ struct Rows {
     // vinv = 2^-vexp.
     __device__ __forceinline__ bf16x8 weigh(int t, const float (&x)[8], float factor, float vexp, float vinv)
     {
-        const float top = factor * fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+        const float top = factor * larger(larger(larger(x[0], x[1]), larger(x[2], x[3])), larger(larger(x[4], x[5]), larger(x[6], x[7])));
         if (__any(top > m[t] + kSlack)) {
-            const float mx = fmaxf(m[t], row_max(top));
+            const float mx = larger(m[t], row_max(top));
             const float f = m[t] == neg_inf() ? 0.f : exp2_(m[t] - mx);
             l[t] *= f;
 #pragma unroll
@@ -543,8 +546,8 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
             const Place there = soon.place(a, line);
             float factor = scale2, vexp = 0.f, vinv = 1.f;
             if (E4M3) {
-                const float vs = fmaxf(kv.vs, kLeastScale);
-                factor = fmaxf(scale2 * kv.ks, kLeastFactor);
+                const float vs = larger(kv.vs, kLeastScale);
+                factor = larger(scale2 * kv.ks, kLeastFactor);
                 vexp = log2_(vs);
                 vinv = __builtin_amdgcn_rcpf(vs);
             }
@@ -596,7 +599,7 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
                 const f32x2 o = merge_ml[wave][16 * t + c];
-                const float mx = fmaxf(acc.m[t], o[0]);
+                const float mx = larger(acc.m[t], o[0]);
                 const float f = acc.m[t] == neg_inf() ? 0.f : exp2_(acc.m[t] - mx), f2 = o[0] == neg_inf() ? 0.f : exp2_(o[0] - mx);
                 acc.m[t] = mx;
                 acc.l[t] = acc.l[t] * f + o[1] * f2;
@@ -705,9 +708,9 @@ __device__ __forceinline__ void join_row(const AttendArgs &a, const f32x2 *ml, c
     f32x2 mine = ml[at(min(lane, count - 1))];
     load(part_wave);
     if (lane < count) m = mine[0];
-    for (int s = lane + 64; s < count; s += 64) m = fmaxf(m, ml[at(s)][0]);
+    for (int s = lane + 64; s < count; s += 64) m = larger(m, ml[at(s)][0]);
 #pragma unroll
-    for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    for (int o = 32; o; o >>= 1) m = larger(m, __shfl_xor(m, o));
     for (int s0 = 0; s0 < count; s0 += 64) {
         if (s0 > 0) mine = ml[at(min(s0 + lane, count - 1))];
         const float w = s0 + lane >= count || mine[0] == neg_inf() ? 0.f : exp2_(mine[0] - m);
@@ -1113,18 +1116,18 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
                         vinv[w] = 1.f;
                         // blocks that no row of the tile sees may have any scale: they are masked, and take none
                         if (E4M3 && (whole || (key0 + 32 * (u + w) < t.hi && key0 + 32 * (u + w) + 32 > t.lo))) {
-                            const float vs = fmaxf(scales[buf][kBlocks + u + w], kLeastScale);
-                            sc[w] = fmaxf(sc[w] * scales[buf][u + w], kLeastFactor);
+                            const float vs = larger(scales[buf][kBlocks + u + w], kLeastScale);
+                            sc[w] = larger(sc[w] * scales[buf][u + w], kLeastFactor);
                             vexp[w] = log2_(vs);
                             vinv[w] = __builtin_amdgcn_rcpf(vs);
                         }
                         float y = x[w][0];
 #pragma unroll
-                        for (int e = 1; e < 16; ++e) y = fmaxf(y, x[w][e]);
-                        top = fmaxf(top, y * sc[w]);
+                        for (int e = 1; e < 16; ++e) y = larger(y, x[w][e]);
+                        top = larger(top, y * sc[w]);
                     }
                     if (__any(top > m + kSlack)) {
-                        const float mx = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
+                        const float mx = larger(m, larger(top, __shfl_xor(top, 32)));
                         const float f = m == neg_inf() ? 0.f : exp2_(m - mx);
                         l *= f;
 #pragma unroll

@@ -306,3 +306,26 @@ def test_contexts_that_may_be_larger_than_a_cache(news):
     """A bound of 2^20 tokens a request: keys are read past the caches, work is shared out as for the longest lengths."""
     check(4, 4, 64, news, [700, 65], 512, True, max_len=1 << 20)
     check(2, 2, 128, news, [700, 65], 512, False, max_len=1 << 20)
+
+
+@pytest.mark.parametrize("e4m3", [True, False])
+@pytest.mark.parametrize("H,kv,d", [(8, 2, 128), (4, 2, 128), (8, 2, 64)])
+@pytest.mark.parametrize("news,lens", [([1, 3], [300, 200]), ([8, 4], [300, 200]), ([90, 70], [300, 200]), ([2, 1], [3000, 2500]),
+                                       ([8, 4], [3000, 2500]), ([90, 70], [3000, 2500])])
+def test_a_nan_that_is_seen_gets_out_of_every_kernel(e4m3, H, kv, d, news, lens):
+    """As above at both head sizes, with one to four query heads a kv head: few and many rows, whole and shared out, at the beginning of
+    a context, in its middle, and at its last key, which only the last row sees."""
+    G, n, L = H // kv, news[0], lens[0]
+    for which in ("k", "v"):
+        for key in (0, 57, L // 2, L - 1):
+            c, held, off, q = build(H, kv, d, news, lens, 64, e4m3, "HND", 0, 13)
+            getattr(c, which)[c.at(0, 1, key) + 5] = 0x7F if e4m3 else 0x7FC0
+            out, lse = call(c, H, off, q, lens, max(lens), 0.125, 1, 0)
+            rows = slice(n - 1, n) if key == L - 1 else slice(0, n)         # that see it
+            if which == "k":
+                assert np.isnan(out[rows, G:]).all() and np.isnan(lse[rows, G:]).all(), key
+            else:
+                assert np.isnan(out[rows, G:, 5]).all() and np.isfinite(lse[rows, G:]).all(), key
+                assert np.isfinite(np.delete(out[rows, G:], 5, axis=2)).all(), key
+            assert np.isfinite(out[:n, :G]).all() and np.isfinite(lse[:n, :G]).all(), key
+            assert np.isfinite(out[n:]).all() and np.isfinite(lse[n:]).all(), key

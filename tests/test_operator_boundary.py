@@ -199,3 +199,11 @@ def test_logprobs_workspace_covers_fewer_rows(vocab, n_top):
     if sizes[2]:
         refused(3, logprobs, n_rows=1, vocab=vocab, row_stride=vocab, n_top=n_top, ws_bytes=sizes[1] - 1)
         refused(3, logprobs, n_rows=2, vocab=vocab, row_stride=vocab, n_top=n_top, ws=None)
+
+
+@pytest.mark.parametrize("name", ["sp_cache.hip", "sp_attend.hip"])
+def test_files_that_may_meet_nans_are_compiled_to_honour_them(name):
+    from paper_2603_02631_amd import build
+    src = os.path.join(build.CSRC, name)
+    assert src in build.sources()
+    assert not [f for f in build.compile_command(src, "x.o") if "no-honor-nans" in f or "fast-math" in f or "finite-math" in f]
