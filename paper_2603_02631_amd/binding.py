@@ -459,6 +459,32 @@ def _offsets(values):
     return values if isinstance(values, ctypes.Array) and values._type_ is ctypes.c_int64 else _host_i64(values)
 
 
+# Types that an argument may have: its own, the other integers of its width, or plain bytes. Filled at the first tensor (torch is not imported before).
+_INT32, _INT64 = set(), set()
+
+
+def _learn_types() -> None:
+    import torch
+    for known, names in ((_INT32, ("int32", "uint32", "uint8")), (_INT64, ("int64", "uint64", "uint8"))):
+        known.update(getattr(torch, name) for name in names if hasattr(torch, name))
+
+
+def _typed(t, what: str, nbytes: int, known: set) -> Optional[int]:
+    """As _ptr, for arguments whose elements could be misread: a tensor's type has to be one of `known`."""
+    try:
+        if t.dtype in known and t.is_cuda and t.is_contiguous() and t.nbytes >= nbytes:
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    p = _ptr(t, what, nbytes)
+    if hasattr(t, "dtype"):
+        if not known:
+            _learn_types()
+        if t.dtype not in known:
+            raise SpError(1, f"{what} is of {t.dtype}, the call needs {' or '.join(sorted(str(x) for x in known))}")
+    return p
+
+
 def _rows(t, what: str, rows: int, width: int, stride: Optional[int], elem: int):
     """(address, row stride in elements) of `rows` rows of `width` contiguous elements: a tensor whose first dimension
     counts rows and whose others are dense, or an address with its stride."""
@@ -500,7 +526,7 @@ def _table(block_table, B: int, table_stride: Optional[int]):
         if block_table.dim() != 2:
             raise SpError(1, "block_table has to be [requests][entries]")
         table_stride = block_table.shape[1]
-    return _ptr(block_table, "block_table", 4 * B * table_stride), table_stride
+    return _typed(block_table, "block_table", 4 * B * table_stride, _INT32), table_stride
 
 
 def _cache_bytes(desc: CacheDesc):
@@ -529,8 +555,8 @@ def sp_cache_append(desc: CacheDesc, k, v, offsets_host, offsets_dev, start, blo
     trig = 2 * n_pos * rot_dim
     _check(load_library().sp_cache_append(
         ctypes.byref(desc), kp, ks, vp, vs, qp, qs, _ptr(q_out, "q_out", 2 * T * qw), off,
-        _ptr(offsets_dev, "offsets_dev", 8 * (B + 1)), B, _ptr(start, "start", 4 * B),
-        _ptr(positions, "positions", 4 * T), tab, width, _ptr(cos, "cos", trig), _ptr(sin, "sin", trig), n_pos, rot_dim, rot_style,
+        _typed(offsets_dev, "offsets_dev", 8 * (B + 1), _INT64), B, _typed(start, "start", 4 * B, _INT32),
+        _typed(positions, "positions", 4 * T, _INT32), tab, width, _ptr(cos, "cos", trig), _ptr(sin, "sin", trig), n_pos, rot_dim, rot_style,
         _ptr(k_pool, "k_pool", pool), _ptr(v_pool, "v_pool", pool), _ptr(k_scale, "k_scale", scales),
         _ptr(v_scale, "v_scale", scales), _stream(stream)))
 
@@ -556,8 +582,8 @@ def sp_attend(desc: CacheDesc, q, offsets_host, offsets_dev, lens, max_len: int,
     H, _, d, pool, scales = _cache_bytes(desc)
     rows = T * H
     _check(load_library().sp_attend(
-        ctypes.byref(desc), _ptr(q, "q", 2 * rows * d), off, _ptr(offsets_dev, "offsets_dev", 8 * (B + 1)), B,
-        _ptr(lens, "lens", 4 * B), max_len, tab, width, _ptr(k_pool, "k_pool", pool), _ptr(v_pool, "v_pool", pool),
+        ctypes.byref(desc), _ptr(q, "q", 2 * rows * d), off, _typed(offsets_dev, "offsets_dev", 8 * (B + 1), _INT64), B,
+        _typed(lens, "lens", 4 * B, _INT32), max_len, tab, width, _ptr(k_pool, "k_pool", pool), _ptr(v_pool, "v_pool", pool),
         _ptr(k_scale, "k_scale", scales), _ptr(v_scale, "v_scale", scales), scale, causal, window,
         _ptr(out, "out", 2 * rows * d), _ptr(lse, "lse", 4 * rows), _ptr(ws, "ws"), _ws_bytes(ws, ws_bytes),
         _stream(stream)))
@@ -581,6 +607,6 @@ def sp_logprobs(logits, n_rows: int, vocab: int, targets, n_top: int, logprob, e
     x, stride = _rows(logits, "logits", n_rows, vocab, row_stride, 4 if dtype == SP_LOGITS_F32 else 2)
     n, k = max(n_rows, 0), max(n_top, 0)
     _check(load_library().sp_logprobs(
-        x, dtype, n_rows, vocab, stride or row_stride or vocab, _ptr(targets, "targets", 4 * n), n_top,
-        _ptr(logprob, "logprob", 4 * n), _ptr(entropy, "entropy", 4 * n), _ptr(top_ids, "top_ids", 4 * n * k),
+        x, dtype, n_rows, vocab, stride or row_stride or vocab, _typed(targets, "targets", 4 * n, _INT32), n_top,
+        _ptr(logprob, "logprob", 4 * n), _ptr(entropy, "entropy", 4 * n), _typed(top_ids, "top_ids", 4 * n * k, _INT32),
         _ptr(top_logprobs, "top_logprobs", 4 * n * k), _ptr(ws, "ws"), _ws_bytes(ws, ws_bytes), _stream(stream)))

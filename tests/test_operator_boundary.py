@@ -207,3 +207,37 @@ def test_files_that_may_meet_nans_are_compiled_to_honour_them(name):
     src = os.path.join(build.CSRC, name)
     assert src in build.sources()
     assert not [f for f in build.compile_command(src, "x.o") if "no-honor-nans" in f or "fast-math" in f or "finite-math" in f]
+
+
+class OnGpu:
+    """A tensor of the CPU that says it is on the GPU: the binding looks at it, the library refuses the call before anything is read."""
+
+    def __init__(self, t):
+        self.t, self.is_cuda = t, True
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    def data_ptr(self):
+        return FAKE
+
+
+INDEX_ARGUMENTS = [(append, "start", 2, 32), (append, "positions", 3, 32), (append, "block_table", 8, 32), (append, "offsets_dev", 3, 64),
+                   (attend, "lens", 2, 32), (attend, "block_table", 8, 32), (attend, "offsets_dev", 3, 64),
+                   (logprobs, "targets", 2, 32), (logprobs, "top_ids", 6, 32)]
+
+
+@pytest.mark.parametrize("fn,name,n,bits", INDEX_ARGUMENTS)
+def test_indices_of_another_width_are_refused(fn, name, n, bits):
+    """64-bit integers are torch's own choice: read as 32-bit ones they would be every other one a zero."""
+    import torch
+    stop = {append: dict(rot_dim=8), attend: dict(causal=2), logprobs: dict(row_stride=1)}[fn]     # refused by the library in any case
+    own, other = (torch.int32, torch.int64) if bits == 32 else (torch.int64, torch.int32)
+    for dtype in (own, torch.uint32 if bits == 32 else torch.uint64):
+        with pytest.raises(sp.SpError) as e:
+            fn(**{name: OnGpu(torch.zeros(2 * n, dtype=dtype)), **stop})
+        assert name not in e.value.message, e.value
+    for dtype in (other, torch.float32, torch.float64, torch.int16):
+        with pytest.raises(sp.SpError) as e:
+            fn(**{name: OnGpu(torch.zeros(4 * n, dtype=dtype)), **stop})
+        assert e.value.status == 1 and name in e.value.message, e.value
