@@ -459,18 +459,26 @@ def _offsets(values):
     return values if isinstance(values, ctypes.Array) and values._type_ is ctypes.c_int64 else _host_i64(values)
 
 
-# Types that an argument may have: its own, the other integers of its width, or plain bytes. Filled at the first tensor (torch is not imported before).
-_INT32, _INT64 = set(), set()
+# Types that an argument may have: its own, and the integers of its width (its bits). Filled at the first tensor (torch is not imported before).
+_INT32, _INT64, _FP32, _BF16, _E4M3 = set(), set(), set(), set(), set()
 
 
 def _learn_types() -> None:
     import torch
-    for known, names in ((_INT32, ("int32", "uint32", "uint8")), (_INT64, ("int64", "uint64", "uint8"))):
+    for known, names in ((_INT32, ("int32", "uint32")), (_INT64, ("int64", "uint64")), (_FP32, ("float32", "int32", "uint32")),
+                         (_BF16, ("bfloat16", "int16", "uint16")), (_E4M3, ("float8_e4m3fn", "uint8", "int8"))):
         known.update(getattr(torch, name) for name in names if hasattr(torch, name))
 
 
+def _check_type(t, what: str, known: set, plain_bytes: bool) -> None:
+    if not known:
+        _learn_types()
+    if t.dtype not in known and not (plain_bytes and str(t.dtype) == "torch.uint8"):
+        raise SpError(1, f"{what} is of {t.dtype}, the call needs {' or '.join(sorted(str(x) for x in known))}")
+
+
 def _typed(t, what: str, nbytes: int, known: set) -> Optional[int]:
-    """As _ptr, for arguments whose elements could be misread: a tensor's type has to be one of `known`."""
+    """As _ptr, for arguments whose elements could be misread: a tensor's type has to be one of `known`, or bytes."""
     try:
         if t.dtype in known and t.is_cuda and t.is_contiguous() and t.nbytes >= nbytes:
             return t.data_ptr()
@@ -478,20 +486,17 @@ def _typed(t, what: str, nbytes: int, known: set) -> Optional[int]:
         pass
     p = _ptr(t, what, nbytes)
     if hasattr(t, "dtype"):
-        if not known:
-            _learn_types()
-        if t.dtype not in known:
-            raise SpError(1, f"{what} is of {t.dtype}, the call needs {' or '.join(sorted(str(x) for x in known))}")
+        _check_type(t, what, known, True)
     return p
 
 
-def _rows(t, what: str, rows: int, width: int, stride: Optional[int], elem: int):
-    """(address, row stride in elements) of `rows` rows of `width` contiguous elements: a tensor whose first dimension
-    counts rows and whose others are dense, or an address with its stride."""
+def _rows(t, what: str, rows: int, width: int, stride: Optional[int], known: set):
+    """(address, row stride in elements) of `rows` rows of `width` contiguous elements: a tensor of a type in `known` whose
+    first dimension counts rows and whose others are dense, or an address with its stride."""
     # two dimensions, the second dense: what a projection's output and its parts are. Few attribute reads, as in _ptr
     try:
         st = t.stride()
-        if t.is_cuda and len(st) == 2 and st[1] == 1 and stride is None and t.element_size() == elem:
+        if t.is_cuda and len(st) == 2 and st[1] == 1 and stride is None and t.dtype in known:
             n, w = t.shape
             if n >= rows and w >= width:
                 return t.data_ptr(), st[0] if rows > 1 else (width + 7) & ~7      # the stride of a single row means nothing
@@ -503,9 +508,10 @@ def _rows(t, what: str, rows: int, width: int, stride: Optional[int], elem: int)
         return t, width if stride is None else stride
     if not getattr(t, "is_cuda", False):
         raise SpError(1, f"{what} is not a device tensor")
+    _check_type(t, what, known, False)
     shape, strides = t.shape, t.stride()
-    if not shape or shape[0] < rows or t.element_size() != elem:
-        raise SpError(1, f"{what} is {tuple(shape)} of {t.element_size()} bytes an element, the call needs {rows} rows of {elem}")
+    if not shape or shape[0] < rows:
+        raise SpError(1, f"{what} is {tuple(shape)}, the call needs {rows} rows")
     dense = 1
     for n, s in zip(reversed(shape[1:]), reversed(strides[1:])):
         if n != 1 and s != dense:
@@ -530,10 +536,13 @@ def _table(block_table, B: int, table_stride: Optional[int]):
 
 
 def _cache_bytes(desc: CacheDesc):
-    """Query heads, kv heads, head_dim, and the bytes that a pool and its scales have to hold."""
+    """Query heads, kv heads, head_dim, a pool's element types, and the bytes that a pool and its scales have to hold."""
     kv, d, pages, page = desc.n_kv_heads, desc.head_dim, desc.n_pages, desc.page_tokens
     pool = (pages - 1) * desc.page_stride + (kv - 1) * desc.stride_head + (page - 1) * desc.stride_token + d
-    return desc.n_q_heads, kv, d, pool if desc.cache_type == SP_CACHE_E4M3 else 2 * pool, 4 * pages * kv * (page // SP_CACHE_BLOCK)
+    scales = 4 * pages * kv * (page // SP_CACHE_BLOCK)
+    if desc.cache_type == SP_CACHE_E4M3:
+        return desc.n_q_heads, kv, d, _E4M3, pool, scales
+    return desc.n_q_heads, kv, d, _BF16, 2 * pool, scales
 
 
 def sp_cache_append(desc: CacheDesc, k, v, offsets_host, offsets_dev, start, block_table, k_pool, v_pool, k_scale=None,
@@ -544,21 +553,21 @@ def sp_cache_append(desc: CacheDesc, k, v, offsets_host, offsets_dev, start, blo
     off = _offsets(offsets_host)
     B = len(off) - 1
     T = max(off[B], 0) if B >= 0 else 0
-    H, kv, d, pool, scales = _cache_bytes(desc)
+    H, kv, d, elems, pool, scales = _cache_bytes(desc)
     kw, qw = kv * d, H * d
-    kp, ks = _rows(k, "k", T, kw, k_stride, 2)
-    vp, vs = _rows(v, "v", T, kw, v_stride, 2)
-    qp, qs = _rows(q, "q", T, qw, q_stride, 2)
+    kp, ks = _rows(k, "k", T, kw, k_stride, _BF16)
+    vp, vs = _rows(v, "v", T, kw, v_stride, _BF16)
+    qp, qs = _rows(q, "q", T, qw, q_stride, _BF16)
     tab, width = _table(block_table, B, table_stride)
     if n_pos is None:
         n_pos = 0 if cos is None or isinstance(cos, int) else cos.shape[0]
     trig = 2 * n_pos * rot_dim
     _check(load_library().sp_cache_append(
-        ctypes.byref(desc), kp, ks, vp, vs, qp, qs, _ptr(q_out, "q_out", 2 * T * qw), off,
+        ctypes.byref(desc), kp, ks, vp, vs, qp, qs, _typed(q_out, "q_out", 2 * T * qw, _BF16), off,
         _typed(offsets_dev, "offsets_dev", 8 * (B + 1), _INT64), B, _typed(start, "start", 4 * B, _INT32),
-        _typed(positions, "positions", 4 * T, _INT32), tab, width, _ptr(cos, "cos", trig), _ptr(sin, "sin", trig), n_pos, rot_dim, rot_style,
-        _ptr(k_pool, "k_pool", pool), _ptr(v_pool, "v_pool", pool), _ptr(k_scale, "k_scale", scales),
-        _ptr(v_scale, "v_scale", scales), _stream(stream)))
+        _typed(positions, "positions", 4 * T, _INT32), tab, width, _typed(cos, "cos", trig, _FP32), _typed(sin, "sin", trig, _FP32), n_pos, rot_dim, rot_style,
+        _typed(k_pool, "k_pool", pool, elems), _typed(v_pool, "v_pool", pool, elems), _typed(k_scale, "k_scale", scales, _FP32),
+        _typed(v_scale, "v_scale", scales, _FP32), _stream(stream)))
 
 
 def sp_attend_workspace(desc: CacheDesc, offsets_host, B: Optional[int] = None, max_len: int = 0) -> int:
@@ -579,13 +588,13 @@ def sp_attend(desc: CacheDesc, q, offsets_host, offsets_dev, lens, max_len: int,
     B = len(off) - 1
     T = max(off[B], 0) if B >= 0 else 0
     tab, width = _table(block_table, B, table_stride)
-    H, _, d, pool, scales = _cache_bytes(desc)
+    H, _, d, elems, pool, scales = _cache_bytes(desc)
     rows = T * H
     _check(load_library().sp_attend(
-        ctypes.byref(desc), _ptr(q, "q", 2 * rows * d), off, _typed(offsets_dev, "offsets_dev", 8 * (B + 1), _INT64), B,
-        _typed(lens, "lens", 4 * B, _INT32), max_len, tab, width, _ptr(k_pool, "k_pool", pool), _ptr(v_pool, "v_pool", pool),
-        _ptr(k_scale, "k_scale", scales), _ptr(v_scale, "v_scale", scales), scale, causal, window,
-        _ptr(out, "out", 2 * rows * d), _ptr(lse, "lse", 4 * rows), _ptr(ws, "ws"), _ws_bytes(ws, ws_bytes),
+        ctypes.byref(desc), _typed(q, "q", 2 * rows * d, _BF16), off, _typed(offsets_dev, "offsets_dev", 8 * (B + 1), _INT64), B,
+        _typed(lens, "lens", 4 * B, _INT32), max_len, tab, width, _typed(k_pool, "k_pool", pool, elems), _typed(v_pool, "v_pool", pool, elems),
+        _typed(k_scale, "k_scale", scales, _FP32), _typed(v_scale, "v_scale", scales, _FP32), scale, causal, window,
+        _typed(out, "out", 2 * rows * d, _BF16), _typed(lse, "lse", 4 * rows, _FP32), _ptr(ws, "ws"), _ws_bytes(ws, ws_bytes),
         _stream(stream)))
 
 
@@ -598,15 +607,19 @@ def sp_logprobs_workspace(n_rows: int, vocab: int, n_top: int) -> int:
 def sp_logprobs(logits, n_rows: int, vocab: int, targets, n_top: int, logprob, entropy, top_ids, top_logprobs, ws,
                 dtype: Optional[int] = None, row_stride: Optional[int] = None, ws_bytes: Optional[int] = None,
                 stream=None) -> None:
-    if dtype is None:       # from the tensor: four bytes an element are fp32, two are bf16 (or its bits)
-        if not hasattr(logits, "element_size"):
+    if dtype is None:       # from the tensor
+        if not hasattr(logits, "dtype"):
             raise SpError(1, "logits given as an address need a dtype")
-        if logits.element_size() not in (2, 4):
-            raise SpError(1, "logits have to be fp32 or bf16")
-        dtype = SP_LOGITS_F32 if logits.element_size() == 4 else SP_LOGITS_BF16
-    x, stride = _rows(logits, "logits", n_rows, vocab, row_stride, 4 if dtype == SP_LOGITS_F32 else 2)
+        if not _BF16:
+            _learn_types()
+        if logits.dtype in _BF16:
+            dtype = SP_LOGITS_BF16
+        else:
+            _check_type(logits, "logits", _FP32, False)
+            dtype = SP_LOGITS_F32
+    x, stride = _rows(logits, "logits", n_rows, vocab, row_stride, _FP32 if dtype == SP_LOGITS_F32 else _BF16)
     n, k = max(n_rows, 0), max(n_top, 0)
     _check(load_library().sp_logprobs(
         x, dtype, n_rows, vocab, stride or row_stride or vocab, _typed(targets, "targets", 4 * n, _INT32), n_top,
-        _ptr(logprob, "logprob", 4 * n), _ptr(entropy, "entropy", 4 * n), _typed(top_ids, "top_ids", 4 * n * k, _INT32),
-        _ptr(top_logprobs, "top_logprobs", 4 * n * k), _ptr(ws, "ws"), _ws_bytes(ws, ws_bytes), _stream(stream)))
+        _typed(logprob, "logprob", 4 * n, _FP32), _typed(entropy, "entropy", 4 * n, _FP32), _typed(top_ids, "top_ids", 4 * n * k, _INT32),
+        _typed(top_logprobs, "top_logprobs", 4 * n * k, _FP32), _ptr(ws, "ws"), _ws_bytes(ws, ws_bytes), _stream(stream)))

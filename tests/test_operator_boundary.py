@@ -241,3 +241,54 @@ def test_indices_of_another_width_are_refused(fn, name, n, bits):
         with pytest.raises(sp.SpError) as e:
             fn(**{name: OnGpu(torch.zeros(4 * n, dtype=dtype)), **stop})
         assert e.value.status == 1 and name in e.value.message, e.value
+
+
+@pytest.mark.parametrize("fn,name,shape,own", [
+    (append, "k", (3, 128), "bfloat16"), (append, "v", (3, 128), "bfloat16"), (append, "q", (3, 512), "bfloat16"), (append, "q_out", (3, 512), "bfloat16"),
+    (append, "k", (3, 2, 64), "bfloat16"), (append, "q", (3, 8, 64), "bfloat16"),
+    (append, "cos", (100, 32), "float32"), (append, "sin", (100, 32), "float32"), (append, "k_scale", (4, 2, 2), "float32"), (append, "v_scale", (4, 2, 2), "float32"),
+    (append, "k_pool", (4, 2, 64, 64), "float8_e4m3fn"), (append, "v_pool", (4, 2, 64, 64), "float8_e4m3fn"),
+    (attend, "q", (4, 8, 64), "bfloat16"), (attend, "out", (4, 8, 64), "bfloat16"), (attend, "lse", (4, 8), "float32"), (attend, "k_scale", (4, 2, 2), "float32"),
+    (attend, "v_scale", (4, 2, 2), "float32"), (attend, "k_pool", (4, 2, 64, 64), "float8_e4m3fn"), (attend, "v_pool", (4, 2, 64, 64), "float8_e4m3fn"),
+    (logprobs, "logprob", (2,), "float32"), (logprobs, "entropy", (2,), "float32"), (logprobs, "top_logprobs", (2, 3), "float32")])
+def test_numbers_of_another_type_are_refused(fn, name, shape, own):
+    """float16 has bf16's width and float64 more than enough bytes: both would be misread without a word. Integers of an element's width are its bits."""
+    import torch
+    stop = {append: dict(rot_dim=8, offsets_host=[0, 2, 3]), attend: dict(causal=2), logprobs: dict(row_stride=1)}[fn]
+    bits = {"bfloat16": ("int16",), "float32": ("int32",), "float8_e4m3fn": ("uint8", "int8")}[own]
+    for dtype in (own, *bits):
+        with pytest.raises(sp.SpError) as e:
+            fn(**{name: OnGpu(torch.zeros(shape, dtype=getattr(torch, dtype))), **stop})
+        assert not e.value.message.startswith(name + " "), e.value
+    others = {"bfloat16": ("float16", "float32", "float64"), "float32": ("float64",), "float8_e4m3fn": ("float8_e5m2", "float16", "float32")}[own]
+    for dtype in others:
+        with pytest.raises(sp.SpError) as e:
+            fn(**{name: OnGpu(torch.zeros(shape, dtype=getattr(torch, dtype))), **stop})
+        assert e.value.status == 1 and e.value.message.startswith(name + " "), e.value
+
+
+def test_pools_of_a_bf16_cache_are_of_its_type():
+    import torch
+    d = cache(cache_type=sp.SP_CACHE_BF16)
+    for dtype in (torch.bfloat16, torch.int16, torch.uint16):
+        refused_by_library = dict(k_pool=OnGpu(torch.zeros(4, 2, 64, 64, dtype=dtype)))
+        with pytest.raises(sp.SpError) as e:
+            attend(d, causal=2, **refused_by_library)
+        assert "causal" in e.value.message
+    for dtype in (torch.float16, torch.float32):
+        with pytest.raises(sp.SpError) as e:
+            attend(d, causal=2, k_pool=OnGpu(torch.zeros(4, 2, 64, 64, dtype=dtype)))
+        assert e.value.message.startswith("k_pool ")
+
+
+@pytest.mark.parametrize("given", [None, sp.SP_LOGITS_BF16, sp.SP_LOGITS_F32])
+def test_logits_of_another_type_are_refused(given):
+    """A projection's output in float16 gave likely-looking tokens and probabilities of its bits read as bf16."""
+    import torch
+    for dtype, own in ((torch.bfloat16, sp.SP_LOGITS_BF16), (torch.int16, sp.SP_LOGITS_BF16), (torch.float32, sp.SP_LOGITS_F32),
+                       (torch.int32, sp.SP_LOGITS_F32), (torch.float16, -1), (torch.float64, -1), (torch.int64, -1)):
+        for shape in ((2, 100), (2, 1, 100)):
+            with pytest.raises(sp.SpError) as e:
+                logprobs(logits=OnGpu(torch.zeros(shape, dtype=dtype)), dtype=given, row_stride=None, n_top=33)
+            fits = own >= 0 and given in (None, own)
+            assert ("n_top" in e.value.message) == fits and e.value.message.startswith("logits ") == (not fits), (dtype, e.value)
