@@ -542,7 +542,8 @@ sp_status sp_attend_workspace(const sp_cache_desc *desc, const int64_t *offsets_
  * max_len bounds the contexts from the host's side (a longer lens[b] counts as
  * max_len, a negative one as 0) and must not exceed table_stride * page_tokens; the call reads the table entries
  * of the tokens below lens[b] only. The probabilities of the second product are rounded to bf16; sums and statistics are held in fp32. The
- * result does not change from call to call on the same inputs. scale: finite and > 0.
+ * result does not change from call to call on the same inputs. 0 < scale <= 2.3e38. Scale times a key scale
+ * counts as about 2^-127 where it is less and as about 2^127 where it is more.
  */
 sp_status sp_attend(const sp_cache_desc *desc, const void *q_dev,
                     const int64_t *offsets_host, const int64_t *offsets_dev, int32_t B,

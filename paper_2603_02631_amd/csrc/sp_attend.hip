@@ -35,8 +35,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // A block's key scale goes into its logits' factor, its value scale into the exponent (and out of the sum again): no operation for an element.
-// The factor stays above zero, so that masked logits stay minus infinity; the value scale above 2^-64, so that exponents keep their range.
-constexpr float kLeastScale = 5.42101086e-20f, kLeastFactor = 1.17549435e-38f;
+// The factor stays above zero, so that masked logits stay minus infinity, and finite, so that a product of zero stays a logit of zero; the value scale
+// above 2^-64, so that exponents keep their range.
+constexpr float kLeastScale = 5.42101086e-20f, kLeastFactor = 1.17549435e-38f, kMostFactor = 3.40282347e38f;
+constexpr float kMostScale = 2.3e38f;      // of a call: times log2(e) it is finite
 
 struct AttendArgs {
     sp::CacheView c;
@@ -75,6 +77,10 @@ __device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x
 // NaN if one of them is. One operation, as are two that are nested; fmaxf would take one more for each operand that may be a signalling NaN: this
 // file is compiled with NaNs honoured, since a row that sees one has to become NaN.
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float factor_of(float scale, float key_scale)
+{
+    return __builtin_elementwise_minimum(larger(scale * key_scale, kLeastFactor), kMostFactor);
+}
 __device__ __forceinline__ uint32_t pack2(float a, float b)
 {
     const bf16x2 r = {(__bf16)a, (__bf16)b};
@@ -547,7 +553,7 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
             float factor = scale2, vexp = 0.f, vinv = 1.f;
             if (E4M3) {
                 const float vs = larger(kv.vs, kLeastScale);
-                factor = larger(scale2 * kv.ks, kLeastFactor);
+                factor = factor_of(scale2, kv.ks);
                 vexp = log2_(vs);
                 vinv = __builtin_amdgcn_rcpf(vs);
             }
@@ -1117,7 +1123,7 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
                         // blocks that no row of the tile sees may have any scale: they are masked, and take none
                         if (E4M3 && (whole || (key0 + 32 * (u + w) < t.hi && key0 + 32 * (u + w) + 32 > t.lo))) {
                             const float vs = larger(scales[buf][kBlocks + u + w], kLeastScale);
-                            sc[w] = larger(sc[w] * scales[buf][u + w], kLeastFactor);
+                            sc[w] = factor_of(scale2, scales[buf][u + w]);
                             vexp[w] = log2_(vs);
                             vinv[w] = __builtin_amdgcn_rcpf(vs);
                         }
@@ -1412,7 +1418,7 @@ extern "C" sp_status sp_attend(const sp_cache_desc *desc, const void *q_dev, con
 {
     Plan p;
     if (sp_status rc = make_plan(desc, offsets_host, B, max_len, &p)) return rc;
-    if (!(scale > 0.f) || scale > 3.0e38f) return sp::fail(SP_ERR_INVALID_ARG, "scale must be finite and > 0");
+    if (!(scale > 0.f) || scale > kMostScale) return sp::fail(SP_ERR_INVALID_ARG, "scale = %g must be > 0 and at most 2.3e38", (double)scale);
     if (causal != 0 && causal != 1) return sp::fail(SP_ERR_INVALID_ARG, "causal = %d is neither 0 nor 1", causal);
     if (window < 0 || (window > 0 && !causal))
         return sp::fail(SP_ERR_INVALID_ARG, "window = %lld must be 0, or positive with causal = 1", (long long)window);

@@ -329,3 +329,19 @@ def test_a_nan_that_is_seen_gets_out_of_every_kernel(e4m3, H, kv, d, news, lens)
                 assert np.isfinite(np.delete(out[rows, G:], 5, axis=2)).all(), key
             assert np.isfinite(out[:n, :G]).all() and np.isfinite(lse[:n, :G]).all(), key
             assert np.isfinite(out[n:]).all() and np.isfinite(lse[n:]).all(), key
+
+
+@pytest.mark.parametrize("news", [[1, 3], [90, 70]])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("e4m3", [True, False])
+def test_queries_of_zero_at_the_largest_scales(news, d, e4m3):
+    """Logits of exactly zero however large scale and key scales are: the values' mean, and the logarithm of the number of keys."""
+    lens = [300, 200]
+    c, held, off, q = build(4, 2, d, news, lens, 32, e4m3, "HND", 0, 14)
+    if e4m3:
+        c.ks = np.where(np.isnan(c.ks), c.ks, np.float32(2.0 ** 100))
+        for b in range(2):
+            held[b] = [np.zeros_like(held[b][0]), held[b][1]]       # whatever the keys are
+    q[:] = 0
+    out, lse = call(c, 4, off, q, lens, 300, 2.3e38, 1, 0)
+    verify(c, 4, held, off, q, lens, 1.0, 1, 0, out, lse)

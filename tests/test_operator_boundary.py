@@ -292,3 +292,14 @@ def test_logits_of_another_type_are_refused(given):
                 logprobs(logits=OnGpu(torch.zeros(shape, dtype=dtype)), dtype=given, row_stride=None, n_top=33)
             fits = own >= 0 and given in (None, own)
             assert ("n_top" in e.value.message) == fits and e.value.message.startswith("logits ") == (not fits), (dtype, e.value)
+
+
+def test_attend_scales_stay_finite_in_units_of_log_2():
+    for scale in (2.3e38, 1.0, 1e-38):
+        with pytest.raises(sp.SpError) as e:
+            attend(scale=scale, causal=2)
+        assert "causal" in e.value.message
+    for scale in (2.4e38, 2.9e38, 3.4e38):
+        with pytest.raises(sp.SpError) as e:
+            attend(scale=scale, causal=2)
+        assert "scale" in e.value.message
