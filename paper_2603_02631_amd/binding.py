@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 SP_LAYER_MEAN = 0
@@ -456,7 +457,7 @@ def host_offsets(values: Sequence[int]):
 
 
 def _offsets(values):
-    return values if isinstance(values, ctypes.Array) and values._type_ is ctypes.c_int64 else _host_i64(values)
+    return values if getattr(values, "_type_", None) is ctypes.c_int64 else _host_i64(values)
 
 
 # Types that an argument may have: its own, and the integers of its width (its bits). Filled at the first tensor (torch is not imported before).
@@ -479,6 +480,8 @@ def _check_type(t, what: str, known: set, plain_bytes: bool) -> None:
 
 def _typed(t, what: str, nbytes: int, known: set) -> Optional[int]:
     """As _ptr, for arguments whose elements could be misread: a tensor's type has to be one of `known`, or bytes."""
+    if t is None:           # before anything raises: an exception takes longer than a tensor's checks
+        return None
     try:
         if t.dtype in known and t.is_cuda and t.is_contiguous() and t.nbytes >= nbytes:
             return t.data_ptr()
@@ -493,6 +496,8 @@ def _typed(t, what: str, nbytes: int, known: set) -> Optional[int]:
 def _rows(t, what: str, rows: int, width: int, stride: Optional[int], known: set):
     """(address, row stride in elements) of `rows` rows of `width` contiguous elements: a tensor of a type in `known` whose
     first dimension counts rows and whose others are dense, or an address with its stride."""
+    if t is None:
+        return None, 0
     # two dimensions, the second dense: what a projection's output and its parts are. Few attribute reads, as in _ptr
     try:
         st = t.stride()
@@ -502,8 +507,6 @@ def _rows(t, what: str, rows: int, width: int, stride: Optional[int], known: set
                 return t.data_ptr(), st[0] if rows > 1 else (width + 7) & ~7      # the stride of a single row means nothing
     except AttributeError:
         pass
-    if t is None:
-        return None, 0
     if isinstance(t, int):
         return t, width if stride is None else stride
     if not getattr(t, "is_cuda", False):
@@ -535,14 +538,25 @@ def _table(block_table, B: int, table_stride: Optional[int]):
     return _typed(block_table, "block_table", 4 * B * table_stride, _INT32), table_stride
 
 
+_desc_fields = struct.Struct("4i5q").unpack_from        # all fields at once: half of what reading them one by one takes
+
+
 def _cache_bytes(desc: CacheDesc):
     """Query heads, kv heads, head_dim, a pool's element types, and the bytes that a pool and its scales have to hold."""
-    kv, d, pages, page = desc.n_kv_heads, desc.head_dim, desc.n_pages, desc.page_tokens
-    pool = (pages - 1) * desc.page_stride + (kv - 1) * desc.stride_head + (page - 1) * desc.stride_token + d
+    H, kv, d, kind, pages, page, page_stride, stride_head, stride_token = _desc_fields(desc)
+    pool = (pages - 1) * page_stride + (kv - 1) * stride_head + (page - 1) * stride_token + d
     scales = 4 * pages * kv * (page // SP_CACHE_BLOCK)
-    if desc.cache_type == SP_CACHE_E4M3:
-        return desc.n_q_heads, kv, d, _E4M3, pool, scales
-    return desc.n_q_heads, kv, d, _BF16, 2 * pool, scales
+    return (H, kv, d, _E4M3, pool, scales) if kind == SP_CACHE_E4M3 else (H, kv, d, _BF16, 2 * pool, scales)
+
+
+def _workspace(ws, ws_bytes: Optional[int]):
+    """(address, bytes) of a workspace."""
+    try:
+        if ws_bytes is None and ws.is_cuda and ws.is_contiguous():
+            return ws.data_ptr(), ws.nbytes
+    except AttributeError:
+        pass
+    return _ptr(ws, "ws"), _ws_bytes(ws, ws_bytes)
 
 
 def sp_cache_append(desc: CacheDesc, k, v, offsets_host, offsets_dev, start, block_table, k_pool, v_pool, k_scale=None,
@@ -552,7 +566,7 @@ def sp_cache_append(desc: CacheDesc, k, v, offsets_host, offsets_dev, start, blo
                     stream=None) -> None:
     off = _offsets(offsets_host)
     B = len(off) - 1
-    T = max(off[B], 0) if B >= 0 else 0
+    T = off[B] if B >= 0 and off[B] > 0 else 0
     H, kv, d, elems, pool, scales = _cache_bytes(desc)
     kw, qw = kv * d, H * d
     kp, ks = _rows(k, "k", T, kw, k_stride, _BF16)
@@ -562,12 +576,14 @@ def sp_cache_append(desc: CacheDesc, k, v, offsets_host, offsets_dev, start, blo
     if n_pos is None:
         n_pos = 0 if cos is None or isinstance(cos, int) else cos.shape[0]
     trig = 2 * n_pos * rot_dim
-    _check(load_library().sp_cache_append(
+    status = (_lib or load_library()).sp_cache_append(
         ctypes.byref(desc), kp, ks, vp, vs, qp, qs, _typed(q_out, "q_out", 2 * T * qw, _BF16), off,
         _typed(offsets_dev, "offsets_dev", 8 * (B + 1), _INT64), B, _typed(start, "start", 4 * B, _INT32),
         _typed(positions, "positions", 4 * T, _INT32), tab, width, _typed(cos, "cos", trig, _FP32), _typed(sin, "sin", trig, _FP32), n_pos, rot_dim, rot_style,
         _typed(k_pool, "k_pool", pool, elems), _typed(v_pool, "v_pool", pool, elems), _typed(k_scale, "k_scale", scales, _FP32),
-        _typed(v_scale, "v_scale", scales, _FP32), _stream(stream)))
+        _typed(v_scale, "v_scale", scales, _FP32), _stream(stream))
+    if status:
+        _check(status)
 
 
 def sp_attend_workspace(desc: CacheDesc, offsets_host, B: Optional[int] = None, max_len: int = 0) -> int:
@@ -586,16 +602,20 @@ def sp_attend(desc: CacheDesc, q, offsets_host, offsets_dev, lens, max_len: int,
               ws_bytes: Optional[int] = None, stream=None) -> None:
     off = _offsets(offsets_host)
     B = len(off) - 1
-    T = max(off[B], 0) if B >= 0 else 0
+    T = off[B] if B >= 0 and off[B] > 0 else 0
     tab, width = _table(block_table, B, table_stride)
     H, _, d, elems, pool, scales = _cache_bytes(desc)
     rows = T * H
-    _check(load_library().sp_attend(
+    ws_at, ws_size = _workspace(ws, ws_bytes)
+    status = (_lib or load_library()).sp_attend(
         ctypes.byref(desc), _typed(q, "q", 2 * rows * d, _BF16), off, _typed(offsets_dev, "offsets_dev", 8 * (B + 1), _INT64), B,
         _typed(lens, "lens", 4 * B, _INT32), max_len, tab, width, _typed(k_pool, "k_pool", pool, elems), _typed(v_pool, "v_pool", pool, elems),
-        _typed(k_scale, "k_scale", scales, _FP32), _typed(v_scale, "v_scale", scales, _FP32), scale, causal, window,
-        _typed(out, "out", 2 * rows * d, _BF16), _typed(lse, "lse", 4 * rows, _FP32), _ptr(ws, "ws"), _ws_bytes(ws, ws_bytes),
-        _stream(stream)))
+        _typed(k_scale, "k_scale", scales, _FP32),
+        _typed(v_scale, "v_scale", scales, _FP32), scale, causal, window,
+        _typed(out, "out", 2 * rows * d, _BF16), _typed(lse, "lse", 4 * rows, _FP32), ws_at, ws_size,
+        _stream(stream))
+    if status:
+        _check(status)
 
 
 def sp_logprobs_workspace(n_rows: int, vocab: int, n_top: int) -> int:
@@ -612,14 +632,13 @@ def sp_logprobs(logits, n_rows: int, vocab: int, targets, n_top: int, logprob, e
             raise SpError(1, "logits given as an address need a dtype")
         if not _BF16:
             _learn_types()
-        if logits.dtype in _BF16:
-            dtype = SP_LOGITS_BF16
-        else:
-            _check_type(logits, "logits", _FP32, False)
-            dtype = SP_LOGITS_F32
+        dtype = SP_LOGITS_BF16 if logits.dtype in _BF16 else SP_LOGITS_F32        # which refuses what is neither
     x, stride = _rows(logits, "logits", n_rows, vocab, row_stride, _FP32 if dtype == SP_LOGITS_F32 else _BF16)
     n, k = max(n_rows, 0), max(n_top, 0)
-    _check(load_library().sp_logprobs(
+    ws_at, ws_size = _workspace(ws, ws_bytes)
+    status = (_lib or load_library()).sp_logprobs(
         x, dtype, n_rows, vocab, stride or row_stride or vocab, _typed(targets, "targets", 4 * n, _INT32), n_top,
         _typed(logprob, "logprob", 4 * n, _FP32), _typed(entropy, "entropy", 4 * n, _FP32), _typed(top_ids, "top_ids", 4 * n * k, _INT32),
-        _typed(top_logprobs, "top_logprobs", 4 * n * k, _FP32), _ptr(ws, "ws"), _ws_bytes(ws, ws_bytes), _stream(stream)))
+        _typed(top_logprobs, "top_logprobs", 4 * n * k, _FP32), ws_at, ws_size, _stream(stream))
+    if status:
+        _check(status)
