@@ -256,7 +256,15 @@ __global__ __launch_bounds__(kThreads) void sp_cache_append_kernel(AppendArgs a)
             float scale = exp2_of(e), inv = exp2_of(-e);
             if (old[i] > scale) {
                 scale = old[i];
-                inv = 1.f / old[i];
+                inv = 1.f / scale;
+                if (fresh && (__float_as_uint(scale) & 0x7fffffu) != 0) {    // not of this call's making: only a quotient is x / s there
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        lo[i][e] /= scale;
+                        hi[i][e] /= scale;
+                    }
+                    inv = 1.f;
+                }
             }
             uint8_t *dst = (val ? a.v_pool : a.k_pool) + elem;
             if (fresh) {

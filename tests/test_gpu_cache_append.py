@@ -284,3 +284,28 @@ def test_append_in_place_queries_and_graph_replays():
         for t, u in zip(pools + scales, first):
             assert torch.equal(t, u)
     assert torch.equal(pools[0], eager[0]) and torch.equal(scales[1], eager[3])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("scale", [7.0, 14.0, 3.0, 0.4375, 1.7])
+def test_append_behind_tokens_whose_scale_is_no_power_of_two(d, scale):
+    """Pages that something else has filled: codes are those of x / s, half-way cases among them (175 / 7 = 25 lies between 24 and 26), which x times
+    the rounded 1 / s misses."""
+    c = ou.Paged(1, d, 32, [1], True, seed=11)
+    page, rng = c.table[0, 0], np.random.default_rng(15)
+    c.ks[page, 0, 0] = c.vs[page, 0, 0] = scale
+    for j in range(3):
+        c.k[c.at(0, 0, j):c.at(0, 0, j) + d] = rng.integers(0, 120, d)
+        c.v[c.at(0, 0, j):c.at(0, 0, j) + d] = rng.integers(0, 120, d)
+    n = 20
+    half = rng.integers(8, 16, (n, 3 * d)) * 2 + 1                  # of codes 16 .. 30, two apart
+    qkv = ou.bf16_round((half * np.float32(scale) * np.exp2(rng.integers(-6, 3, half.shape))).astype(np.float32) * rng.choice([-1, 1], half.shape))
+    qkv = np.clip(qkv, -128 * scale, 128 * scale).astype(np.float32)
+    qkv = ou.bf16_round(qkv)
+    got = run(c, 1, [0, n], [3], qkv, None, None, 0, "half")
+    Reference(c).store(0, 3, qkv[:, None, d:2 * d], qkv[:, None, 2 * d:])
+    assert c.ks[page, 0, 0] == np.float32(scale)
+    same_codes(got[0], c.k)
+    same_codes(got[1], c.v)
+    np.testing.assert_array_equal(got[2], c.ks)
+    np.testing.assert_array_equal(got[3], c.vs)
