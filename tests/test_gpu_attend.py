@@ -345,3 +345,24 @@ def test_queries_of_zero_at_the_largest_scales(news, d, e4m3):
     q[:] = 0
     out, lse = call(c, 4, off, q, lens, 300, 2.3e38, 1, 0)
     verify(c, 4, held, off, q, lens, 1.0, 1, 0, out, lse)
+
+
+@pytest.mark.parametrize("e4m3", [True, False])
+@pytest.mark.parametrize("H,kv,d", [(8, 2, 64), (4, 2, 128)])
+def test_masks_where_few_rows_are_shared_out(e4m3, H, kv, d):
+    """Windows leave far fewer blocks than the bound on the lengths says; without a mask every row sees all. One context is shorter than its rows."""
+    news, lens = [1, 8, 3, 5, 2], [3000, 9000, 5200, 2, 0]
+    c, held, off, q = build(H, kv, d, news, lens, 64, e4m3, "HND", 0, 15, max_len=9000)
+    assert sp.sp_attend_workspace(desc_of(c, H), off.tolist(), len(lens), 9000) > 0
+    for causal, window in ((0, 0), (1, 0), (1, 1), (1, 31), (1, 100), (1, 2500), (1, 8999), (1, 9000), (1, 1 << 40)):
+        out, lse = call(c, H, off, q, lens, 9000, 0.125, causal, window)
+        verify(c, H, held, off, q, lens, 0.125, causal, window, out, lse)
+
+
+@pytest.mark.parametrize("e4m3", [True, False])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("others", [1, 99])
+def test_lines_of_more_parts_than_lanes(e4m3, d, others):
+    """A context of 40000 tokens of one kv head is joined from more than 64 partial results: by four waves a row, or by one where there are many lines."""
+    rng = np.random.default_rng(16)
+    check(2, 1, d, [2] + [1] * others, [40000] + rng.integers(1, 80, others).tolist(), 512, e4m3)
