@@ -495,9 +495,9 @@ typedef enum { SP_ROTATE_HALF = 0, SP_ROTATE_PAIRS = 1 } sp_rotate_style;
  *    of SP_CACHE_BLOCK slots and kv head that this call brings, the largest magnitude m gives
  *    the smallest power of two s >= 2^-64 with m <= 448 s; a block that already holds tokens
  *    before start_dev[b] keeps the larger of s and its present scale, and the codes of those
- *    tokens are brought to it (exactly, but for values that fall among E4M3's subnormals); new codes
- *    are E4M3(x / s), rounded to nearest, x / s in float. Results that are not finite are stored as NaN
- *    codes and do not count for m.
+ *    tokens are brought to it (exactly where that scale was a power of two, but for values that fall among
+ *    E4M3's subnormals); new codes are E4M3(x / s), rounded to nearest, x / s in float. Results that are not
+ *    finite are stored as NaN codes and do not count for m.
  * Slots at and behind start + new tokens are not touched, except that a new token may lie in a
  * slot that is in use: then it is replaced (a rejected lookahead token), and with it
  * whatever follows it in its block. Tokens whose slot lies beyond the block table's row, or whose page is not

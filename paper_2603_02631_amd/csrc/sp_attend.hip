@@ -5,6 +5,11 @@
 //   lse = m + log l,
 // in one pass over the keys: a reference m and a sum l that run along, and the partial output, scaled whenever m moves.
 //
+// Rounded to fewer bits: the probabilities that go into the second product, to bf16 (2^-8 of each at most), since the matrix instructions take
+// both operands in one type and the values are bf16, or 8-bit codes that bf16 holds exactly; fp32 operands would take a sixteenth of the rate. Their sum is taken
+// before, in fp32, as are m, l, the logits and the partial outputs. The output is bf16 itself: its error against 64 bits is 0.0015 to 0.0017 of
+// the 2-norm with the probabilities in fp32, 0.0016 to 0.0021 with these.
+//
 // Query rows of one request that share a kv head (n_b tokens of G heads) are taken together, so that a key is read once for
 // all of them. Requests of up to few_rows_of() rows go to sp_attend_few_kernel, which is bound by the cache's bytes, others to
 // sp_attend_many_kernel, tiles of 256 rows, which is bound by its operations.
@@ -353,7 +358,7 @@ struct Rows {
     }
 
     // x: products <q, k> of this lane's eight keys, factor: what makes logits in units of log 2 of them. Returns 2^vexp times the probabilities as bf16;
-    // vinv = 2^-vexp.
+    // vinv = 2^-vexp by v_rcp_f32: exact for powers of two, 2^-23 of a block's part of the sum for others.
     __device__ __forceinline__ bf16x8 weigh(int t, const float (&x)[8], float factor, float vexp, float vinv)
     {
         const float top = factor * larger(larger(larger(x[0], x[1]), larger(x[2], x[3])), larger(larger(x[4], x[5]), larger(x[6], x[7])));
