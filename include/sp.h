@@ -433,15 +433,23 @@ sp_status sp_assemble(const int32_t *target_ids_dev, int64_t M,
  * logits, one decoder layer at a time: new keys and values go into a paged
  * cache (sp_cache_append), queries attend over it (sp_attend), and the next
  * token and the probabilities of given ones are read off the logits
- * (sp_logprobs). A bf16 cache with pages of a multiple of 512 tokens is what
+ * (sp_logprobs). Projections can be products in 4 bits (sp_mx4_quantise,
+ * sp_mx4_matmul), and a cache can be held to a budget: what its tokens draw is
+ * added up (sp_attend_weights) and the rest is dropped (sp_cache_evict). A bf16 cache with pages of a multiple of 512 tokens is what
  * sp_score_paged reads afterwards.
  */
 
 /* How a paged cache holds its elements. SP_CACHE_BF16: as they are.
  * SP_CACHE_E4M3: OCP E4M3 codes, one byte each, with one float scale for every
- * SP_CACHE_BLOCK consecutive tokens of a page and kv head: value = scale * E4M3(code). */
-typedef enum { SP_CACHE_BF16 = 0, SP_CACHE_E4M3 = 1 } sp_cache_type;
+ * SP_CACHE_BLOCK consecutive tokens of a page and kv head: value = scale * E4M3(code).
+ * SP_CACHE_MX4: microscaled 4-bit elements (OCP MXFP4): E2M1 codes (1 sign, 2 exponent
+ * bits, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6), two to a byte, the lower element in the
+ * lower bits, with one scale for every SP_MX4_GROUP consecutive elements of a token and
+ * head: a byte e that stands for 2^(e - 127), or for NaN (as does every element of the
+ * group then) where it is 255. */
+typedef enum { SP_CACHE_BF16 = 0, SP_CACHE_E4M3 = 1, SP_CACHE_MX4 = 3 } sp_cache_type;
 #define SP_CACHE_BLOCK 32
+#define SP_MX4_GROUP 32
 
 /* A layer's paged cache: two pools (keys, values) of n_pages pages each with the
  * same strides, in elements, head_dim contiguous:
@@ -450,12 +458,13 @@ typedef enum { SP_CACHE_BF16 = 0, SP_CACHE_E4M3 = 1 } sp_cache_type;
  *   page = block_table_dev[b * table_stride + j / page_tokens]
  * block_table_dev: device, int32; table_stride entries for each request. E4M3
  * pools come with dense float scale arrays
- * [n_pages][n_kv_heads][page_tokens / SP_CACHE_BLOCK] (k_scale, v_scale; null for
- * bf16). Pools, queries, keys and values are 16-byte aligned. Query head h reads
- * kv head h / (n_q_heads / n_kv_heads).
+ * [n_pages][n_kv_heads][page_tokens / SP_CACHE_BLOCK], MX4 pools with dense byte scale
+ * arrays [n_pages][n_kv_heads][page_tokens][head_dim / SP_MX4_GROUP], 16-byte aligned
+ * (k_scale, v_scale; null for bf16). Pools, queries, keys and values are 16-byte aligned.
+ * Query head h reads kv head h / (n_q_heads / n_kv_heads).
  * Supported: head_dim 64 or 128; n_q_heads a multiple of n_kv_heads with ratio
  * G <= 16; n_kv_heads <= 4096; page_tokens a positive multiple of SP_CACHE_BLOCK, at most
- * 2^24; strides multiples of 16 (E4M3) or 8 (bf16) elements, stride_token >=
+ * 2^24; strides multiples of 32 (MX4), 16 (E4M3) or 8 (bf16) elements, stride_token >=
  * head_dim and <= 2^24, none above 2^40; 1 <= n_pages < 2^31. */
 typedef struct {
     int32_t n_q_heads;
@@ -497,12 +506,13 @@ typedef enum { SP_ROTATE_HALF = 0, SP_ROTATE_PAIRS = 1 } sp_rotate_style;
  *    before start_dev[b] keeps the larger of s and its present scale, and the codes of those
  *    tokens are brought to it (exactly where that scale was a power of two, but for values that fall among
  *    E4M3's subnormals); new codes are E4M3(x / s), rounded to nearest, x / s in float. Results that are not
- *    finite are stored as NaN codes and do not count for m.
+ *    finite are stored as NaN codes and do not count for m. MX4 caches: each group of a token by itself,
+ *    by the rule of sp_mx4_quantise; no other token's codes or scales are looked at.
  * Slots at and behind start + new tokens are not touched, except that a new token may lie in a
- * slot that is in use: then it is replaced (a rejected lookahead token), and with it
+ * slot that is in use: then it is replaced (a rejected lookahead token), and, in an E4M3 cache, with it
  * whatever follows it in its block. Tokens whose slot lies beyond the block table's row, or whose page is not
  * in [0, n_pages), are not stored (their queries are still rotated). Two requests
- * of one call must not append to the same page's same block.
+ * of one call must not append to the same page's same block (MX4 and bf16: slot).
  */
 sp_status sp_cache_append(const sp_cache_desc *desc, const void *k_dev, int64_t k_stride,
                           const void *v_dev, int64_t v_stride, const void *q_dev,
@@ -511,8 +521,8 @@ sp_status sp_cache_append(const sp_cache_desc *desc, const void *k_dev, int64_t 
                           const int32_t *positions_dev, const int32_t *block_table_dev,
                           int64_t table_stride, const float *cos_dev, const float *sin_dev,
                           int64_t n_pos, int32_t rot_dim, int32_t rot_style,
-                          void *k_pool_dev, void *v_pool_dev, float *k_scale_dev,
-                          float *v_scale_dev, void *hip_stream);
+                          void *k_pool_dev, void *v_pool_dev, void *k_scale_dev,
+                          void *v_scale_dev, void *hip_stream);
 
 /* Bytes of workspace sp_attend needs for these queries and contexts of at most
  * max_len tokens (0 where it needs none). They are enough for every smaller max_len too, so
@@ -536,7 +546,7 @@ sp_status sp_attend_workspace(const sp_cache_desc *desc, const int64_t *offsets_
  * context among them) may hold anything, NaN included.
  * What a row sees should be finite: logits below 2^120, values below 2^90 in magnitude, scales
  * finite and not negative (a value scale below 2^-64 may count as 2^-64: zero is in order for a block
- * of zeros). A row that sees a NaN becomes NaN, and other rows of its request may.
+ * of zeros); scale bytes of MX4 caches below 2^90. A row that sees a NaN becomes NaN, and other rows of its request may.
  * At most 2^26 query tokens and contexts of at most 2^30 tokens; requests times kv heads, and tiles of 256
  * query rows times kv heads, below 2^23.
  * max_len bounds the contexts from the host's side (a longer lens[b] counts as
@@ -550,11 +560,60 @@ sp_status sp_attend(const sp_cache_desc *desc, const void *q_dev,
                     const int32_t *lens_dev, int64_t max_len,
                     const int32_t *block_table_dev, int64_t table_stride,
                     const void *k_pool_dev, const void *v_pool_dev,
-                    const float *k_scale_dev, const float *v_scale_dev, float scale,
+                    const void *k_scale_dev, const void *v_scale_dev, float scale,
                     int32_t causal, int64_t window, void *out_dev, float *lse_dev,
                     void *ws_dev, size_t ws_bytes, void *hip_stream);
 
-/* Type of logits. */
+/*
+ * How much attention the tokens of a paged cache have drawn: the weight that decides which of them sp_cache_evict
+ * keeps. Queries, contexts, masks and the cache's keys are those of an sp_attend call, whose lse_dev this call
+ * takes; the values are not looked at:
+ *   weights_dev[b, h, j] = old + sum over rows r of request b that see key j, and over the query heads g of kv head h, of
+ *                          exp( scale * <q[r, g], K[b, h, j]> - lse_dev[r, g] )
+ * for j < lens[b]; entries behind are left as they were. weights_dev: float [B][n_kv_heads][weights_stride],
+ * weights_stride >= max_len. old = old_dev[b, h, j] (the same layout; may be weights_dev itself, else they must not overlap) for
+ * tokens that were there before the rows' own: j < lens[b] - n_b with causal = 1, all with causal = 0; 0 for the others
+ * and where old_dev is null. A request without rows keeps its old weights. Rows with an lse of minus infinity add nothing.
+ * Arithmetic is in fp32, in an order that is fixed by the lengths.
+ * A row that sees a NaN, or whose lse is NaN, makes NaN of the weights that it adds to, and of others of its request.
+ * Limits as in sp_attend; requests times kv heads at most 65535.
+ */
+sp_status sp_attend_weights(const sp_cache_desc *desc, const void *q_dev, const int64_t *offsets_host,
+                            const int64_t *offsets_dev, int32_t B, const int32_t *lens_dev, int64_t max_len,
+                            const int32_t *block_table_dev, int64_t table_stride, const void *k_pool_dev,
+                            const void *k_scale_dev, float scale, int32_t causal, int64_t window,
+                            const float *lse_dev, const float *old_dev, float *weights_dev,
+                            int64_t weights_stride, void *hip_stream);
+
+/*
+ * Eviction: the cached tokens of most weight, of each kv head by itself, into other pages. Request b has lens_dev[b] tokens
+ * and a budget of budget_dev[b] (device, int32; a negative one counts as 0, one above max_budget as max_budget). With n = min(len, budget):
+ *   - a context of at most the budget is kept whole;
+ *   - else the first s = min(sinks, budget) tokens, the last r = min(recent, budget - s), and of those between the
+ *     budget - s - r with the largest weights_dev[b, h, j], equal weights in favour of the earlier token. Weights are compared
+ *     as numbers, a positive NaN above and a negative one below all others, -0 equal to 0.
+ * The kept tokens of kv head h, in their order, become tokens 0 .. n - 1 of the pages that dst_table_dev names:
+ *   - their keys and values (v_pool_dev and v_scale_dev as in sp_attend). bf16 and MX4 as they are, with their scales. E4M3: a block takes the
+ *     largest scale s among those of its tokens (a NaN counts as the largest), codes are brought to it, E4M3(code * (scale / s)): exactly where scales are powers of
+ *     two, but for what falls among the subnormals;
+ *   - kept_dev[b, h, i] (int32 [B][n_kv_heads][max_budget]): which token it was;
+ *   - new_weights_dev[b, h, i] (optional, float [B][n_kv_heads][max_budget], not weights_dev itself): its weight.
+ * new_lens_dev[b] = n (int32, neither lens_dev nor budget_dev itself). Entries and slots at and behind n are left as they were.
+ * Keys keep the rotation of their old position: new tokens go on from there (sp_cache_append's positions_dev), while attention's masks and windows
+ * count slots. The pages of dst_table must not be among those that block_table names (for any request): source pages are only read, and free afterwards;
+ * pages that requests share stay as they are. Tokens whose destination lies beyond dst_table's row, or whose destination page is not in [0, n_pages), are not moved.
+ * weights_dev: float [B][n_kv_heads][weights_stride], weights_stride >= max_len. Contexts are bounded by max_len as in sp_attend. sinks, recent >= 0.
+ * 0 <= max_budget <= 2^30, min(max_len, max_budget) < 2^29; requests times kv heads at most 65535. The result does not change from call to call.
+ */
+sp_status sp_cache_evict(const sp_cache_desc *desc, int32_t B, const int32_t *lens_dev, int64_t max_len,
+                         const int32_t *budget_dev, int64_t max_budget, int64_t sinks, int64_t recent,
+                         const float *weights_dev, int64_t weights_stride,
+                         const int32_t *block_table_dev, int64_t table_stride,
+                         const int32_t *dst_table_dev, int64_t dst_stride, void *k_pool_dev, void *v_pool_dev,
+                         void *k_scale_dev, void *v_scale_dev, int32_t *new_lens_dev, int32_t *kept_dev,
+                         float *new_weights_dev, void *hip_stream);
+
+/* Type of logits, and of what goes into and comes out of a product in 4 bits. */
 typedef enum { SP_LOGITS_F32 = 0, SP_LOGITS_BF16 = 1 } sp_logits_type;
 
 /* Largest number of alternatives sp_logprobs reports. */
@@ -586,6 +645,30 @@ sp_status sp_logprobs(const void *logits_dev, int32_t dtype, int64_t n_rows, int
                       float *logprob_dev, float *entropy_dev, int32_t *top_ids_dev,
                       float *top_logprobs_dev, void *ws_dev, size_t ws_bytes,
                       void *hip_stream);
+
+/*
+ * Rows of numbers to microscaled 4-bit elements (as in SP_CACHE_MX4 caches). Of each SP_MX4_GROUP elements x of a row the
+ * largest magnitude m gives the smallest power of two s >= 2^-64 with m <= 6 s; scales_dev[r][k / 32] = log2 s + 127, and
+ * codes are E2M1(x / s), rounded to nearest, halfway to the even code, the sign of zero kept. A group that holds a NaN or an
+ * infinity gets scale byte 255 and codes of zero.
+ * x_dev: float or bf16 (dtype an sp_logits_type), row r at r * row_stride elements (row_stride >= K, a multiple of 8, rows 16-byte
+ * aligned). codes_dev: [rows][K / 2] bytes, scales_dev: [rows][K / 32] bytes, both dense, codes 16-byte, scales 4-byte aligned. K is a positive multiple of 32
+ * below 2^31. 0 <= rows < 2^31; rows * K < 2^35.
+ */
+sp_status sp_mx4_quantise(const void *x_dev, int32_t dtype, int64_t rows, int64_t K, int64_t row_stride,
+                          void *codes_dev, void *scales_dev, void *hip_stream);
+
+/*
+ * Product of two microscaled 4-bit matrices, a projection's activations and weights:
+ *   out_dev[m][n] = sum_k A[m][k] W[n][k],  0 <= m < M, 0 <= n < N
+ * with A and W as sp_mx4_quantise leaves them: a_codes_dev [M][K / 2], a_scales_dev [M][K / 32], w_codes_dev [N][K / 2], w_scales_dev
+ * [N][K / 32], dense, codes 16-byte, scales 4-byte aligned. out_dev: float or bf16 (dtype an sp_logits_type), row m at m * out_stride
+ * elements (out_stride >= N). Products are exact, sums are held in fp32 in an order that the sizes fix, the result is rounded once.
+ * Rows with a NaN scale give NaN. K is a positive multiple of 32 below 2^31, 0 <= M, N < 2^31; (M / 16 + 1) * (N / 16 + 1) < 2^26.
+ */
+sp_status sp_mx4_matmul(const void *a_codes_dev, const void *a_scales_dev, int64_t M, const void *w_codes_dev,
+                        const void *w_scales_dev, int64_t N, int64_t K, void *out_dev, int32_t dtype, int64_t out_stride,
+                        void *hip_stream);
 
 /*
  * Measurement aid: streams `bytes` bytes of buf_dev (device, 16-byte aligned,

@@ -16,7 +16,9 @@ SP_LAYER_MEAN = 0
 SP_LAYER_MAX = 1
 SP_CACHE_BF16 = 0
 SP_CACHE_E4M3 = 1
+SP_CACHE_MX4 = 3
 SP_CACHE_BLOCK = 32
+SP_MX4_GROUP = 32
 SP_ROTATE_HALF = 0
 SP_ROTATE_PAIRS = 1
 SP_LOGITS_F32 = 0
@@ -34,6 +36,7 @@ EXPORTS = (
     "sp_assemble_workspace", "sp_assemble", "sp_last_error", "sp_version",
     "sp_debug_fused_giveup", "sp_debug_score_path", "sp_hbm_read_probe",
     "sp_cache_append", "sp_attend_workspace", "sp_attend", "sp_logprobs_workspace", "sp_logprobs",
+    "sp_attend_weights", "sp_cache_evict", "sp_mx4_quantise", "sp_mx4_matmul",
 )
 
 
@@ -127,6 +130,12 @@ def load_library():
     lib.sp_attend_workspace.argtypes = [CD, I64P, c.c_int32, c.c_int64, c.POINTER(c.c_size_t)]
     lib.sp_attend.argtypes = [CD, P, I64P, P, c.c_int32, P, c.c_int64, P, c.c_int64, P, P, P, P, c.c_float, c.c_int32,
                               c.c_int64, P, P, P, c.c_size_t, P]
+    lib.sp_attend_weights.argtypes = [CD, P, I64P, P, c.c_int32, P, c.c_int64, P, c.c_int64, P, P, c.c_float, c.c_int32, c.c_int64,
+                                      P, P, P, c.c_int64, P]
+    lib.sp_cache_evict.argtypes = [CD, c.c_int32, P, c.c_int64, P, c.c_int64, c.c_int64, c.c_int64, P, c.c_int64, P, c.c_int64,
+                                   P, c.c_int64, P, P, P, P, P, P, P, P]
+    lib.sp_mx4_quantise.argtypes = [P, c.c_int32, c.c_int64, c.c_int64, c.c_int64, P, P, P]
+    lib.sp_mx4_matmul.argtypes = [P, P, c.c_int64, P, P, c.c_int64, c.c_int64, P, c.c_int32, c.c_int64, P]
     lib.sp_logprobs_workspace.argtypes = [c.c_int64, c.c_int64, c.c_int32, c.POINTER(c.c_size_t)]
     lib.sp_logprobs.argtypes = [P, c.c_int32, c.c_int64, c.c_int64, c.c_int64, P, c.c_int32, P, P, P, P, P, c.c_size_t, P]
     lib.sp_hbm_read_probe.argtypes = [P, c.c_size_t, P, P]
@@ -461,13 +470,14 @@ def _offsets(values):
 
 
 # Types that an argument may have: its own, and the integers of its width (its bits). Filled at the first tensor (torch is not imported before).
-_INT32, _INT64, _FP32, _BF16, _E4M3 = set(), set(), set(), set(), set()
+_INT32, _INT64, _FP32, _BF16, _E4M3, _BYTES = set(), set(), set(), set(), set(), set()
 
 
 def _learn_types() -> None:
     import torch
     for known, names in ((_INT32, ("int32", "uint32")), (_INT64, ("int64", "uint64")), (_FP32, ("float32", "int32", "uint32")),
-                         (_BF16, ("bfloat16", "int16", "uint16")), (_E4M3, ("float8_e4m3fn", "uint8", "int8"))):
+                         (_BF16, ("bfloat16", "int16", "uint16")), (_E4M3, ("float8_e4m3fn", "uint8", "int8")),
+                         (_BYTES, ("uint8", "int8", "float4_e2m1fn_x2", "float8_e8m0fnu"))):
         known.update(getattr(torch, name) for name in names if hasattr(torch, name))
 
 
@@ -542,11 +552,13 @@ _desc_fields = struct.Struct("4i5q").unpack_from        # all fields at once: ha
 
 
 def _cache_bytes(desc: CacheDesc):
-    """Query heads, kv heads, head_dim, a pool's element types, and the bytes that a pool and its scales have to hold."""
+    """Query heads, kv heads, head_dim, a pool's element types and those of its scales, and the bytes that a pool and its scales have to hold."""
     H, kv, d, kind, pages, page, page_stride, stride_head, stride_token = _desc_fields(desc)
     pool = (pages - 1) * page_stride + (kv - 1) * stride_head + (page - 1) * stride_token + d
+    if kind == SP_CACHE_MX4:
+        return H, kv, d, _BYTES, _BYTES, pool // 2, pages * kv * page * (d // SP_MX4_GROUP)
     scales = 4 * pages * kv * (page // SP_CACHE_BLOCK)
-    return (H, kv, d, _E4M3, pool, scales) if kind == SP_CACHE_E4M3 else (H, kv, d, _BF16, 2 * pool, scales)
+    return (H, kv, d, _E4M3, _FP32, pool, scales) if kind == SP_CACHE_E4M3 else (H, kv, d, _BF16, _FP32, 2 * pool, scales)
 
 
 def _workspace(ws, ws_bytes: Optional[int]):
@@ -567,7 +579,7 @@ def sp_cache_append(desc: CacheDesc, k, v, offsets_host, offsets_dev, start, blo
     off = _offsets(offsets_host)
     B = len(off) - 1
     T = off[B] if B >= 0 and off[B] > 0 else 0
-    H, kv, d, elems, pool, scales = _cache_bytes(desc)
+    H, kv, d, elems, of_scales, pool, scales = _cache_bytes(desc)
     kw, qw = kv * d, H * d
     kp, ks = _rows(k, "k", T, kw, k_stride, _BF16)
     vp, vs = _rows(v, "v", T, kw, v_stride, _BF16)
@@ -580,8 +592,8 @@ def sp_cache_append(desc: CacheDesc, k, v, offsets_host, offsets_dev, start, blo
         ctypes.byref(desc), kp, ks, vp, vs, qp, qs, _typed(q_out, "q_out", 2 * T * qw, _BF16), off,
         _typed(offsets_dev, "offsets_dev", 8 * (B + 1), _INT64), B, _typed(start, "start", 4 * B, _INT32),
         _typed(positions, "positions", 4 * T, _INT32), tab, width, _typed(cos, "cos", trig, _FP32), _typed(sin, "sin", trig, _FP32), n_pos, rot_dim, rot_style,
-        _typed(k_pool, "k_pool", pool, elems), _typed(v_pool, "v_pool", pool, elems), _typed(k_scale, "k_scale", scales, _FP32),
-        _typed(v_scale, "v_scale", scales, _FP32), _stream(stream))
+        _typed(k_pool, "k_pool", pool, elems), _typed(v_pool, "v_pool", pool, elems), _typed(k_scale, "k_scale", scales, of_scales),
+        _typed(v_scale, "v_scale", scales, of_scales), _stream(stream))
     if status:
         _check(status)
 
@@ -604,14 +616,14 @@ def sp_attend(desc: CacheDesc, q, offsets_host, offsets_dev, lens, max_len: int,
     B = len(off) - 1
     T = off[B] if B >= 0 and off[B] > 0 else 0
     tab, width = _table(block_table, B, table_stride)
-    H, _, d, elems, pool, scales = _cache_bytes(desc)
+    H, _, d, elems, of_scales, pool, scales = _cache_bytes(desc)
     rows = T * H
     ws_at, ws_size = _workspace(ws, ws_bytes)
     status = (_lib or load_library()).sp_attend(
         ctypes.byref(desc), _typed(q, "q", 2 * rows * d, _BF16), off, _typed(offsets_dev, "offsets_dev", 8 * (B + 1), _INT64), B,
         _typed(lens, "lens", 4 * B, _INT32), max_len, tab, width, _typed(k_pool, "k_pool", pool, elems), _typed(v_pool, "v_pool", pool, elems),
-        _typed(k_scale, "k_scale", scales, _FP32),
-        _typed(v_scale, "v_scale", scales, _FP32), scale, causal, window,
+        _typed(k_scale, "k_scale", scales, of_scales),
+        _typed(v_scale, "v_scale", scales, of_scales), scale, causal, window,
         _typed(out, "out", 2 * rows * d, _BF16), _typed(lse, "lse", 4 * rows, _FP32), ws_at, ws_size,
         _stream(stream))
     if status:
@@ -640,5 +652,93 @@ def sp_logprobs(logits, n_rows: int, vocab: int, targets, n_top: int, logprob, e
         x, dtype, n_rows, vocab, stride or row_stride or vocab, _typed(targets, "targets", 4 * n, _INT32), n_top,
         _typed(logprob, "logprob", 4 * n, _FP32), _typed(entropy, "entropy", 4 * n, _FP32), _typed(top_ids, "top_ids", 4 * n * k, _INT32),
         _typed(top_logprobs, "top_logprobs", 4 * n * k, _FP32), ws_at, ws_size, _stream(stream))
+    if status:
+        _check(status)
+
+
+def _line_stride(t, what: str, lines: int, width: int, stride: Optional[int]) -> int:
+    """Entries of a (request, kv head) line of a dense [requests][kv heads][entries] array."""
+    if stride is not None:
+        return stride
+    if not hasattr(t, "shape"):
+        return width
+    if t.dim() != 3:
+        raise SpError(1, f"{what} has to be [requests][kv heads][entries]")
+    return t.shape[2]
+
+
+def sp_attend_weights(desc: CacheDesc, q, offsets_host, offsets_dev, lens, max_len: int, block_table, k_pool, k_scale, scale: float, lse,
+                      old, weights, causal: int = 1, window: int = 0, table_stride: Optional[int] = None,
+                      weights_stride: Optional[int] = None, stream=None) -> None:
+    off = _offsets(offsets_host)
+    B = len(off) - 1
+    T = off[B] if B >= 0 and off[B] > 0 else 0
+    tab, width = _table(block_table, B, table_stride)
+    H, kv, d, elems, of_scales, pool, scales = _cache_bytes(desc)
+    entries = _line_stride(weights, "weights", B * kv, max_len, weights_stride)
+    if old is not None and entries != _line_stride(old, "old", B * kv, max_len, weights_stride):
+        raise SpError(1, "old and weights differ in shape")
+    size = 4 * B * kv * max(entries, 0)
+    status = (_lib or load_library()).sp_attend_weights(
+        ctypes.byref(desc), _typed(q, "q", 2 * T * H * d, _BF16), off, _typed(offsets_dev, "offsets_dev", 8 * (B + 1), _INT64), B,
+        _typed(lens, "lens", 4 * B, _INT32), max_len, tab, width, _typed(k_pool, "k_pool", pool, elems), _typed(k_scale, "k_scale", scales, of_scales),
+        scale, causal, window, _typed(lse, "lse", 4 * T * H, _FP32), _typed(old, "old", size, _FP32), _typed(weights, "weights", size, _FP32), entries,
+        _stream(stream))
+    if status:
+        _check(status)
+
+
+def sp_cache_evict(desc: CacheDesc, lens, max_len: int, budget, max_budget: int, sinks: int, recent: int, weights, block_table, dst_table,
+                   k_pool, v_pool, k_scale, v_scale, new_lens, kept, new_weights=None, B: Optional[int] = None,
+                   weights_stride: Optional[int] = None, table_stride: Optional[int] = None, dst_stride: Optional[int] = None, stream=None) -> None:
+    if B is None:
+        if not hasattr(lens, "shape"):
+            raise SpError(1, "lens given as an address needs B")
+        B = lens.numel()
+    n = max(B, 0)
+    tab, width = _table(block_table, n, table_stride)
+    dst, dst_width = _table(dst_table, n, dst_stride)
+    _, kv, _, elems, of_scales, pool, scales = _cache_bytes(desc)
+    entries = _line_stride(weights, "weights", n * kv, max_len, weights_stride)
+    held = 4 * n * kv * max(max_budget, 0)
+    status = (_lib or load_library()).sp_cache_evict(
+        ctypes.byref(desc), B, _typed(lens, "lens", 4 * n, _INT32), max_len, _typed(budget, "budget", 4 * n, _INT32), max_budget, sinks, recent,
+        _typed(weights, "weights", 4 * n * kv * max(entries, 0), _FP32), entries, tab, width, dst, dst_width, _typed(k_pool, "k_pool", pool, elems),
+        _typed(v_pool, "v_pool", pool, elems), _typed(k_scale, "k_scale", scales, of_scales), _typed(v_scale, "v_scale", scales, of_scales),
+        _typed(new_lens, "new_lens", 4 * n, _INT32), _typed(kept, "kept", held, _INT32), _typed(new_weights, "new_weights", held, _FP32), _stream(stream))
+    if status:
+        _check(status)
+
+
+def _float_kind(t, what: str, dtype: Optional[int]) -> int:
+    """SP_LOGITS_BF16 or SP_LOGITS_F32, from the tensor if it is not given."""
+    if dtype is not None:
+        return dtype
+    if not hasattr(t, "dtype"):
+        raise SpError(1, f"{what} given as an address needs a dtype")
+    if not _BF16:
+        _learn_types()
+    return SP_LOGITS_BF16 if t.dtype in _BF16 else SP_LOGITS_F32        # the caller refuses what is neither
+
+
+def sp_mx4_quantise(x, rows: int, K: int, codes, scales, dtype: Optional[int] = None, row_stride: Optional[int] = None, stream=None) -> None:
+    dtype = _float_kind(x, "x", dtype)
+    at, stride = _rows(x, "x", rows, K, row_stride, _FP32 if dtype == SP_LOGITS_F32 else _BF16)
+    n, k = max(rows, 0), max(K, 0)
+    status = (_lib or load_library()).sp_mx4_quantise(at, dtype, rows, K, stride or row_stride or K, _typed(codes, "codes", n * k // 2, _BYTES),
+                                                      _typed(scales, "scales", n * (k // SP_MX4_GROUP), _BYTES), _stream(stream))
+    if status:
+        _check(status)
+
+
+def sp_mx4_matmul(a_codes, a_scales, M: int, w_codes, w_scales, N: int, K: int, out, dtype: Optional[int] = None,
+                  out_stride: Optional[int] = None, stream=None) -> None:
+    dtype = _float_kind(out, "out", dtype)
+    to, stride = _rows(out, "out", M, N, out_stride, _FP32 if dtype == SP_LOGITS_F32 else _BF16)
+    m, n, k = max(M, 0), max(N, 0), max(K, 0)
+    status = (_lib or load_library()).sp_mx4_matmul(
+        _typed(a_codes, "a_codes", m * k // 2, _BYTES), _typed(a_scales, "a_scales", m * (k // SP_MX4_GROUP), _BYTES), M,
+        _typed(w_codes, "w_codes", n * k // 2, _BYTES), _typed(w_scales, "w_scales", n * (k // SP_MX4_GROUP), _BYTES), N, K, to, dtype,
+        stride or out_stride or N, _stream(stream))
     if status:
         _check(status)

@@ -25,7 +25,7 @@ FLAGS = [
 NO_NANS = ["-Xarch_device", "-fno-honor-nans"]
 # ... but for what may meet them and has to let them through: the cache stores what it is given, and attention makes
 # a row NaN that sees one. With the flag a NaN there would mean nothing to the compiler.
-HONOUR_NANS = {"sp_cache.hip", "sp_attend.hip"}
+HONOUR_NANS = {"sp_cache.hip", "sp_attend.hip", "sp_weights.hip", "sp_evict.hip", "sp_mx4.hip"}
 
 
 def sources():

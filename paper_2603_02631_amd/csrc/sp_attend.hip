@@ -18,16 +18,9 @@
 // are laid end to end, and workgroup i of N takes the i-th of N equal stretches. A line that lies in one stretch is finished there;
 // of others every stretch leaves a partial result (reference, sum, unscaled output), at most two a workgroup, which a second
 // launch joins. Nothing is added atomically: the order of every sum is fixed by the lengths.
-#include "sp_cache.hpp"
+#include "sp_context.hpp"
 
 namespace {
-
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(2))) float f32x2;
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
@@ -35,29 +28,12 @@ constexpr int kWaves = kThreads / 64;
 // 20000 tokens take 38 us there and 35 in the other kernel (head_dim 64, four of 30000 to 64000: 60 and 125).
 constexpr int few_rows_of(int d) { return d == 128 ? 32 : 64; }
 constexpr int kManyList = 64;
-constexpr int kBlock = sp::kCacheBlock;
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// A block's key scale goes into its logits' factor, its value scale into the exponent (and out of the sum again): no operation for an element.
-// The factor stays above zero, so that masked logits stay minus infinity, and finite, so that a product of zero stays a logit of zero; the value scale
-// above 2^-64, so that exponents keep their range.
-constexpr float kLeastScale = 5.42101086e-20f, kLeastFactor = 1.17549435e-38f, kMostFactor = 3.40282347e38f;
-constexpr float kMostScale = 2.3e38f;      // of a call: times log2(e) it is finite
 
-struct AttendArgs {
-    sp::CacheView c;
-    const uint16_t *q;
-    const int64_t *off;
-    const int32_t *lens;
-    const uint8_t *k_pool, *v_pool;
-    const float *k_scale, *v_scale;
+struct AttendArgs : ContextArgs {
     uint16_t *out;
     float *lse;
-    int32_t max_len, window;            // a window is shorter than max_len, or 0
-    int32_t B, causal;
-    float scale;
-    int32_t page_blocks, page_shift;    // blocks of 32 tokens in a page; their logarithm, or -1
     // sp_attend_few_kernel: workgroups that share the work (0: one for each request and kv head), rows of a partial result
     int32_t few_shares, few_rows, few_least;    // the last: blocks of a share
     f32x2 *few_ml;                      // [2 few_shares][few_rows]: reference (in units of log 2), sum
@@ -76,22 +52,6 @@ struct ManyList {
     int32_t count, b[kManyList], tile[kManyList];
 };
 
-__device__ __forceinline__ float neg_inf() { return -__builtin_huge_valf(); }
-__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
-// NaN if one of them is. One operation, as are two that are nested; fmaxf would take one more for each operand that may be a signalling NaN: this
-// file is compiled with NaNs honoured, since a row that sees one has to become NaN.
-__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
-__device__ __forceinline__ float factor_of(float scale, float key_scale)
-{
-    return __builtin_elementwise_minimum(larger(scale * key_scale, kLeastFactor), kMostFactor);
-}
-__device__ __forceinline__ uint32_t pack2(float a, float b)
-{
-    const bf16x2 r = {(__bf16)a, (__bf16)b};
-    return __builtin_bit_cast(uint32_t, r);
-}
-
 // What a row's result is multiplied by, and its logarithm of the denominator (m in units of log 2). A row that saw no key has a sum of exactly
 // zero; that of a row that saw a NaN is NaN and gets out.
 __device__ __forceinline__ bool saw_nothing(float l) { return l == 0.f; }
@@ -99,230 +59,6 @@ __device__ __forceinline__ float inverse(float l) { return saw_nothing(l) ? 0.f 
 __device__ __forceinline__ float lse_of(float m, float l) { return saw_nothing(l) ? neg_inf() : (m + log2_(l)) * kLn2; }
 
 // ---- a few rows: single tokens, lookahead rows -----------------------------------------------------------------------
-
-// What a request's rows see: row r (token r / G) keys [first(r), last(r)), all rows together [lo, hi). Key indices fit 32 bits:
-// contexts are limited to 2^30 tokens, queries to 2^26.
-struct Range {
-    int len, n, lo, hi;
-};
-
-__device__ __forceinline__ Range range_of(const AttendArgs &a, int b)
-{
-    Range g;
-    g.n = (int)(a.off[b + 1] - a.off[b]);
-    g.len = a.lens[b];
-    g.len = g.len < 0 ? 0 : (g.len > a.max_len ? a.max_len : g.len);
-    g.lo = 0;
-    g.hi = g.len;
-    if (a.causal && a.window > 0) {
-        const int64_t f = (int64_t)g.len - g.n - a.window + 1;
-        g.lo = f > 0 ? (int)f : 0;
-    }
-    return g;
-}
-
-__device__ __forceinline__ uint32_t page_of_block(const AttendArgs &a, uint32_t blk)
-{
-    return a.page_shift >= 0 ? blk >> a.page_shift : blk / (uint32_t)a.page_blocks;
-}
-
-// An entry of request b's row of the block table.
-__device__ __forceinline__ int page_entry(const AttendArgs &a, int b, uint32_t i)
-{
-    int page = a.c.table[b * a.c.table_stride + i];
-    page = page < 0 ? 0 : page;                                     // never outside the pools
-    return page >= (int)a.c.n_pages ? (int)a.c.n_pages - 1 : page;
-}
-
-// Two E4M3 codes of a word (the lower or the upper two) as bf16, exactly.
-template <bool UPPER>
-__device__ __forceinline__ uint32_t widen2(uint32_t w)
-{
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.f, UPPER));
-}
-
-__device__ __forceinline__ bf16x8 widen8(uint32_t c0, uint32_t c1)
-{
-    return __builtin_bit_cast(bf16x8, u32x4{widen2<false>(c0), widen2<true>(c0), widen2<false>(c1), widen2<true>(c1)});
-}
-
-// Four codes each of two keys: element i's pair of them as bf16.
-__device__ __forceinline__ void widen_pairs(uint32_t x, uint32_t y, uint32_t (&pair)[4])
-{
-    const uint32_t lo = __builtin_amdgcn_perm(y, x, 0x05010400u), hi = __builtin_amdgcn_perm(y, x, 0x07030602u);
-    pair[0] = widen2<false>(lo);
-    pair[1] = widen2<true>(lo);
-    pair[2] = widen2<false>(hi);
-    pair[3] = widen2<true>(hi);
-}
-
-// A scalar address that moves, and loads at a lane's 32-bit offset from it: a load takes both as they are. What the compiler does not know to stay
-// the same in a loop (asm) it does not add up beforehand, which would cost two vector operations for each load.
-struct Moving {
-    uint64_t p;
-
-    Moving() = default;
-
-    __device__ __forceinline__ explicit Moving(const uint8_t *at) : p(reinterpret_cast<uint64_t>(at)) { asm("" : "+s"(p)); }
-
-    __device__ __forceinline__ void advance(int64_t bytes)
-    {
-        p += (uint64_t)bytes;
-        asm("" : "+s"(p));
-    }
-
-    template <class T, bool STREAM = false>
-    __device__ __forceinline__ T load(uint32_t lane) const
-    {
-        typedef const __attribute__((address_space(1))) uint8_t *Bytes;
-        const auto *x = reinterpret_cast<const __attribute__((address_space(1))) T *>(reinterpret_cast<Bytes>(p) + lane);
-        if constexpr (STREAM) return __builtin_nontemporal_load(x);
-        else return *x;
-    }
-};
-
-__device__ __forceinline__ uint32_t opaque(uint32_t lane)
-{
-    asm volatile("" : "+v"(lane));
-    return lane;
-}
-
-// A request's cache of one kv head, and where a block of it lies: bytes from k and v, floats from ks and vs.
-struct Line {
-    const uint8_t *k, *v;
-    const float *ks, *vs;
-    int64_t page_bytes;
-    uint32_t row_bytes, page_scales;
-
-    const int32_t *table;
-
-    __device__ __forceinline__ Line(const AttendArgs &a, int b, int kvh, int es)
-    {
-        table = a.c.table + b * a.c.table_stride;
-        k = a.k_pool + kvh * a.c.stride_head * es;
-        v = a.v_pool + kvh * a.c.stride_head * es;
-        ks = a.k_scale + (int64_t)kvh * a.page_blocks;
-        vs = a.v_scale + (int64_t)kvh * a.page_blocks;
-        page_bytes = a.c.page_stride * es;
-        row_bytes = (uint32_t)a.c.stride_token * es;
-        page_scales = (uint32_t)a.c.n_kv_heads * (uint32_t)a.page_blocks;
-    }
-};
-
-struct Place {
-    int64_t off, scale;
-};
-
-// Block blk of request b as the block table has it: requested here, looked at in place(), as scalars, so that loads take a scalar base.
-struct Entry {
-    int page;
-    uint32_t in_page;
-
-    __device__ __forceinline__ Entry(const AttendArgs &a, const Line &l, int blk)
-    {
-        const uint32_t i = page_of_block(a, (uint32_t)blk);
-        page = l.table[i];
-        in_page = (uint32_t)blk - i * (uint32_t)a.page_blocks;
-    }
-
-    __device__ __forceinline__ Place place(const AttendArgs &a, const Line &l) const
-    {
-        const int p = min(max(__builtin_amdgcn_readfirstlane(page), 0), (int)a.c.n_pages - 1);      // never outside the pools
-        return {p * l.page_bytes + (int64_t)((uint64_t)in_page * (kBlock * l.row_bytes)), (int64_t)((uint64_t)(uint32_t)p * l.page_scales) + in_page};
-    }
-};
-
-// One block of 32 tokens as a wave loads it, straight into the registers that the matrix instructions take it from.
-// Lane l = 16 g + c. Keys: row c of 16-key tile t, the contraction's elements in an order that makes a lane's share of a row contiguous
-// (queries are loaded in the same order). Values: elements [c D/16, (c+1) D/16) of the eight keys 4g + j and 16 + 4g + j, j < 4: the
-// keys whose logits the lane holds after the first product.
-// Loads that take whole lines of 128 bytes pass the caches by: values, unless their rows have 64 bytes, and keys whose rows do. 32 requests of bf16, head_dim
-// 128, 172 us without and 160 with; 48 of E4M3, head_dim 64, 157 and 143 (200 of up to 4000 tokens 52 and 49, but 56 with values too). The latter only
-// for contexts that no cache would hold until the next call: 64 of up to 2000 tokens, called again and again, take 15.7 us without and 18.7 with.
-template <int D, bool E4M3, bool STREAM>
-struct Block {
-    static constexpr int kLoads = E4M3 ? D / 64 : D / 32;           // 16-byte loads of a key's row share; dwords of a value's
-    u32x4 k[2][kLoads];
-    uint32_t v[8][kLoads];
-    float ks, vs;
-
-    __device__ __forceinline__ void load_keys(const Line &l, const Place &at, uint32_t lane)
-    {
-        lane = opaque(lane);
-        Moving p(l.k + at.off);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) k[t][i] = p.load<u32x4, STREAM && kLoads == 1>(lane + 64 * i);
-            p.advance(16 * (int64_t)l.row_bytes);
-        }
-        ks = 1.f;
-        if (E4M3) ks = l.ks[at.scale];
-    }
-
-    __device__ __forceinline__ void load_values(const Line &l, const Place &at, uint32_t lane)
-    {
-        lane = opaque(lane);
-        Moving p(l.v + at.off);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if constexpr (kLoads == 1) v[j][0] = p.load<uint32_t>(lane);
-            else if constexpr (kLoads == 2) {
-                const u32x2 w = p.load<u32x2, true>(lane);
-                v[j][0] = w[0];
-                v[j][1] = w[1];
-            } else {
-                const u32x4 w = p.load<u32x4, true>(lane);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[j][i] = w[i];
-            }
-            p.advance((j == 3 ? 13 : 1) * (int64_t)l.row_bytes);
-        }
-        vs = 1.f;
-        if (E4M3) vs = l.vs[at.scale];
-    }
-
-    // Elements of step s of tile t's rows.
-    __device__ __forceinline__ bf16x8 key(int t, int s) const
-    {
-        if (E4M3) return widen8(k[t][s / 2][2 * (s % 2)], k[t][s / 2][2 * (s % 2) + 1]);
-        return __builtin_bit_cast(bf16x8, k[t][s]);
-    }
-
-    // Element c D/16 + i of the lane's eight keys.
-    __device__ __forceinline__ void values(bf16x8 (&f)[D / 16]) const
-    {
-        u32x4 r[D / 16];
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {                           // keys 2p and 2p + 1
-                if (E4M3) {
-                    uint32_t pair[4];
-                    widen_pairs(v[2 * p][i], v[2 * p + 1][i], pair);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) r[4 * i + e][p] = pair[e];
-                } else {
-                    r[2 * i][p] = __builtin_amdgcn_perm(v[2 * p + 1][i], v[2 * p][i], 0x05040100u);
-                    r[2 * i + 1][p] = __builtin_amdgcn_perm(v[2 * p + 1][i], v[2 * p][i], 0x07060302u);
-                }
-            }
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) f[i] = __builtin_bit_cast(bf16x8, r[i]);
-    }
-
-    // Values of tokens outside [lo, hi) may be NaN: they become zero.
-    __device__ __forceinline__ void clear_values(int g, int first, int lo, int hi)
-    {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int key = first + 4 * g + (j & 3) + (j >> 2) * 16;
-            if (key < lo || key >= hi)
-#pragma unroll
-                for (int i = 0; i < kLoads; ++i) v[j][i] = 0;
-        }
-    }
-};
 
 // Maximum over the four lanes that hold a query row's logits.
 __device__ __forceinline__ float row_max(float x)
@@ -486,9 +222,11 @@ __device__ __forceinline__ int few_blocks(const AttendArgs &a, int b)
 // over 131072, 36 us, 3.7 TB/s. Four waves take every fourth block of 32 tokens of a stretch; a wave holds its rows' statistics and output by itself
 // and loads a block ahead, the four meet in LDS at the end. Blocks [k0, k1) of request b and kv head kvh; `slot` of the partial results, or -1 if
 // that is all of them.
-template <int D, bool E4M3, int MT, bool STREAM>
+template <int D, int KIND, int MT, bool STREAM>
 __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh, int k0, int k1, int slot)
 {
+    using B = Block<D, KIND, STREAM>;
+    constexpr bool E4M3 = KIND == SP_CACHE_E4M3, MX4 = KIND == SP_CACHE_MX4;
     constexpr int kSteps = D / 32, kTiles = D / 16;
     __shared__ float merge_o[2][16 * MT][D + 4];       // padded: sixteen rows are written side by side
     __shared__ f32x2 merge_ml[2][16 * MT];
@@ -508,7 +246,7 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
         const uint16_t *src = a.q + ((a.off[b] + token) * a.c.n_q_heads + head) * D;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-            const int e = E4M3 ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;
+            const int e = MX4 ? D / 4 * g + 8 * s : E4M3 ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;
             u32x4 w = {0, 0, 0, 0};
             if (r < rows) w = *reinterpret_cast<const u32x4 *>(src + e);
             q[t][s] = __builtin_bit_cast(bf16x8, w);
@@ -520,19 +258,29 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
 
     Rows<D, MT> acc;
     acc.clear();
-    const Line line(a, b, kvh, E4M3 ? 1 : 2);
-    const uint32_t k_lane = c * line.row_bytes + 16 * g, v_lane = 4 * g * line.row_bytes + c * (D / 16) * (E4M3 ? 1 : 2);
+    const Line line(a, b, kvh, KIND, D);
+    const uint32_t k_lane = MX4 ? 2 * c * line.row_bytes + D / 8 * g : c * line.row_bytes + 16 * g;
+    const uint32_t v_lane = (MX4 ? 8 : 4) * g * line.row_bytes + (uint32_t)sp::cache_bytes(KIND, c * (D / 16));
+    const uint32_t ks_lane = c * (D / 16), vs_lane = g * (D / 4);           // of MX4 scales: two keys, eight keys
+    const auto load_keys = [&](B &kv, const Place &at) {
+        if constexpr (MX4) kv.load_keys(line, at, k_lane, ks_lane);
+        else kv.load_keys(line, at, k_lane);
+    };
+    const auto load_values = [&](B &kv, const Place &at) {
+        if constexpr (MX4) kv.load_values(line, at, v_lane, vs_lane);
+        else kv.load_values(line, at, v_lane);
+    };
     // The next block's keys are loaded once this one's are in the first product, its values once these are in operand form. Block table entries
     // are requested two blocks ahead.
-    Block<D, E4M3, STREAM> kv;
+    B kv;
     int blk = from + wave;
     if (blk < to) {
         const int end = blk + (to - 1 - blk) / kWaves * kWaves;         // this wave's last block, loaded again behind it
         const Entry now(a, line, blk);
         Entry soon(a, line, min(blk + kWaves, end));
         const Place here = now.place(a, line);
-        kv.load_keys(line, here, k_lane);
-        kv.load_values(line, here, v_lane);
+        load_keys(kv, here);
+        load_values(kv, here);
         for (;;) {
             const int key0 = blk * kBlock;
             const Entry later(a, line, min(blk + 2 * kWaves, end));
@@ -543,7 +291,10 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int s = 0; s < kSteps; ++s) kf[t][s] = kv.key(t, s);
+                    for (int s = 0; s < kSteps; ++s) {
+                        if constexpr (MX4) kf[t][s] = kv.key(t, s, g);
+                        else kf[t][s] = kv.key(t, s);
+                    }
 #pragma unroll
                 for (int t = 0; t < MT; ++t) {
                     s0[t] = s1[t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -556,30 +307,31 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
             }
             const Place there = soon.place(a, line);
             float factor = scale2, vexp = 0.f, vinv = 1.f;
-            if (E4M3) {
+            if constexpr (E4M3) {
                 const float vs = larger(kv.vs, kLeastScale);
                 factor = factor_of(scale2, kv.ks);
                 vexp = log2_(vs);
                 vinv = __builtin_amdgcn_rcpf(vs);
             }
-            kv.load_keys(line, there, k_lane);
+            load_keys(kv, there);
             bf16x8 vf[kTiles];
             if (!whole) kv.clear_values(g, key0, rg.lo, rg.hi);
-            kv.values(vf);
-            kv.load_values(line, there, v_lane);
+            if constexpr (MX4) kv.values(vf, c);
+            else kv.values(vf);
+            load_values(kv, there);
             soon = later;
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
                 float x[8];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    x[j] = s0[t][j];
-                    x[4 + j] = s1[t][j];
+                    x[MX4 ? 2 * j : j] = s0[t][j];
+                    x[MX4 ? 2 * j + 1 : 4 + j] = s1[t][j];
                 }
                 if (!whole)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const int key = key0 + 4 * g + (j & 3) + (j >> 2) * 16;
+                        const int key = key0 + B::key_of(g, j);
                         if (key >= last[t] || (a.window > 0 && key < last[t] - a.window)) x[j] = neg_inf();
                     }
                 const bf16x8 p = acc.weigh(t, x, factor, vexp, vinv);
@@ -649,7 +401,7 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
     }
 }
 
-template <int D, bool E4M3, int MT, bool SHARED, bool STREAM>
+template <int D, int KIND, int MT, bool SHARED, bool STREAM>
 __global__ __launch_bounds__(kThreads, D == 128 && MT > 1 ? 1 : 2) void sp_attend_few_kernel(AttendArgs a)
 {
     const int kv = a.c.n_kv_heads, share = blockIdx.x;
@@ -676,7 +428,7 @@ __global__ __launch_bounds__(kThreads, D == 128 && MT > 1 ? 1 : 2) void sp_atten
             continue;
         }
         const int rel = (int)(pos - begin), kvh = rel / n, k0 = rel % n, k1 = (int)min((int64_t)n, k0 + (end - pos));
-        few_stretch<D, E4M3, MT, STREAM>(a, b, kvh, k0, k1, k0 == 0 && k1 == n ? -1 : 2 * share + (part > 0));
+        few_stretch<D, KIND, MT, STREAM>(a, b, kvh, k0, k1, k0 == 0 && k1 == n ? -1 : 2 * share + (part > 0));
         pos += k1 - k0;
         __syncthreads();                    // the merge's LDS is used again
     }
@@ -819,8 +571,9 @@ __device__ __forceinline__ bool tile_of(const AttendArgs &a, const ManyList &lis
 // transposed, so that both products take 16-byte operands from LDS. The transposed logits put a row into a lane column; the order of keys in a row of
 // transposed values is the one in which a lane holds its probabilities, so these are the second product's operand as they are. Tiles are
 // double-buffered, one barrier a tile; the next tile's loads are under way during the products.
-template <int D, bool E4M3>
+template <int D, int KIND>
 struct Stage {
+    static constexpr bool E4M3 = KIND == SP_CACHE_E4M3;
     static constexpr int kKeys = 8192 / D, kBlocks = kKeys / kBlock;
     static constexpr int ES = E4M3 ? 1 : 2;
     static constexpr int kKeyLoads = E4M3 ? 1 : 2;              // 16-byte loads of a thread
@@ -866,10 +619,12 @@ struct Stage {
     }
 
     // The address of the cursor's block; moves it to the next tile's.
-    __device__ __forceinline__ static Moving next(const AttendArgs &a, const Line &l, const uint8_t *pool, uint32_t last_page, Cursor &c)
+    __device__ __forceinline__ static Moving next(const AttendArgs &a, const Line &l, const uint8_t *pool, uint32_t last_page, Cursor &c,
+                                                  uint64_t *scale = nullptr)
     {
         const int p = min(max(__builtin_amdgcn_readfirstlane(c.entry), 0), (int)a.c.n_pages - 1);       // never outside the pools
         const Moving at(pool + p * l.page_bytes + (int64_t)((uint64_t)c.in * (kBlock * l.row_bytes)));
+        if (scale) *scale = (uint64_t)(uint32_t)p * l.page_scales + c.in;
         c.in += kBlocks;
         if (c.in >= (uint32_t)a.page_blocks) {
             do {
@@ -893,7 +648,7 @@ struct Stage {
 
     __device__ __forceinline__ static const float *scale_place(const AttendArgs &a, int b, int kvh, const Cursors &c)
     {
-        const float *scales = threadIdx.x < kBlocks ? a.k_scale : a.v_scale;
+        const float *scales = static_cast<const float *>(threadIdx.x < kBlocks ? a.k_scale : a.v_scale);
         return scales + ((int64_t)page_entry(a, b, c.scale_page) * a.c.n_kv_heads + kvh) * a.page_blocks + c.scale_in;
     }
 
@@ -994,6 +749,83 @@ struct Stage {
     }
 };
 
+// The same for an MX4 cache: a thread has 16 codes of a key, half a group, and the same four elements of four keys.
+template <int D>
+struct Stage<D, SP_CACHE_MX4> : Stage<D, SP_CACHE_E4M3> {
+    using Base = Stage<D, SP_CACHE_E4M3>;
+    static constexpr int kKeys = Base::kKeys, kBlocks = Base::kBlocks;
+    static constexpr int kScaleWords = D / 64;                  // dwords of two keys' scales
+    struct Raw {
+        u32x2 k;
+        uint32_t ks;
+        uint32_t v[4];
+        uint32_t vs[2 * kScaleWords];
+    };
+    struct Cursors {
+        typename Base::Cursor key, value;
+    };
+
+    __device__ __forceinline__ Cursors cursors(const AttendArgs &a, const Line &l, int, int, uint32_t blk, uint32_t last_page) const
+    {
+        Cursors c;
+        c.key = Base::cursor(a, l.table, blk + __builtin_amdgcn_readfirstlane(this->key_row / kBlock), last_page);
+        c.value = Base::cursor(a, l.table, blk + __builtin_amdgcn_readfirstlane(this->value_octet >> 2), last_page);
+        return c;
+    }
+
+    __device__ __forceinline__ void load(const AttendArgs &a, const Line &l, int, int, uint32_t last_page, Cursors &c, Raw &w) const
+    {
+        uint64_t ks, vs;
+        const Moving k = Base::next(a, l, l.k, last_page, c.key, &ks);
+        Moving v = Base::next(a, l, l.v, last_page, c.value, &vs);
+        const Moving ksp(l.ks4 + ks * D), vsp(l.vs4 + vs * D);
+        const uint32_t key = this->key_row % kBlock, val = this->value_key % kBlock;
+        w.k = k.template load<u32x2>(opaque(key * l.row_bytes + this->key_col * 8));
+        w.ks = ksp.template load<uint8_t>(opaque(key * (D / 32) + this->key_col / 2));
+        const uint32_t lane = opaque(val * l.row_bytes + this->value_col * 2);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            w.v[j] = v.template load<uint16_t>(lane);
+            v.advance(l.row_bytes);
+        }
+        const uint32_t at = opaque(val * (D / 32));
+        if constexpr (D == 64) {
+            const u32x2 s = vsp.template load<u32x2>(at);
+            w.vs[0] = s[0];
+            w.vs[1] = s[1];
+        } else {
+            const u32x4 s = vsp.template load<u32x4>(at);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w.vs[j % (2 * kScaleWords)] = s[j];
+        }
+    }
+
+    __device__ __forceinline__ void store(Raw &w, u32x4 *keys, u32x4 *values, float *, int first, int lo, int hi) const
+    {
+        const int r = this->key_row;
+        const float s = __uint_as_float(w.ks << 23);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            keys[Base::key_slot(r, 2 * this->key_col + i)] = u32x4{widen4<0>(w.k[i], s), widen4<1>(w.k[i], s), widen4<2>(w.k[i], s), widen4<3>(w.k[i], s)};
+        const int group = this->value_col * 4 / sp::kMx4Group;
+        uint32_t x[4][2];                                       // four elements of four keys
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float vs = D == 64 ? exponent_of(w.vs[j / 2], turn_of(group + 2 * (j & 1))) : exponent_of(w.vs[j % (2 * kScaleWords)], turn_of(group));
+            const int key = first + this->value_key + j;
+            if (key < lo || key >= hi) vs = 0.f;                // whose scale may say NaN
+            x[j][0] = widen4<0>(w.v[j], vs);
+            x[j][1] = widen4<1>(w.v[j], vs);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t pick = i & 1 ? 0x07060302u : 0x05040100u;
+            reinterpret_cast<u32x2 *>(values)[2 * Base::value_slot(4 * this->value_col + i, this->value_octet) + this->value_half] =
+                u32x2{__builtin_amdgcn_perm(x[1][i / 2], x[0][i / 2], pick), __builtin_amdgcn_perm(x[3][i / 2], x[2][i / 2], pick)};
+        }
+    }
+};
+
 // Tiles of keys that a tile of rows sees; one for a tile that sees nothing, whose rows are still written.
 template <int D>
 __device__ __forceinline__ int many_units(const Tile &t)
@@ -1004,10 +836,11 @@ __device__ __forceinline__ int many_units(const Tile &t)
 }
 
 // Tiles [k0, k1) of the keys that tile t of query rows sees; `slot` of the partial results, or -1 if that is all of them.
-template <int D, bool E4M3>
+template <int D, int KIND>
 __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t, int kvh, int k0, int k1, int slot)
 {
-    using S = Stage<D, E4M3>;
+    using S = Stage<D, KIND>;
+    constexpr bool E4M3 = KIND == SP_CACHE_E4M3;
     constexpr int kKeys = S::kKeys, kBlocks = S::kBlocks, kSteps = D / 16, kOut = D / 32;
     constexpr float kSlack = 8.f;
     constexpr int kVectorOnly = 0x406;      // what may cross a scheduling barrier: vector, scalar and transcendental operations
@@ -1056,7 +889,7 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
         const uint32_t last_page = page_of_block(a, last_blk);
         const int last_tile = (to - from + kKeys - 1) / kKeys - 1;
         typename S::Raw ra, rb;
-        const Line line(a, t.b, kvh, S::ES);
+        const Line line(a, t.b, kvh, KIND, D);
         typename S::Cursors cur = st.cursors(a, line, t.b, kvh, (uint32_t)(from / kBlock), last_page);
         st.load(a, line, t.b, kvh, last_page, cur, ra);
         st.load(a, line, t.b, kvh, last_page, cur, rb);
@@ -1198,7 +1031,7 @@ __device__ __forceinline__ void many_stretch(const AttendArgs &a, const Tile &t,
     if (a.lse && h == 0) a.lse[row] = lse_of(m, l);
 }
 
-template <int D, bool E4M3, bool SHARED>
+template <int D, int KIND, bool SHARED>
 __global__ __launch_bounds__(kManyThreads) void sp_attend_many_kernel(AttendArgs a, ManyList list)
 {
     const int kv = a.c.n_kv_heads;
@@ -1206,7 +1039,7 @@ __global__ __launch_bounds__(kManyThreads) void sp_attend_many_kernel(AttendArgs
     if constexpr (!SHARED) {
         // A line each. Neighbouring workgroups take different kv heads: with eight of them, each die's L2 holds one head's cache. Later
         // tiles of a prompt see more: they go first
-        if (tile_of(a, list, few_rows_of(D), a.tiles - 1 - blockIdx.x / kv, &t)) many_stretch<D, E4M3>(a, t, blockIdx.x % kv, 0, many_units<D>(t), -1);
+        if (tile_of(a, list, few_rows_of(D), a.tiles - 1 - blockIdx.x / kv, &t)) many_stretch<D, KIND>(a, t, blockIdx.x % kv, 0, many_units<D>(t), -1);
     } else {
         // stretches of one kv head lie on one die, as far as they divide
         const int per_die = a.many_shares / 8, x = blockIdx.x;
@@ -1235,7 +1068,7 @@ __global__ __launch_bounds__(kManyThreads) void sp_attend_many_kernel(AttendArgs
                 continue;
             }
             const int k0 = (int)(rel - begin), k1 = (int)min((int64_t)n, k0 + (end - pos));
-            many_stretch<D, E4M3>(a, t, kvh, k0, k1, k0 == 0 && k1 == n ? -1 : 2 * share + (part > 0));
+            many_stretch<D, KIND>(a, t, kvh, k0, k1, k0 == 0 && k1 == n ? -1 : 2 * share + (part > 0));
             pos += k1 - k0;
         }
     }
@@ -1270,7 +1103,6 @@ struct Plan {
     size_t few_o, few_before, many_ml, many_o, many_before, bytes;      // where the workspace's parts begin (few_ml at 0)
 };
 
-constexpr int64_t kMaxLen = int64_t(1) << 30, kMaxTokens = int64_t(1) << 26;     // key indices and rows fit 32 bits
 constexpr int64_t kUnits = 256;         // compute units
 constexpr int64_t kStream = int64_t(1) << 28;                   // bytes that the last cache before memory holds
 constexpr int64_t kMaxGroups = int64_t(1) << 23;                // a launch's threads fit 32 bits
@@ -1321,7 +1153,7 @@ sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64
     const int64_t spread = kUnits * ((D == 64 ? (p->few_rows == 16 ? 4 : p->few_rows == 32 ? 3 : 2) : p->few_rows == 16 ? 2 : 1) - (fill || (D == 128 && p->few_rows > 16) ? 0 : 1));
     // Joining takes longer with more parts of a line, its stretches with fewer: the best size grows with the root of the length (one context of 3000
     // tokens: at least 4 or 16 blocks 11.7 and 13.4 us; of 32768: 4 or 16 blocks 18.2 and 15.1).
-    p->stream = 2 * max_len * B * kv * D * (sp::cache_is_e4m3(*d) ? 1 : 2) > kStream;
+    p->stream = 2 * sp::cache_bytes(d->cache_type, max_len * B * kv * D) > kStream;
     p->few_least = 4;
     while (8 * p->few_least * p->few_least < blocks) p->few_least *= 2;
     const auto shares_of = [&](int64_t n, int64_t least) {
@@ -1352,30 +1184,30 @@ sp_status make_plan(const sp_cache_desc *d, const int64_t *off, int32_t B, int64
     return SP_OK;
 }
 
-template <int D, bool E4M3, int MT, bool STREAM>
+template <int D, int KIND, int MT, bool STREAM>
 void few_of(const AttendArgs &a, dim3 grid, hipStream_t st)
 {
-    if (a.few_shares) hipLaunchKernelGGL((sp_attend_few_kernel<D, E4M3, MT, true, STREAM>), grid, dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL((sp_attend_few_kernel<D, E4M3, MT, false, STREAM>), grid, dim3(kThreads), 0, st, a);
+    if (a.few_shares) hipLaunchKernelGGL((sp_attend_few_kernel<D, KIND, MT, true, STREAM>), grid, dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL((sp_attend_few_kernel<D, KIND, MT, false, STREAM>), grid, dim3(kThreads), 0, st, a);
 }
 
-template <int D, bool E4M3, int MT>
+template <int D, int KIND, int MT>
 void few(const AttendArgs &a, bool stream, dim3 grid, hipStream_t st)
 {
-    if constexpr (D == 64 && E4M3)              // keys of 64 bytes: as they stand the only loads that the answer changes
-        if (stream) return few_of<D, E4M3, MT, true>(a, grid, st);
-    few_of<D, E4M3, MT, false>(a, grid, st);
+    if constexpr (D == 64 && KIND == SP_CACHE_E4M3)     // keys of 64 bytes: as they stand the only loads that the answer changes
+        if (stream) return few_of<D, KIND, MT, true>(a, grid, st);
+    few_of<D, KIND, MT, false>(a, grid, st);
 }
 
-template <int D, bool E4M3>
+template <int D, int KIND>
 sp_status run(const AttendArgs &a, const Plan &p, hipStream_t st)
 {
     const unsigned kv = (unsigned)a.c.n_kv_heads;
     if (p.few) {
         const dim3 grid(p.few_shares ? (unsigned)p.few_shares : (unsigned)a.B * kv);
-        if (p.few_rows == 16) few<D, E4M3, 1>(a, p.stream, grid, st);
-        else if (p.few_rows == 32) few<D, E4M3, 2>(a, p.stream, grid, st);
-        else if constexpr (few_rows_of(D) > 32) few<D, E4M3, 4>(a, p.stream, grid, st);
+        if (p.few_rows == 16) few<D, KIND, 1>(a, p.stream, grid, st);
+        else if (p.few_rows == 32) few<D, KIND, 2>(a, p.stream, grid, st);
+        else if constexpr (few_rows_of(D) > 32) few<D, KIND, 4>(a, p.stream, grid, st);
         SP_HIP_CHECK(hipGetLastError());
         if (p.few_shares) {
             // four waves a row where a line has many parts
@@ -1388,8 +1220,8 @@ sp_status run(const AttendArgs &a, const Plan &p, hipStream_t st)
     }
     if (p.many) {
         const dim3 grid(p.many_shares ? (unsigned)p.many_shares : (unsigned)p.tiles * kv);
-        if (p.many_shares) hipLaunchKernelGGL((sp_attend_many_kernel<D, E4M3, true>), grid, dim3(kManyThreads), 0, st, a, p.list);
-        else hipLaunchKernelGGL((sp_attend_many_kernel<D, E4M3, false>), grid, dim3(kManyThreads), 0, st, a, p.list);
+        if (p.many_shares) hipLaunchKernelGGL((sp_attend_many_kernel<D, KIND, true>), grid, dim3(kManyThreads), 0, st, a, p.list);
+        else hipLaunchKernelGGL((sp_attend_many_kernel<D, KIND, false>), grid, dim3(kManyThreads), 0, st, a, p.list);
         SP_HIP_CHECK(hipGetLastError());
         if (p.many_shares) {
             const bool parts = p.many_shares > 8 * p.tiles * (int64_t)kv;
@@ -1400,6 +1232,13 @@ sp_status run(const AttendArgs &a, const Plan &p, hipStream_t st)
         }
     }
     return SP_OK;
+}
+
+template <int D>
+sp_status run_kind(const AttendArgs &a, int kind, const Plan &p, hipStream_t st)
+{
+    if (kind == SP_CACHE_MX4) return run<D, SP_CACHE_MX4>(a, p, st);
+    return kind == SP_CACHE_E4M3 ? run<D, SP_CACHE_E4M3>(a, p, st) : run<D, SP_CACHE_BF16>(a, p, st);
 }
 
 }  // namespace
@@ -1417,21 +1256,13 @@ extern "C" sp_status sp_attend_workspace(const sp_cache_desc *desc, const int64_
 extern "C" sp_status sp_attend(const sp_cache_desc *desc, const void *q_dev, const int64_t *offsets_host,
                                const int64_t *offsets_dev, int32_t B, const int32_t *lens_dev, int64_t max_len,
                                const int32_t *block_table_dev, int64_t table_stride, const void *k_pool_dev,
-                               const void *v_pool_dev, const float *k_scale_dev, const float *v_scale_dev, float scale,
+                               const void *v_pool_dev, const void *k_scale_dev, const void *v_scale_dev, float scale,
                                int32_t causal, int64_t window, void *out_dev, float *lse_dev, void *ws_dev,
                                size_t ws_bytes, void *hip_stream)
 {
     Plan p;
     if (sp_status rc = make_plan(desc, offsets_host, B, max_len, &p)) return rc;
-    if (!(scale > 0.f) || scale > kMostScale) return sp::fail(SP_ERR_INVALID_ARG, "scale = %g must be > 0 and at most 2.3e38", (double)scale);
-    if (causal != 0 && causal != 1) return sp::fail(SP_ERR_INVALID_ARG, "causal = %d is neither 0 nor 1", causal);
-    if (window < 0 || (window > 0 && !causal))
-        return sp::fail(SP_ERR_INVALID_ARG, "window = %lld must be 0, or positive with causal = 1", (long long)window);
-    if (table_stride < 1 || table_stride > (int64_t(1) << 31))
-        return sp::fail(SP_ERR_INVALID_ARG, "table_stride = %lld outside 1..2^31", (long long)table_stride);
-    if (max_len > table_stride * desc->page_tokens)
-        return sp::fail(SP_ERR_INVALID_ARG, "max_len = %lld exceeds the block table's %lld tokens", (long long)max_len,
-                        (long long)(table_stride * desc->page_tokens));
+    if (sp_status rc = check_masks(desc, max_len, table_stride, scale, causal, window)) return rc;
     if (p.total == 0) return SP_OK;
     if (!q_dev || !out_dev || !offsets_dev || !lens_dev || !block_table_dev)
         return sp::fail(SP_ERR_INVALID_ARG, "only lse_dev, and ws_dev where no workspace is needed, may be null");
@@ -1444,14 +1275,11 @@ extern "C" sp_status sp_attend(const sp_cache_desc *desc, const void *q_dev, con
         if (ws_bytes < p.bytes) return sp::fail(SP_ERR_WORKSPACE, "workspace too small: %zu < %zu", ws_bytes, p.bytes);
     }
 
-    AttendArgs a{sp::view_of(*desc, block_table_dev, table_stride), static_cast<const uint16_t *>(q_dev), offsets_dev,
-                 lens_dev, static_cast<const uint8_t *>(k_pool_dev), static_cast<const uint8_t *>(v_pool_dev),
-                 k_scale_dev, v_scale_dev, static_cast<uint16_t *>(out_dev), lse_dev, (int32_t)max_len,
-                 window < max_len ? (int32_t)window : 0, B, causal, scale};      // a longer window takes no key from a row
-    a.page_blocks = (int32_t)(desc->page_tokens / kBlock);
-    a.page_shift = -1;
-    for (int s = 0; s < 24; ++s)
-        if (a.page_blocks == 1 << s) a.page_shift = s;
+    AttendArgs a{};
+    static_cast<ContextArgs &>(a) = context_args(*desc, q_dev, offsets_dev, lens_dev, max_len, block_table_dev, table_stride, k_pool_dev, v_pool_dev,
+                                                 k_scale_dev, v_scale_dev, scale, causal, window, B);
+    a.out = static_cast<uint16_t *>(out_dev);
+    a.lse = lse_dev;
     a.tiles = p.tiles;
     uint8_t *ws = static_cast<uint8_t *>(ws_dev);
     a.few_shares = p.few_shares;
@@ -1465,7 +1293,5 @@ extern "C" sp_status sp_attend(const sp_cache_desc *desc, const void *q_dev, con
     a.many_o = reinterpret_cast<float *>(ws + p.many_o);
     a.many_before = reinterpret_cast<int64_t *>(ws + p.many_before);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const bool e4m3 = sp::cache_is_e4m3(*desc);
-    if (desc->head_dim == 64) return e4m3 ? run<64, true>(a, p, st) : run<64, false>(a, p, st);
-    return e4m3 ? run<128, true>(a, p, st) : run<128, false>(a, p, st);
+    return desc->head_dim == 64 ? run_kind<64>(a, desc->cache_type, p, st) : run_kind<128>(a, desc->cache_type, p, st);
 }

@@ -16,6 +16,7 @@
 // reaches; a prompt of 8192 tokens (32 heads of 64 over 8, bf16), one round of workgroups, 26 us, 4.0. By a chain of four dependent loads (offsets, block table,
 // inputs, old codes) and the call itself for single tokens: 13 us. With the kv heads of the same tokens far apart in the grid the chunks took 114.
 #include "sp_cache.hpp"
+#include "sp_mx4.hpp"
 
 namespace {
 
@@ -38,7 +39,7 @@ struct AppendArgs {
     const float *cos, *sin;
     int64_t n_pos;
     uint8_t *k_pool, *v_pool;
-    float *k_scale, *v_scale;
+    void *k_scale, *v_scale;
     int32_t B, rot;
     bool single;        // no request brings more than one token: item x belongs to request x
 };
@@ -163,9 +164,10 @@ __device__ __forceinline__ int find_request(const AppendArgs &a, int x, int64_t 
     return lo;
 }
 
-template <int D, bool E4M3, bool PAIRS>
+template <int D, int KIND, bool PAIRS>
 __global__ __launch_bounds__(kThreads) void sp_cache_append_kernel(AppendArgs a)
 {
+    constexpr bool E4M3 = KIND == SP_CACHE_E4M3, MX4 = KIND == SP_CACHE_MX4;
     constexpr int kVecs = D / 16;                       // threads of a token
     constexpr int kParts = kThreads / (kBlock * kVecs); // 2 at head_dim 64: half the threads take keys, half values
     __shared__ uint32_t wave_max[2][kThreads / 64];
@@ -224,7 +226,7 @@ __global__ __launch_bounds__(kThreads) void sp_cache_append_kernel(AppendArgs a)
                 if (!val && ln.turned) rotate<PAIRS>(lo[i], hi[i], c, s);
             }
             if (E4M3) {
-                if (start > slot0) old[i] = val ? a.v_scale[scale_at] : a.k_scale[scale_at];
+                if (start > slot0) old[i] = static_cast<const float *>(val ? a.v_scale : a.k_scale)[scale_at];
                 if (fresh)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -240,6 +242,41 @@ __global__ __launch_bounds__(kThreads) void sp_cache_append_kernel(AppendArgs a)
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
             const bool val = kItems == 2 ? i == 1 : part == 1;
+            if constexpr (MX4) {
+                // A group's largest magnitude: of the octets of a token's neighbouring threads that lie in it.
+                constexpr int kGroups = D / sp::kMx4Group;
+                uint32_t tops[2] = {0, 0};
+                if (fresh)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        tops[0] = max(tops[0], sp::mx4_magnitude(lo[i][e]));
+                        tops[1] = max(tops[1], sp::mx4_magnitude(hi[i][e]));
+                    }
+                const int glo = ln.lo / sp::kMx4Group, ghi = ln.hi / sp::kMx4Group;
+                int blo = 0, bhi = 0;
+                uint32_t bytes = 0;
+#pragma unroll
+                for (int n = 0; n < kGroups; ++n) {
+                    uint32_t top = max(glo == n ? tops[0] : 0u, ghi == n ? tops[1] : 0u);
+#pragma unroll
+                    for (int o = 1; o < kVecs; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+                    const int byte = sp::mx4_scale(top);
+                    if (glo == n) blo = byte;
+                    if (ghi == n) bhi = byte;
+                    bytes |= (uint32_t)byte << (8 * n);
+                }
+                if (fresh) {
+                    uint8_t *dst = (val ? a.v_pool : a.k_pool) + elem / 2;
+                    *reinterpret_cast<uint32_t *>(dst + ln.lo / 2) = sp::mx4_codes(lo[i], blo);
+                    *reinterpret_cast<uint32_t *>(dst + ln.hi / 2) = sp::mx4_codes(hi[i], bhi);
+                    if (vec == 0) {
+                        uint8_t *to = static_cast<uint8_t *>(val ? a.v_scale : a.k_scale) + (scale_at * kBlock + slot) * kGroups;
+                        if constexpr (kGroups == 2) *reinterpret_cast<uint16_t *>(to) = (uint16_t)bytes;
+                        else *reinterpret_cast<uint32_t *>(to) = bytes;
+                    }
+                }
+                continue;
+            }
             if (!E4M3) {
                 if (fresh) {
                     uint16_t *dst = reinterpret_cast<uint16_t *>(val ? a.v_pool : a.k_pool) + elem;
@@ -276,7 +313,7 @@ __global__ __launch_bounds__(kThreads) void sp_cache_append_kernel(AppendArgs a)
                 *lp = rescale(*lp, ratio);
                 *hp = rescale(*hp, ratio);
             }
-            if (slot == 0 && vec == 0) (val ? a.v_scale : a.k_scale)[scale_at] = scale;
+            if (slot == 0 && vec == 0) static_cast<float *>(val ? a.v_scale : a.k_scale)[scale_at] = scale;
         }
     }
 
@@ -294,13 +331,21 @@ __global__ __launch_bounds__(kThreads) void sp_cache_append_kernel(AppendArgs a)
         }
 }
 
-template <int D, bool E4M3>
+template <int D, int KIND>
 void launch(const AppendArgs &a, bool pairs, dim3 grid, hipStream_t st)
 {
     if (pairs)
-        hipLaunchKernelGGL((sp_cache_append_kernel<D, E4M3, true>), grid, dim3(kThreads), 0, st, a);
+        hipLaunchKernelGGL((sp_cache_append_kernel<D, KIND, true>), grid, dim3(kThreads), 0, st, a);
     else
-        hipLaunchKernelGGL((sp_cache_append_kernel<D, E4M3, false>), grid, dim3(kThreads), 0, st, a);
+        hipLaunchKernelGGL((sp_cache_append_kernel<D, KIND, false>), grid, dim3(kThreads), 0, st, a);
+}
+
+template <int D>
+void launch_kind(const AppendArgs &a, int kind, bool pairs, dim3 grid, hipStream_t st)
+{
+    if (kind == SP_CACHE_MX4) launch<D, SP_CACHE_MX4>(a, pairs, grid, st);
+    else if (kind == SP_CACHE_E4M3) launch<D, SP_CACHE_E4M3>(a, pairs, grid, st);
+    else launch<D, SP_CACHE_BF16>(a, pairs, grid, st);
 }
 
 bool bad_stride(int64_t stride, int64_t width) { return stride < width || stride % 8 != 0 || stride > (int64_t(1) << 40); }
@@ -313,7 +358,7 @@ extern "C" sp_status sp_cache_append(const sp_cache_desc *desc, const void *k_de
                                      const int32_t *start_dev, const int32_t *positions_dev,
                                      const int32_t *block_table_dev, int64_t table_stride, const float *cos_dev,
                                      const float *sin_dev, int64_t n_pos, int32_t rot_dim, int32_t rot_style,
-                                     void *k_pool_dev, void *v_pool_dev, float *k_scale_dev, float *v_scale_dev,
+                                     void *k_pool_dev, void *v_pool_dev, void *k_scale_dev, void *v_scale_dev,
                                      void *hip_stream)
 {
     if (sp_status rc = sp::check_cache(desc)) return rc;
@@ -358,10 +403,8 @@ extern "C" sp_status sp_cache_append(const sp_cache_desc *desc, const void *k_de
     const dim3 grid((unsigned)groups);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const bool pairs = rot_style == SP_ROTATE_PAIRS;
-    if (desc->head_dim == 64)
-        sp::cache_is_e4m3(*desc) ? launch<64, true>(a, pairs, grid, st) : launch<64, false>(a, pairs, grid, st);
-    else
-        sp::cache_is_e4m3(*desc) ? launch<128, true>(a, pairs, grid, st) : launch<128, false>(a, pairs, grid, st);
+    if (desc->head_dim == 64) launch_kind<64>(a, desc->cache_type, pairs, grid, st);
+    else launch_kind<128>(a, desc->cache_type, pairs, grid, st);
     SP_HIP_CHECK(hipGetLastError());
     return SP_OK;
 }

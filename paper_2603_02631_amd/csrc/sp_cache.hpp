@@ -17,14 +17,18 @@ struct CacheView {
 };
 
 inline bool cache_is_e4m3(const sp_cache_desc &d) { return d.cache_type == SP_CACHE_E4M3; }
+inline bool cache_is_mx4(const sp_cache_desc &d) { return d.cache_type == SP_CACHE_MX4; }
+
+// Bytes of n elements (a multiple of two where two share one).
+constexpr __host__ __device__ int64_t cache_bytes(int kind, int64_t n) { return kind == SP_CACHE_MX4 ? n / 2 : kind == SP_CACHE_E4M3 ? n : 2 * n; }
 
 inline sp_status check_cache(const sp_cache_desc *d)
 {
     if (!d) return fail(SP_ERR_INVALID_ARG, "desc is null");
     if (d->n_q_heads < 1 || d->n_kv_heads < 1 || d->n_q_heads % d->n_kv_heads != 0)
         return fail(SP_ERR_INVALID_ARG, "n_q_heads = %d must be a positive multiple of n_kv_heads = %d", d->n_q_heads, d->n_kv_heads);
-    if (d->cache_type != SP_CACHE_BF16 && d->cache_type != SP_CACHE_E4M3)
-        return fail(SP_ERR_INVALID_ARG, "cache_type = %d is neither SP_CACHE_BF16 nor SP_CACHE_E4M3", d->cache_type);
+    if (d->cache_type != SP_CACHE_BF16 && d->cache_type != SP_CACHE_E4M3 && d->cache_type != SP_CACHE_MX4)
+        return fail(SP_ERR_INVALID_ARG, "cache_type = %d is none of SP_CACHE_BF16, SP_CACHE_E4M3 and SP_CACHE_MX4", d->cache_type);
     if (d->head_dim != 64 && d->head_dim != 128) return fail(SP_ERR_UNSUPPORTED, "head_dim = %d is neither 64 nor 128", d->head_dim);
     if (d->n_q_heads / d->n_kv_heads > 16)
         return fail(SP_ERR_UNSUPPORTED, "%d query heads share a kv head, at most 16 are supported", d->n_q_heads / d->n_kv_heads);
@@ -34,7 +38,7 @@ inline sp_status check_cache(const sp_cache_desc *d)
     if (d->page_tokens < 1 || d->page_tokens % kCacheBlock != 0 || d->page_tokens > (1 << 24))
         return fail(SP_ERR_INVALID_ARG, "page_tokens = %lld is not a positive multiple of %d of at most 2^24",
                     (long long)d->page_tokens, kCacheBlock);
-    const int64_t unit = cache_is_e4m3(*d) ? 16 : 8, most = int64_t(1) << 40;
+    const int64_t unit = cache_is_mx4(*d) ? 32 : cache_is_e4m3(*d) ? 16 : 8, most = int64_t(1) << 40;
     const int64_t strides[3] = {d->page_stride, d->stride_head, d->stride_token};
     for (int64_t s : strides)
         if (s < 0 || s > most || s % unit != 0)
@@ -52,13 +56,18 @@ inline sp_status check_cache(const sp_cache_desc *d)
 }
 
 // Pointers of the pools and their scales.
-inline sp_status check_pools(const sp_cache_desc &d, const void *k, const void *v, const float *ks, const float *vs)
+inline sp_status check_pools(const sp_cache_desc &d, const void *k, const void *v, const void *ks, const void *vs)
 {
     if (!k || !v) return fail(SP_ERR_INVALID_ARG, "k_pool_dev or v_pool_dev is null");
     if ((uintptr_t)k % 16 != 0 || (uintptr_t)v % 16 != 0) return fail(SP_ERR_INVALID_ARG, "cache pools must be 16-byte aligned");
     if (cache_is_e4m3(d)) {
         if (!ks || !vs) return fail(SP_ERR_INVALID_ARG, "an E4M3 cache needs k_scale_dev and v_scale_dev");
         if ((uintptr_t)ks % 4 != 0 || (uintptr_t)vs % 4 != 0) return fail(SP_ERR_INVALID_ARG, "scales must be 4-byte aligned");
+    }
+    if (cache_is_mx4(d)) {
+        if (!ks || !vs) return fail(SP_ERR_INVALID_ARG, "an MX4 cache needs k_scale_dev and v_scale_dev");
+        if ((uintptr_t)ks % 16 != 0 || (uintptr_t)vs % 16 != 0)
+            return fail(SP_ERR_INVALID_ARG, "scales of an MX4 cache must be 16-byte aligned");
     }
     return SP_OK;
 }

@@ -1,0 +1,364 @@
+// sp_attend_weights: how much attention each token of a paged cache has drawn (what an eviction goes by; the paper's importance
+// of a token is the attention that it draws, Appendix A.1.1, there over all layers at once and here for one layer's cache).
+//
+//   w[b, h, j] = old + sum_{r, g} exp(scale <q[r, g], k[b, h, j]> - lse[r, g])
+// over the rows r that see key j and the query heads g of kv head h; lse is what sp_attend wrote. A key's weight is the sum over the rows of a kv head, so a wave
+// that holds a block of keys goes through the rows and no sum crosses workgroups: nothing is added atomically, the order is fixed by the lengths.
+// The products are Q K^T with a key in a lane column: a lane adds up its rows, and the lanes of a column meet once at the end.
+#include "sp_context.hpp"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kFewRows = 16;            // rows of a kv head that sp_weights_few_kernel takes at most
+constexpr int kManyRows = 32;           // rows of a tile of sp_weights_many_kernel
+constexpr int kManyKeys = 64;           // keys of a wave there
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+struct WeightArgs : ContextArgs {
+    const float *lse, *old;
+    float *weights;
+    int64_t stride;                     // entries of a line of weights
+    int32_t per;                        // blocks of 32 tokens that a wave of sp_weights_few_kernel takes
+};
+
+// Keys [first, last) that a row sees; rows that a tile does not have see none.
+struct Seen {
+    int first, last;
+
+    __device__ __forceinline__ Seen(const ContextArgs &a, const Range &rg, int token, bool there)
+    {
+        last = !there ? 0 : a.causal ? rg.len - rg.n + token + 1 : rg.len;
+        first = a.causal && a.window > 0 && last > a.window ? last - a.window : 0;
+    }
+
+    __device__ __forceinline__ bool sees(int key) const { return key >= first && key < last; }
+};
+
+// What is taken from a row's logits, in units of log 2: its lse, or infinity for a row that adds nothing.
+__device__ __forceinline__ float reference(float lse) { return lse == neg_inf() ? __builtin_huge_valf() : lse * kLog2e; }
+
+// Stores a key's weight: what was there counts for keys before `older`.
+__device__ __forceinline__ void store_weight(const WeightArgs &a, int64_t at, int key, int older, float sum)
+{
+    a.weights[at + key] = a.old && key < older ? a.old[at + key] + sum : sum;
+}
+
+__device__ __forceinline__ int older_of(const ContextArgs &a, const Range &rg) { return a.causal ? rg.len - rg.n : rg.len; }
+
+// Requests of up to 16 rows a kv head (none too: their weights are what they were). A wave has its rows in registers and takes every fourth of its
+// workgroup's blocks of 32 tokens, a block ahead.
+template <int D, int KIND>
+__global__ __launch_bounds__(kThreads) void sp_weights_few_kernel(WeightArgs a)
+{
+    using B = Block<D, KIND, false>;
+    constexpr bool E4M3 = KIND == SP_CACHE_E4M3, MX4 = KIND == SP_CACHE_MX4;
+    constexpr int kSteps = D / 32;
+    const int b = blockIdx.y / a.c.n_kv_heads, kvh = blockIdx.y % a.c.n_kv_heads, G = a.c.group;
+    const Range rg = range_of(a, b);
+    const int64_t rows = (int64_t)rg.n * G;
+    const int blocks = (rg.len + kBlock - 1) / kBlock, lo = blockIdx.x * a.per * kWaves, hi = min(lo + a.per * kWaves, blocks);
+    if (rows > kFewRows || lo >= hi) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+    const int64_t line_at = ((int64_t)b * a.c.n_kv_heads + kvh) * a.stride;
+    const int older = older_of(a, rg);
+
+    // this lane's part of row c for the products, and of the results rows 4g .. 4g + 3
+    bf16x8 q[kSteps];
+    {
+        const int token = c / G, head = kvh * G + c % G;
+        const uint16_t *src = a.q + ((a.off[b] + token) * a.c.n_q_heads + head) * D;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const int e = MX4 ? D / 4 * g + 8 * s : E4M3 ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;
+            u32x4 w = {0, 0, 0, 0};
+            if (c < rows) w = *reinterpret_cast<const u32x4 *>(src + e);
+            q[s] = __builtin_bit_cast(bf16x8, w);
+        }
+    }
+    float ref[4];
+    int first[4], last[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int r = 4 * g + j;
+        const Seen s(a, rg, r / G, r < rows);
+        first[j] = s.first;
+        last[j] = s.last;
+        ref[j] = __builtin_huge_valf();
+        if (r < rows) ref[j] = reference(a.lse[(a.off[b] + r / G) * a.c.n_q_heads + kvh * G + r % G]);
+    }
+    // every row sees the keys of [all_lo, all_hi)
+    const int all_lo = a.causal && a.window > 0 && rg.len - a.window > 0 ? rg.len - a.window : 0;
+    const int all_hi = a.causal ? rg.len - rg.n + 1 : rg.len;
+
+    const Line line(a, b, kvh, KIND, D);
+    const uint32_t k_lane = MX4 ? 2 * c * line.row_bytes + D / 8 * g : c * line.row_bytes + 16 * g;
+    const auto load = [&](B &kv, const Place &at) {
+        if constexpr (MX4) kv.load_keys(line, at, k_lane, c * (D / 16));
+        else kv.load_keys(line, at, k_lane);
+    };
+    const float scale2 = a.scale * kLog2e;
+    int blk = lo + wave;
+    if (blk >= hi) return;
+    const int end = blk + (hi - 1 - blk) / kWaves * kWaves;
+    B kv;
+    Entry soon(a, line, min(blk + kWaves, end));
+    load(kv, Entry(a, line, blk).place(a, line));
+    // where this lane's result goes: lanes of groups 0 and 1 store the two tiles
+    const int mine = MX4 ? 2 * c + (g & 1) : 16 * (g & 1) + c;
+    for (;;) {
+        const int key0 = blk * kBlock, key = key0 + mine;
+        const Entry later(a, line, min(blk + 2 * kWaves, end));
+        float was = 0.f;
+        if (a.old && key < older) was = a.old[line_at + key];
+        f32x4 x[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            x[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                bf16x8 k;
+                if constexpr (MX4) k = kv.key(t, s, g);
+                else k = kv.key(t, s);
+                x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[s], k, x[t], 0, 0, 0);
+            }
+        }
+        float factor = scale2;
+        if constexpr (E4M3) factor = factor_of(scale2, kv.ks);
+        load(kv, soon.place(a, line));
+        soon = later;
+        if (key0 < all_lo || key0 + kBlock > all_hi)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int at = key0 + (MX4 ? 2 * c + t : 16 * t + c);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (at < first[j] || at >= last[j]) x[t][j] = neg_inf();
+            }
+        float sum[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            float p[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) p[j] = exp2_(x[t][j] * factor - ref[j]);
+            sum[t] = (p[0] + p[1]) + (p[2] + p[3]);
+            sum[t] += __shfl_xor(sum[t], 16);
+            sum[t] += __shfl_xor(sum[t], 32);
+        }
+        if (g < 2 && key < rg.len) a.weights[line_at + key] = was + (g ? sum[1] : sum[0]);
+        if (blk == end) break;
+        blk += kWaves;
+    }
+}
+
+// Requests with more rows: a wave holds 64 keys as bf16 and goes through tiles of 32 rows, which its workgroup brings to LDS. For an MX4 or E4M3 cache the
+// keys become bf16 (exact); a block's E4M3 scale goes into the factor.
+template <int D, int KIND>
+__global__ __launch_bounds__(kThreads) void sp_weights_many_kernel(WeightArgs a)
+{
+    constexpr bool E4M3 = KIND == SP_CACHE_E4M3, MX4 = KIND == SP_CACHE_MX4;
+    constexpr int kSteps = D / 16, kChunks = D / 8, kLoads = kManyRows * kChunks / kThreads;     // 16-byte pieces of a row; of a thread
+    constexpr int kKeyLoads = (int)sp::cache_bytes(KIND, D) / 32;                       // 16-byte loads of half a key's row
+    __shared__ u32x4 rows_lds[2][kManyRows * kChunks];
+    __shared__ float ref_lds[2][kManyRows];
+    __shared__ int first_lds[2][kManyRows], last_lds[2][kManyRows];
+
+    const int b = blockIdx.y / a.c.n_kv_heads, kvh = blockIdx.y % a.c.n_kv_heads, G = a.c.group;
+    const Range rg = range_of(a, b);
+    const int64_t rows64 = (int64_t)rg.n * G;
+    const int key_wg = blockIdx.x * kWaves * kManyKeys;
+    if (rows64 <= kFewRows || key_wg >= rg.len) return;
+    const int rows = (int)rows64;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = lane >> 5, c = lane & 31;
+    const int key0 = key_wg + wave * kManyKeys, older = older_of(a, rg);
+    const int64_t line_at = ((int64_t)b * a.c.n_kv_heads + kvh) * a.stride;
+    const float scale2 = a.scale * kLog2e;
+
+    // elements of step s of a lane's half of a key: E4M3 and MX4 loads bring more than one step's
+    const auto piece = [&](int s) { return MX4 ? 8 * (s / 4) + 4 * h + s % 4 : E4M3 ? 4 * (s / 2) + 2 * h + s % 2 : 2 * s + h; };
+    bf16x8 k[2][kSteps];
+    float factor[2] = {scale2, scale2};
+    const Line line(a, b, kvh, KIND, D);
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        // blocks behind the context are those of its last token: what they give is not stored
+        const int blk = min(key0 + 32 * w, rg.len - 1) / kBlock;
+        const Place at = Entry(a, line, blk).place(a, line);
+        const uint8_t *src = line.k + at.off + (int64_t)c * line.row_bytes + 16 * h;
+        if constexpr (E4M3) factor[w] = factor_of(scale2, line.ks[at.scale]);
+#pragma unroll
+        for (int i = 0; i < kKeyLoads; ++i) {
+            const u32x4 x = *reinterpret_cast<const u32x4 *>(src + 32 * i);
+            if constexpr (MX4) {
+                const float s = __uint_as_float((uint32_t)line.ks4[at.scale * D + c * (D / 32) + 2 * i + h] << 23);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    k[w][4 * i + j] = __builtin_bit_cast(bf16x8, u32x4{widen4<0>(x[j], s), widen4<1>(x[j], s), widen4<2>(x[j], s), widen4<3>(x[j], s)});
+            } else if constexpr (E4M3) {
+                k[w][2 * i] = widen8(x[0], x[1]);
+                k[w][2 * i + 1] = widen8(x[2], x[3]);
+            } else
+                k[w][i] = __builtin_bit_cast(bf16x8, x);
+        }
+    }
+
+    // rows that may see a key of this workgroup: [from, to) in tiles
+    int from = 0, to = rows;
+    if (a.causal) {
+        const int64_t p = (int64_t)rg.len - rg.n;                       // token t sees keys up to p + t
+        const int64_t t0 = key_wg - p, t1 = a.window > 0 ? (int64_t)key_wg + kWaves * kManyKeys - 1 + a.window - p : rg.n;   // tokens [t0, t1)
+        from = t0 > 0 ? (int)min(t0, (int64_t)rg.n) * G : 0;
+        to = t1 < rg.n ? (t1 > 0 ? (int)t1 * G : 0) : rows;
+    }
+    const int tile0 = from / kManyRows, tiles = to > from ? (to + kManyRows - 1) / kManyRows : tile0;
+    u32x4 next[kLoads];
+    float next_ref = 0.f;
+    Seen next_seen(a, rg, 0, false);
+    const auto slot = [&](int r, int p) { return r * kChunks + (p ^ (r & (D == 128 ? 15 : 7))); };
+    const auto fetch = [&](int tile) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int x = tid + i * kThreads, r = tile * kManyRows + x / kChunks;
+            next[i] = u32x4{0, 0, 0, 0};
+            if (r < rows)
+                next[i] = reinterpret_cast<const u32x4 *>(a.q + ((a.off[b] + r / G) * a.c.n_q_heads + kvh * G + r % G) * D)[x % kChunks];
+        }
+        if (tid < kManyRows) {
+            const int r = tile * kManyRows + tid;
+            next_seen = Seen(a, rg, r / G, r < rows);
+            next_ref = __builtin_huge_valf();
+            if (r < rows) next_ref = reference(a.lse[(a.off[b] + r / G) * a.c.n_q_heads + kvh * G + r % G]);
+        }
+    };
+    const auto put = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int x = tid + i * kThreads;
+            rows_lds[buf][slot(x / kChunks, x % kChunks)] = next[i];
+        }
+        if (tid < kManyRows) {
+            ref_lds[buf][tid] = next_ref;
+            first_lds[buf][tid] = next_seen.first;
+            last_lds[buf][tid] = next_seen.last;
+        }
+    };
+    float sum[2] = {0.f, 0.f};
+    if (tile0 < tiles) {
+        fetch(tile0);
+        put(0);
+        __syncthreads();
+    }
+    for (int tile = tile0; tile < tiles; ++tile) {
+        const int buf = (tile - tile0) & 1;
+        if (tile + 1 < tiles) fetch(tile + 1);
+        f32x16 x[2];
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[w][e] = 0.f;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const bf16x8 q = __builtin_bit_cast(bf16x8, rows_lds[buf][slot(c, piece(s))]);
+#pragma unroll
+            for (int w = 0; w < 2; ++w) x[w] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, k[w][s], x[w], 0, 0, 0);
+        }
+        // rows of a tile are in order: those in between see what its first and last row both see
+        const int t_lo = tile * kManyRows / G, t_hi = min(tile * kManyRows + kManyRows - 1, rows - 1) / G;
+        const int all_hi = a.causal ? rg.len - rg.n + t_lo + 1 : rg.len, all_lo = a.causal && a.window > 0 ? rg.len - rg.n + t_hi + 1 - a.window : 0;
+        const bool whole = key0 >= all_lo && key0 + kManyKeys <= all_hi;
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {                                // rows 8 e4 + 4 h + e
+            const f32x4 ref = *reinterpret_cast<const f32x4 *>(&ref_lds[buf][8 * e4 + 4 * h]);
+            if (!whole)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = 8 * e4 + 4 * h + e, first = first_lds[buf][r], last = last_lds[buf][r];
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        const int key = key0 + 32 * w + c;
+                        if (key < first || key >= last) x[w][4 * e4 + e] = neg_inf();
+                    }
+                }
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                float p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p[e] = exp2_(x[w][4 * e4 + e] * factor[w] - ref[e]);
+                sum[w] += (p[0] + p[1]) + (p[2] + p[3]);
+            }
+        }
+        if (tile + 1 < tiles) put(buf ^ 1);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int w = 0; w < 2; ++w) sum[w] += __shfl_xor(sum[w], 32);
+    const int key = key0 + 32 * h + c;
+    if (key < rg.len) store_weight(a, line_at, key, older, h ? sum[1] : sum[0]);
+}
+
+template <int D, int KIND>
+sp_status run(const WeightArgs &a, bool few, bool many, hipStream_t st)
+{
+    const unsigned lines = (unsigned)(a.B * a.c.n_kv_heads);
+    const int64_t blocks = sp::ceil_div(a.max_len, kBlock);
+    if (few) {
+        hipLaunchKernelGGL((sp_weights_few_kernel<D, KIND>), dim3((unsigned)sp::ceil_div(blocks, (int64_t)a.per * kWaves), lines), dim3(kThreads), 0, st, a);
+        SP_HIP_CHECK(hipGetLastError());
+    }
+    if (many) {
+        hipLaunchKernelGGL((sp_weights_many_kernel<D, KIND>), dim3((unsigned)sp::ceil_div(a.max_len, kManyKeys * kWaves), lines), dim3(kThreads), 0, st, a);
+        SP_HIP_CHECK(hipGetLastError());
+    }
+    return SP_OK;
+}
+
+template <int D>
+sp_status run_kind(const WeightArgs &a, int kind, bool few, bool many, hipStream_t st)
+{
+    if (kind == SP_CACHE_MX4) return run<D, SP_CACHE_MX4>(a, few, many, st);
+    return kind == SP_CACHE_E4M3 ? run<D, SP_CACHE_E4M3>(a, few, many, st) : run<D, SP_CACHE_BF16>(a, few, many, st);
+}
+
+}  // namespace
+
+extern "C" sp_status sp_attend_weights(const sp_cache_desc *desc, const void *q_dev, const int64_t *offsets_host, const int64_t *offsets_dev,
+                                       int32_t B, const int32_t *lens_dev, int64_t max_len, const int32_t *block_table_dev, int64_t table_stride,
+                                       const void *k_pool_dev, const void *k_scale_dev, float scale, int32_t causal, int64_t window,
+                                       const float *lse_dev, const float *old_dev, float *weights_dev, int64_t weights_stride, void *hip_stream)
+{
+    if (sp_status rc = sp::check_cache(desc)) return rc;
+    int64_t total, longest;
+    if (sp_status rc = sp::check_ragged(offsets_host, B, &total, &longest)) return rc;
+    if (max_len < 0 || max_len > kMaxLen) return sp::fail(SP_ERR_INVALID_ARG, "max_len = %lld outside 0..2^30", (long long)max_len);
+    if (total > kMaxTokens) return sp::fail(SP_ERR_UNSUPPORTED, "%lld query tokens exceed 2^26", (long long)total);
+    if (sp_status rc = check_masks(desc, max_len, table_stride, scale, causal, window)) return rc;
+    if (weights_stride < max_len || weights_stride > (int64_t(1) << 40))
+        return sp::fail(SP_ERR_INVALID_ARG, "weights_stride = %lld is less than max_len = %lld or above 2^40", (long long)weights_stride, (long long)max_len);
+    if ((int64_t)B * desc->n_kv_heads > 65535)
+        return sp::fail(SP_ERR_UNSUPPORTED, "%d requests of %d kv heads are more than a launch holds", B, desc->n_kv_heads);
+    if (B == 0 || max_len == 0) return SP_OK;
+    if (!offsets_dev || !lens_dev || !block_table_dev || !weights_dev)
+        return sp::fail(SP_ERR_INVALID_ARG, "only old_dev may be null");
+    if (total > 0 && (!q_dev || !lse_dev)) return sp::fail(SP_ERR_INVALID_ARG, "q_dev or lse_dev is null");
+    if ((uintptr_t)q_dev % 16 != 0) return sp::fail(SP_ERR_INVALID_ARG, "q_dev must be 16-byte aligned");
+    if (sp_status rc = sp::check_pools(*desc, k_pool_dev, k_pool_dev, k_scale_dev, k_scale_dev)) return rc;
+
+    const int64_t G = desc->n_q_heads / desc->n_kv_heads;
+    bool few = false, many = false;
+    for (int32_t b = 0; b < B; ++b) ((offsets_host[b + 1] - offsets_host[b]) * G > kFewRows ? many : few) = true;
+    WeightArgs a{};
+    static_cast<ContextArgs &>(a) = context_args(*desc, q_dev, offsets_dev, lens_dev, max_len, block_table_dev, table_stride, k_pool_dev, k_pool_dev,
+                                                 k_scale_dev, k_scale_dev, scale, causal, window, B);
+    a.lse = lse_dev;
+    a.old = old_dev;
+    a.weights = weights_dev;
+    a.stride = weights_stride;
+    // a wave's blocks: more of them spare queries being read again, as long as workgroups are left to fill the device
+    const int64_t blocks = sp::ceil_div(max_len, kBlock) * B * desc->n_kv_heads;
+    a.per = 1;
+    while (a.per < 16 && blocks > (int64_t)a.per * 2 * kWaves * 2048) a.per *= 2;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    return desc->head_dim == 64 ? run_kind<64>(a, desc->cache_type, few, many, st) : run_kind<128>(a, desc->cache_type, few, many, st);
+}
