@@ -664,7 +664,7 @@ sp_status sp_mx4_quantise(const void *x_dev, int32_t dtype, int64_t rows, int64_
  * with A and W as sp_mx4_quantise leaves them: a_codes_dev [M][K / 2], a_scales_dev [M][K / 32], w_codes_dev [N][K / 2], w_scales_dev
  * [N][K / 32], dense, codes 16-byte, scales 4-byte aligned. out_dev: float or bf16 (dtype an sp_logits_type), row m at m * out_stride
  * elements (out_stride >= N). Products are exact, sums are held in fp32 in an order that the sizes fix, the result is rounded once.
- * Rows with a NaN scale give NaN. K is a positive multiple of 32 below 2^31, 0 <= M, N < 2^31; (M / 16 + 1) * (N / 16 + 1) < 2^26.
+ * Rows with a NaN scale give NaN. K is a positive multiple of 32 below 2^31, 0 <= M, N < 2^31; (M / 16 + 1) * (N / 16 + 1) < 2^24.
  */
 sp_status sp_mx4_matmul(const void *a_codes_dev, const void *a_scales_dev, int64_t M, const void *w_codes_dev,
                         const void *w_scales_dev, int64_t N, int64_t K, void *out_dev, int32_t dtype, int64_t out_stride,

@@ -10,6 +10,7 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
 constexpr int kThreads = 256;
@@ -60,6 +61,8 @@ struct MatmulArgs {
     const uint8_t *a, *as, *w, *ws;
     void *out;
     int64_t M, N, K, out_stride;
+    int32_t tiles_m, tiles_n;
+    bool wide;              // rows of results can be stored four at a time
 };
 
 template <bool BF16>
@@ -69,32 +72,295 @@ __device__ __forceinline__ void store(const MatmulArgs &p, int64_t m, int64_t n,
     else static_cast<float *>(p.out)[m * p.out_stride + n] = y;
 }
 
-// A wave for 16 x 16 results.
+// Results n .. n + 3 of row m.
 template <bool BF16>
-__global__ __launch_bounds__(kThreads) void sp_mx4_matmul_kernel(MatmulArgs p)
+__device__ __forceinline__ void store4(const MatmulArgs &p, int64_t m, int64_t n, f32x4 y)
 {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
-    const int64_t tiles = (p.N + 15) / 16, x = (int64_t)blockIdx.x * (kThreads / 64) + wave, m0 = x / tiles * 16, n0 = x % tiles * 16;
-    if (m0 >= p.M) return;
-    const int64_t m = min(m0 + c, p.M - 1), n = min(n0 + c, p.N - 1), groups = p.K / kGroup;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t k0 = 0; k0 < groups; k0 += 4) {
-        const int64_t k = k0 + g;
-        u32x4 u = {0, 0, 0, 0}, v = {0, 0, 0, 0};
-        int su = 127, sv = 127;
-        if (k < groups) {
-            u = *reinterpret_cast<const u32x4 *>(p.w + (n * groups + k) * 16);
-            v = *reinterpret_cast<const u32x4 *>(p.a + (m * groups + k) * 16);
-            su = p.ws[n * groups + k];
-            sv = p.as[m * groups + k];
-        }
-        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(i32x8{(int)u[0], (int)u[1], (int)u[2], (int)u[3]}, i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3]},
-                                                               acc, 4, 4, 0, su, 0, sv);
-    }
-    if (m0 + c < p.M)
+    if (p.wide && n + 4 <= p.N) {
+        if constexpr (BF16)
+            *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(p.out) + m * p.out_stride + n) = u32x2{pack2(y[0], y[1]), pack2(y[2], y[3])};
+        else *reinterpret_cast<f32x4 *>(static_cast<float *>(p.out) + m * p.out_stride + n) = y;
+    } else
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (n0 + 4 * g + j < p.N) store<BF16>(p, m0 + c, n0 + 4 * g + j, acc[j]);
+        for (int e = 0; e < 4; ++e)
+            if (n + e < p.N) store<BF16>(p, m, n + e, y[e]);
+}
+
+__device__ __forceinline__ i32x8 operand(u32x4 x) { return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], 0, 0, 0, 0}; }
+
+// Up to four scale bytes of a row from group k on, as they lie there (at any address); 1 for groups that the row does not have.
+__device__ __forceinline__ uint32_t scales4(const uint8_t *row, int64_t k, int64_t groups)
+{
+    if (k + 4 <= groups) {
+        uint32_t w;
+        __builtin_memcpy(&w, row + k, 4);
+        return w;
+    }
+    uint32_t w = 0x7f7f7f7fu;
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+        if (k + i < groups) w = (w & ~(255u << (8 * i))) | (uint32_t)row[k + i] << (8 * i);
+    return w;
+}
+
+// ---- few rows: the weights are read once ------------------------------------------------------------------------------
+
+// Sixteen weight rows and 16 MT activation rows a workgroup. Its waves take stretches of 512 elements of the rows in turn, a lane four neighbouring groups of
+// one (64 bytes, and one word of scales), and add up in LDS.
+template <bool BF16, int MT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void sp_mx4_few_kernel(MatmulArgs p)
+{
+    __shared__ f32x4 part[WAVES][MT][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+    const int64_t m0 = (int64_t)(blockIdx.x / p.tiles_n) * 16 * MT, n0 = (int64_t)(blockIdx.x % p.tiles_n) * 16, groups = p.K / kGroup;
+    const int64_t n = min(n0 + c, p.N - 1);
+    f32x4 acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int64_t k = 16 * wave + 4 * g; k - 4 * g < groups; k += 16 * WAVES) {
+        const uint8_t *w = p.w + (n * groups + k) * 16;
+        u32x4 u[4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            u[s] = u32x4{0, 0, 0, 0};
+            if (k + s < groups) u[s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(w) + s);
+        }
+        const uint32_t su = scales4(p.ws + n * groups, k, groups);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            const int64_t m = min(m0 + 16 * t + c, p.M - 1);
+            const uint8_t *a = p.a + (m * groups + k) * 16;
+            u32x4 v[4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                v[s] = u32x4{0, 0, 0, 0};
+                if (k + s < groups) v[s] = reinterpret_cast<const u32x4 *>(a)[s];
+            }
+            const uint32_t sv = scales4(p.as + m * groups, k, groups);
+            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(u[0]), operand(v[0]), acc[t], 4, 4, 0, (int)su, 0, (int)sv);
+            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(u[1]), operand(v[1]), acc[t], 4, 4, 1, (int)su, 1, (int)sv);
+            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(u[2]), operand(v[2]), acc[t], 4, 4, 2, (int)su, 2, (int)sv);
+            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(u[3]), operand(v[3]), acc[t], 4, 4, 3, (int)su, 3, (int)sv);
+        }
+    }
+    if (WAVES > 1) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t) part[wave][t][lane] = acc[t];
+        __syncthreads();
+    }
+    for (int t = wave; t < MT; t += WAVES) {
+        f32x4 y = acc[0];
+        if (WAVES > 1) {
+            y = part[0][t][lane];
+#pragma unroll
+            for (int v = 1; v < WAVES; ++v) y += part[v][t][lane];
+        }
+        const int64_t m = m0 + 16 * t + c;
+        if (m < p.M) store4<BF16>(p, m, n0 + 4 * g, y);
+    }
+}
+
+// ---- many rows: tiles in LDS -------------------------------------------------------------------------------------------
+
+constexpr int kStep = 256;              // elements of a row that a tile takes at a time
+constexpr int kRowBytes = kStep / 2, kPieces = kRowBytes / 16, kStepGroups = kStep / kGroup;
+constexpr int64_t kMostTiledK = int64_t(1) << 22;       // offsets of a tile's rows fit 32 bits
+
+// 64 lanes x 16 bytes from base + off (each lane its own) straight into LDS from byte `to` on. asm, since the compiler would wait for all of them before it
+// reads anything else from LDS; the loop waits itself.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load_to_lds(const uint8_t *base, uint32_t off, uint32_t to)
+{
+    __asm__ volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(to) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// WM x WN waves, each with FM x FN blocks of 32 x 32 results: columns are activation rows m, rows weight rows n.
+template <bool BF16, int WM, int WN, int FM, int FN>
+struct Tiled {
+    static constexpr int kThreadsT = 64 * WM * WN, TM = 32 * WM * FM, TN = 32 * WN * FN, kRows = TM + TN;
+    static constexpr int kLoads = kRows * kPieces / kThreadsT;
+    static_assert(kRows == kThreadsT && TM % (kThreadsT / kPieces) == 0, "a thread has the scales of one row; a load is of activations or of weights");
+    static constexpr int kCodes = kRows * kRowBytes, kScales = kRows * kStepGroups;
+    static constexpr int kPad = 32 * FN + 4;
+    static constexpr int kStaged = WM * WN * 32 * kPad * 4;             // results on their way out
+    static constexpr int kLds = 2 * (kCodes + kScales) > kStaged ? 2 * (kCodes + kScales) : kStaged;
+};
+
+// The codes that a wave multiplies at a time: groups of 32 elements of its rows, one for each half of the wave.
+template <int FM, int FN>
+struct Codes {
+    u32x4 x[FM], y[FN];
+
+    __device__ __forceinline__ void read(const uint8_t *a, const uint8_t *w, uint32_t lane)
+    {
+#pragma unroll
+        for (int i = 0; i < FM; ++i) x[i] = *reinterpret_cast<const u32x4 *>(a + 32 * i * kRowBytes + lane);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) y[j] = *reinterpret_cast<const u32x4 *>(w + 32 * j * kRowBytes + lane);
+    }
+
+    template <int S>
+    __device__ __forceinline__ void multiply(f32x16 (&acc)[FM][FN], const uint32_t (&sa)[FM], const uint32_t (&sw)[FN]) const
+    {
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(y[j]), operand(x[i]), acc[i][j], 4, 4, S, (int)sw[j], S, (int)sa[i]);
+    }
+};
+
+template <bool BF16, int WM, int WN, int FM, int FN>
+__global__ __launch_bounds__(64 * WM * WN) void sp_mx4_tiled_kernel(MatmulArgs p)
+{
+    using T = Tiled<BF16, WM, WN, FM, FN>;
+    __shared__ alignas(16) uint8_t lds[T::kLds];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = lane >> 5, c = lane & 31;
+    // neighbouring tiles on one die: eight rows of tiles at a time
+    int x = blockIdx.x;
+    const int total = p.tiles_m * p.tiles_n, per = total / 8;
+    if (x < 8 * per) x = x % 8 * per + x / 8;
+    const int band = 8 * p.tiles_n, first = x / band * 8, deep = min(8, p.tiles_m - first);
+    const int64_t m0 = (int64_t)(first + x % band % deep) * T::TM, n0 = (int64_t)(x % band / deep) * T::TN;
+    const int64_t row_bytes = p.K / 2, groups = p.K / kGroup;
+    const int steps = (int)((p.K + kStep - 1) / kStep), rest = (int)(p.K % kStep);       // elements of the last step, 0: all
+
+    // this thread's pieces: row (of the activations, then of the weights) and place in it, swapped about so that sixteen lanes read sixteen places of 16 bytes
+    uint32_t off[T::kLoads];
+    const int slot = tid % kPieces, piece = slot ^ (tid / kPieces >> 1 & 7);
+#pragma unroll
+    for (int i = 0; i < T::kLoads; ++i) {
+        const int r = tid / kPieces + i * (T::kThreadsT / kPieces);
+        const int64_t row = r < T::TM ? min((int64_t)r, p.M - 1 - m0) : min((int64_t)(r - T::TM), p.N - 1 - n0);
+        off[i] = (uint32_t)(row * row_bytes + 16 * piece);
+    }
+    const uint8_t *a_base = p.a + m0 * row_bytes, *w_base = p.w + n0 * row_bytes;
+    const uint8_t *scale_row = tid < T::TM ? p.as + min(m0 + tid, p.M - 1) * groups : p.ws + min(n0 + tid - T::TM, p.N - 1) * groups;
+    const uint32_t lds_at = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t *)lds);
+    uint8_t *const scale_lds = lds + 2 * T::kCodes;
+
+    const auto load_codes = [&](int step, int buf) {
+        const bool tail = rest != 0 && step == steps - 1;
+#pragma unroll
+        for (int i = 0; i < T::kLoads; ++i) {
+            const bool of_a = i * (T::kThreadsT / kPieces) < T::TM;
+            const uint32_t to = buf * T::kCodes + i * T::kThreadsT * 16;
+            if (!tail || 32 * piece < rest) load_to_lds((of_a ? a_base : w_base) + (int64_t)step * kRowBytes, off[i], lds_at + to + wave * 1024);
+            else *reinterpret_cast<u32x4 *>(lds + to + tid * 16) = u32x4{0, 0, 0, 0};
+        }
+    };
+    const auto load_scales = [&](int step) {
+        const int64_t k = (int64_t)step * kStepGroups;
+        return u32x2{scales4(scale_row, k, groups), scales4(scale_row, k + 4, groups)};
+    };
+    const auto put_scales = [&](u32x2 w, int buf) { *reinterpret_cast<u32x2 *>(scale_lds + buf * T::kScales + tid * kStepGroups) = w; };
+
+    f32x16 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    const int wm = wave / WN, wn = wave % WN;
+    const int row_a = 32 * FM * wm + c, row_w = T::TM + 32 * FN * wn + c;
+    uint32_t at[4];             // a lane's place in its row: half h takes groups 4h .. 4h + 3 of a step, one after another
+#pragma unroll
+    for (int s = 0; s < 4; ++s) at[s] = 16 * ((4 * h + s) ^ (c >> 1 & 7));
+
+    put_scales(load_scales(0), 0);
+    u32x2 scales = load_scales(1);
+    load_codes(0, 0);
+    __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    for (int step = 0; step < steps; ++step) {
+        const int buf = step & 1;
+        put_scales(scales, buf ^ 1);                        // of the next step, loaded in the one before
+        if (step + 1 < steps) {
+            scales = load_scales(step + 2);
+            load_codes(step + 1, buf ^ 1);
+        }
+        const uint8_t *a = lds + buf * T::kCodes + row_a * kRowBytes, *w = lds + buf * T::kCodes + row_w * kRowBytes;
+        uint32_t sa[FM], sw[FN];
+#pragma unroll
+        for (int i = 0; i < FM; ++i) sa[i] = *reinterpret_cast<const uint32_t *>(scale_lds + buf * T::kScales + (row_a + 32 * i) * kStepGroups + 4 * h);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) sw[j] = *reinterpret_cast<const uint32_t *>(scale_lds + buf * T::kScales + (row_w + 32 * j) * kStepGroups + 4 * h);
+        // codes are read one group of products ahead; the scheduling barriers keep them from being read later, or further ahead, for which there are no registers
+        Codes<FM, FN> even, odd;
+        even.read(a, w, at[0]);
+        odd.read(a, w, at[1]);
+        __builtin_amdgcn_sched_barrier(0);
+        even.template multiply<0>(acc, sa, sw);
+        __builtin_amdgcn_sched_barrier(0);
+        even.read(a, w, at[2]);
+        __builtin_amdgcn_sched_barrier(0);
+        odd.template multiply<1>(acc, sa, sw);
+        __builtin_amdgcn_sched_barrier(0);
+        odd.read(a, w, at[3]);
+        __builtin_amdgcn_sched_barrier(0);
+        even.template multiply<2>(acc, sa, sw);
+        odd.template multiply<3>(acc, sa, sw);
+        __builtin_amdgcn_sched_barrier(0);                  // products before the wait
+        __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    }
+
+    // A wave's results go through LDS, 32 rows at a time, so that rows leave in pieces of 128 bytes and more.
+    float *mine = reinterpret_cast<float *>(lds) + wave * 32 * T::kPad;
+    constexpr int kLanes = 8 * FN;                          // of a row, four results each
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<f32x4 *>(mine + c * T::kPad + 32 * j + 2 * e + 4 * h) = f32x4{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int r = 0; r < 32; r += 64 / kLanes) {
+            const int row = r + lane / kLanes, col = 4 * (lane % kLanes);
+            const f32x4 y = *reinterpret_cast<const f32x4 *>(mine + row * T::kPad + col);
+            const int64_t m = m0 + 32 * (FM * wm + i) + row, n = n0 + 32 * FN * wn + col;
+            if (m < p.M && n < p.N) store4<BF16>(p, m, n, y);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+template <bool BF16, int WM, int WN, int FM, int FN>
+sp_status tiled(MatmulArgs p, hipStream_t st)
+{
+    using T = Tiled<BF16, WM, WN, FM, FN>;
+    p.tiles_m = (int32_t)sp::ceil_div(p.M, T::TM);
+    p.tiles_n = (int32_t)sp::ceil_div(p.N, T::TN);
+    hipLaunchKernelGGL((sp_mx4_tiled_kernel<BF16, WM, WN, FM, FN>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(T::kThreadsT), 0, st, p);
+    SP_HIP_CHECK(hipGetLastError());
+    return SP_OK;
+}
+
+template <bool BF16, int MT>
+sp_status few(MatmulArgs p, hipStream_t st)
+{
+    p.tiles_m = (int32_t)sp::ceil_div(p.M, 16 * MT);
+    p.tiles_n = (int32_t)sp::ceil_div(p.N, 16);
+    hipLaunchKernelGGL((sp_mx4_few_kernel<BF16, MT, 4>), dim3((unsigned)((int64_t)p.tiles_m * p.tiles_n)), dim3(256), 0, st, p);
+    SP_HIP_CHECK(hipGetLastError());
+    return SP_OK;
+}
+
+template <bool BF16>
+sp_status run(const MatmulArgs &p, hipStream_t st)
+{
+    if (p.M <= 16) return few<BF16, 1>(p, st);
+    if (p.M <= 32) return few<BF16, 2>(p, st);
+    if (p.K <= kMostTiledK) {
+        if (sp::ceil_div(p.M, 256) * sp::ceil_div(p.N, 256) >= 192) return tiled<BF16, 2, 4, 4, 2>(p, st);
+        if (sp::ceil_div(p.M, 128) * sp::ceil_div(p.N, 128) >= 128) return tiled<BF16, 2, 2, 2, 2>(p, st);
+    }
+    return few<BF16, 4>(p, st);
 }
 
 bool bad_kind(int32_t dtype) { return dtype != SP_LOGITS_F32 && dtype != SP_LOGITS_BF16; }
@@ -143,13 +409,11 @@ extern "C" sp_status sp_mx4_matmul(const void *a_codes_dev, const void *a_scales
     if ((uintptr_t)a_codes_dev % 16 != 0 || (uintptr_t)w_codes_dev % 16 != 0 || (uintptr_t)a_scales_dev % 4 != 0 || (uintptr_t)w_scales_dev % 4 != 0)
         return sp::fail(SP_ERR_INVALID_ARG, "codes must be 16-byte, scales 4-byte aligned");
     if ((uintptr_t)out_dev % (dtype == SP_LOGITS_F32 ? 4 : 2) != 0) return sp::fail(SP_ERR_INVALID_ARG, "out_dev is not aligned to its elements");
-    const int64_t tiles = sp::ceil_div(M, 16) * sp::ceil_div(N, 16), groups = sp::ceil_div(tiles, kThreads / 64);
-    if (groups >= (int64_t(1) << 24)) return sp::fail(SP_ERR_UNSUPPORTED, "%lld x %lld results are more than a launch holds", (long long)M, (long long)N);
+    if ((M / 16 + 1) * (N / 16 + 1) >= (int64_t(1) << 24))
+        return sp::fail(SP_ERR_UNSUPPORTED, "%lld x %lld results are more than a launch holds", (long long)M, (long long)N);
     const MatmulArgs p{static_cast<const uint8_t *>(a_codes_dev), static_cast<const uint8_t *>(a_scales_dev), static_cast<const uint8_t *>(w_codes_dev),
-                       static_cast<const uint8_t *>(w_scales_dev), out_dev, M, N, K, out_stride};
+                       static_cast<const uint8_t *>(w_scales_dev), out_dev, M, N, K, out_stride, 0, 0,
+                       out_stride % 4 == 0 && (uintptr_t)out_dev % (dtype == SP_LOGITS_F32 ? 16 : 8) == 0};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (dtype == SP_LOGITS_BF16) hipLaunchKernelGGL((sp_mx4_matmul_kernel<true>), dim3((unsigned)groups), dim3(kThreads), 0, st, p);
-    else hipLaunchKernelGGL((sp_mx4_matmul_kernel<false>), dim3((unsigned)groups), dim3(kThreads), 0, st, p);
-    SP_HIP_CHECK(hipGetLastError());
-    return SP_OK;
+    return dtype == SP_LOGITS_BF16 ? run<true>(p, st) : run<false>(p, st);
 }
