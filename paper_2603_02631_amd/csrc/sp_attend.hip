@@ -118,13 +118,6 @@ struct Rows {
     }
 };
 
-// A value that is the same in all lanes, as a scalar.
-__device__ __forceinline__ int64_t uniform(int64_t x)
-{
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)x >> 32));
-    return (int64_t)((uint64_t)hi << 32 | lo);
-}
-
 // Where a stretch of work begins: the unit `pos` lies in item `item`, whose units begin at `before`; all items have `total`.
 struct Start {
     int item;

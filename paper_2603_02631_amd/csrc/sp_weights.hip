@@ -21,7 +21,7 @@ struct WeightArgs : ContextArgs {
     const float *lse, *old;
     float *weights;
     int64_t stride;                     // entries of a line of weights
-    int32_t per;                        // blocks of 32 tokens that a wave of sp_weights_few_kernel takes
+    int32_t per;                        // pairs of blocks of 32 tokens that a wave of sp_weights_few_kernel takes
 };
 
 // Keys [first, last) that a row sees; rows that a tile does not have see none.
@@ -48,9 +48,24 @@ __device__ __forceinline__ void store_weight(const WeightArgs &a, int64_t at, in
 
 __device__ __forceinline__ int older_of(const ContextArgs &a, const Range &rg) { return a.causal ? rg.len - rg.n : rg.len; }
 
-// Requests of up to 16 rows a kv head (none too: their weights are what they were). A wave has its rows in registers and takes every fourth of its
-// workgroup's blocks of 32 tokens, a block ahead.
-template <int D, int KIND>
+// Lanes of group g (16 of them) take x of tile g: lanes of group 0 of every one of four tiles hold what counts.
+__device__ __forceinline__ float gather4(float x0, float x1, float x2, float x3)
+{
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x0), __float_as_uint(x2), false, false);     // [x0 lower | x2 lower]
+    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(x1), __float_as_uint(x3), false, false);
+    return __uint_as_float(__builtin_amdgcn_permlane16_swap(p[0], q[0], false, false)[0]);
+}
+
+// Lower half of a wave: x of tile 0, upper half: x of tile 1; their lower halves hold what counts.
+__device__ __forceinline__ float gather2(float x0, float x1)
+{
+    return __uint_as_float(__builtin_amdgcn_permlane32_swap(__float_as_uint(x0), __float_as_uint(x1), false, false)[0]);
+}
+
+// Requests of up to 16 rows a kv head (none too: their weights are what they were). A wave has its rows in registers and takes pairs of blocks of 32 tokens, one of
+// its workgroup's in turn, a pair ahead. After the products lane 16 g + c holds rows 4g .. 4g + 3 of a column's key. With at most four rows (LIVE = 1) only lanes of group 0
+// hold any, so four tiles of 16 keys are gathered into all lanes before the exponentials, with at most eight (LIVE = 2) two.
+template <int D, int KIND, int LIVE>
 __global__ __launch_bounds__(kThreads) void sp_weights_few_kernel(WeightArgs a)
 {
     using B = Block<D, KIND, false>;
@@ -59,13 +74,15 @@ __global__ __launch_bounds__(kThreads) void sp_weights_few_kernel(WeightArgs a)
     const int b = blockIdx.y / a.c.n_kv_heads, kvh = blockIdx.y % a.c.n_kv_heads, G = a.c.group;
     const Range rg = range_of(a, b);
     const int64_t rows = (int64_t)rg.n * G;
-    const int blocks = (rg.len + kBlock - 1) / kBlock, lo = blockIdx.x * a.per * kWaves, hi = min(lo + a.per * kWaves, blocks);
+    const int pairs = (rg.len + 2 * kBlock - 1) / (2 * kBlock), lo = blockIdx.x * a.per * kWaves, hi = __builtin_amdgcn_readfirstlane(min(lo + a.per * kWaves, pairs));
     if (rows > kFewRows || lo >= hi) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+    int pair = lo + wave;
+    if (pair >= hi) return;
     const int64_t line_at = ((int64_t)b * a.c.n_kv_heads + kvh) * a.stride;
     const int older = older_of(a, rg);
 
-    // this lane's part of row c for the products, and of the results rows 4g .. 4g + 3
+    // this lane's part of row c for the products, and what it needs of the rows whose results it holds: 4 (g % LIVE) .. + 3
     bf16x8 q[kSteps];
     {
         const int token = c / G, head = kvh * G + c % G;
@@ -82,7 +99,7 @@ __global__ __launch_bounds__(kThreads) void sp_weights_few_kernel(WeightArgs a)
     int first[4], last[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int r = 4 * g + j;
+        const int r = 4 * (g % LIVE) + j;
         const Seen s(a, rg, r / G, r < rows);
         first[j] = s.first;
         last[j] = s.last;
@@ -95,61 +112,98 @@ __global__ __launch_bounds__(kThreads) void sp_weights_few_kernel(WeightArgs a)
 
     const Line line(a, b, kvh, KIND, D);
     const uint32_t k_lane = MX4 ? 2 * c * line.row_bytes + D / 8 * g : c * line.row_bytes + 16 * g;
-    const auto load = [&](B &kv, const Place &at) {
+    const int last_block = __builtin_amdgcn_readfirstlane((rg.len - 1) / kBlock);           // the second of a last pair may not be there
+    const auto load = [&](B &kv, const Entry &e) {
+        Place at = e.place(a, line);
+        at = {uniform(at.off), uniform(at.scale)};
         if constexpr (MX4) kv.load_keys(line, at, k_lane, c * (D / 16));
         else kv.load_keys(line, at, k_lane);
     };
     const float scale2 = a.scale * kLog2e;
-    int blk = lo + wave;
-    if (blk >= hi) return;
-    const int end = blk + (hi - 1 - blk) / kWaves * kWaves;
-    B kv;
-    Entry soon(a, line, min(blk + kWaves, end));
-    load(kv, Entry(a, line, blk).place(a, line));
-    // where this lane's result goes: lanes of groups 0 and 1 store the two tiles
-    const int mine = MX4 ? 2 * c + (g & 1) : 16 * (g & 1) + c;
+    const int end = pair + (hi - 1 - pair) / kWaves * kWaves;
+    B kv[2];
+    const auto entry = [&](int blk) { return Entry(a, line, min(blk, last_block)); };
+    Entry soon[2] = {entry(2 * min(pair + kWaves, end)), entry(2 * min(pair + kWaves, end) + 1)};
+#pragma unroll
+    for (int u = 0; u < 2; ++u) load(kv[u], entry(2 * pair + u));
+    // key of column c of tile t (0, 1) of a block; the key of a pair whose weight this lane stores
+    const auto key_in = [&](int t) { return MX4 ? 2 * c + t : 16 * t + c; };
+    const int mine = LIVE == 2 ? kBlock * (g & 1) + key_in(g >> 1) : kBlock * (g >> 1) + key_in(g & 1);
+    const auto weight_before = [&](int of) {
+        const int key = 2 * kBlock * of + mine;
+        return a.old && key < older ? a.old[line_at + key] : 0.f;
+    };
+    float was = weight_before(pair);
     for (;;) {
-        const int key0 = blk * kBlock, key = key0 + mine;
-        const Entry later(a, line, min(blk + 2 * kWaves, end));
-        float was = 0.f;
-        if (a.old && key < older) was = a.old[line_at + key];
-        f32x4 x[2];
+        const int key0 = pair * 2 * kBlock, then = 2 * min(pair + 2 * kWaves, end), own = key0 + mine;
+        const Entry later[2] = {entry(then), entry(then + 1)};
+        f32x4 x[4];                                         // tiles 0, 1 of the first block, then of the second
+        float factor[2] = {scale2, scale2};
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            x[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                bf16x8 k;
-                if constexpr (MX4) k = kv.key(t, s, g);
-                else k = kv.key(t, s);
-                x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[s], k, x[t], 0, 0, 0);
-            }
-        }
-        float factor = scale2;
-        if constexpr (E4M3) factor = factor_of(scale2, kv.ks);
-        load(kv, soon.place(a, line));
-        soon = later;
-        if (key0 < all_lo || key0 + kBlock > all_hi)
+        for (int u = 0; u < 2; ++u) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const int at = key0 + (MX4 ? 2 * c + t : 16 * t + c);
+                x[2 * u + t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (at < first[j] || at >= last[j]) x[t][j] = neg_inf();
+                for (int s = 0; s < kSteps; ++s) {
+                    bf16x8 k;
+                    if constexpr (MX4) k = kv[u].key(t, s, g);
+                    else k = kv[u].key(t, s);
+                    x[2 * u + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[s], k, x[2 * u + t], 0, 0, 0);
+                }
             }
-        float sum[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
+            if constexpr (E4M3) factor[u] = factor_of(scale2, kv[u].ks);
+            load(kv[u], soon[u]);
+            soon[u] = later[u];
+        }
+        const float will = weight_before(min(pair + kWaves, end));
+        const bool whole = key0 >= all_lo && key0 + 2 * kBlock <= all_hi;
+        // the key's logits of this lane's four rows become its part of the weight
+        const auto part = [&](f32x4 y, float f, int key) {
             float p[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) p[j] = exp2_(x[t][j] * factor - ref[j]);
-            sum[t] = (p[0] + p[1]) + (p[2] + p[3]);
-            sum[t] += __shfl_xor(sum[t], 16);
-            sum[t] += __shfl_xor(sum[t], 32);
+            for (int j = 0; j < 4; ++j) {
+                if (!whole && (key < first[j] || key >= last[j])) y[j] = neg_inf();
+                p[j] = exp2_(y[j] * f - ref[j]);
+            }
+            return (p[0] + p[1]) + (p[2] + p[3]);
+        };
+        float sum;
+        if constexpr (LIVE == 1) {
+            f32x4 y;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] = gather4(x[0][j], x[1][j], x[2][j], x[3][j]);
+            sum = part(y, g < 2 ? factor[0] : factor[1], own);
+        } else if constexpr (LIVE == 2) {
+            float s[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                f32x4 y;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = gather2(x[2 * u][j], x[2 * u + 1][j]);
+                s[u] = part(y, factor[u], key0 + kBlock * u + key_in(g >> 1));
+            }
+            // lanes of even groups keep the first block's, those of odd ones the second's
+            const float give = g & 1 ? s[0] : s[1], keep = g & 1 ? s[1] : s[0];
+            sum = keep + __shfl_xor(give, 16);
+        } else {
+            float s[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) s[t] = part(x[t], factor[t >> 1], key0 + kBlock * (t >> 1) + key_in(t & 1));
+            // tile t ends up in group t: its halves meet, then its quarters
+            float half[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const float give = g & 2 ? s[t] : s[2 + t], keep = g & 2 ? s[2 + t] : s[t];
+                half[t] = keep + __shfl_xor(give, 32);
+            }
+            const float give = g & 1 ? half[0] : half[1], keep = g & 1 ? half[1] : half[0];
+            sum = keep + __shfl_xor(give, 16);
         }
-        if (g < 2 && key < rg.len) a.weights[line_at + key] = was + (g ? sum[1] : sum[0]);
-        if (blk == end) break;
-        blk += kWaves;
+        if (own < rg.len) a.weights[line_at + own] = was + sum;
+        was = will;
+        if (pair == end) break;
+        pair += kWaves;
     }
 }
 
@@ -298,13 +352,16 @@ __global__ __launch_bounds__(kThreads) void sp_weights_many_kernel(WeightArgs a)
     if (key < rg.len) store_weight(a, line_at, key, older, h ? sum[1] : sum[0]);
 }
 
+// few: rows of a kv head of the largest request that has few, -1 if none has
 template <int D, int KIND>
-sp_status run(const WeightArgs &a, bool few, bool many, hipStream_t st)
+sp_status run(const WeightArgs &a, int few, bool many, hipStream_t st)
 {
     const unsigned lines = (unsigned)(a.B * a.c.n_kv_heads);
-    const int64_t blocks = sp::ceil_div(a.max_len, kBlock);
-    if (few) {
-        hipLaunchKernelGGL((sp_weights_few_kernel<D, KIND>), dim3((unsigned)sp::ceil_div(blocks, (int64_t)a.per * kWaves), lines), dim3(kThreads), 0, st, a);
+    if (few >= 0) {
+        const dim3 grid((unsigned)sp::ceil_div(sp::ceil_div(a.max_len, 2 * kBlock), (int64_t)a.per * kWaves), lines);
+        if (few <= 4) hipLaunchKernelGGL((sp_weights_few_kernel<D, KIND, 1>), grid, dim3(kThreads), 0, st, a);
+        else if (few <= 8) hipLaunchKernelGGL((sp_weights_few_kernel<D, KIND, 2>), grid, dim3(kThreads), 0, st, a);
+        else hipLaunchKernelGGL((sp_weights_few_kernel<D, KIND, 4>), grid, dim3(kThreads), 0, st, a);
         SP_HIP_CHECK(hipGetLastError());
     }
     if (many) {
@@ -315,7 +372,7 @@ sp_status run(const WeightArgs &a, bool few, bool many, hipStream_t st)
 }
 
 template <int D>
-sp_status run_kind(const WeightArgs &a, int kind, bool few, bool many, hipStream_t st)
+sp_status run_kind(const WeightArgs &a, int kind, int few, bool many, hipStream_t st)
 {
     if (kind == SP_CACHE_MX4) return run<D, SP_CACHE_MX4>(a, few, many, st);
     return kind == SP_CACHE_E4M3 ? run<D, SP_CACHE_E4M3>(a, few, many, st) : run<D, SP_CACHE_BF16>(a, few, many, st);
@@ -346,8 +403,13 @@ extern "C" sp_status sp_attend_weights(const sp_cache_desc *desc, const void *q_
     if (sp_status rc = sp::check_pools(*desc, k_pool_dev, k_pool_dev, k_scale_dev, k_scale_dev)) return rc;
 
     const int64_t G = desc->n_q_heads / desc->n_kv_heads;
-    bool few = false, many = false;
-    for (int32_t b = 0; b < B; ++b) ((offsets_host[b + 1] - offsets_host[b]) * G > kFewRows ? many : few) = true;
+    int few = -1;
+    bool many = false;
+    for (int32_t b = 0; b < B; ++b) {
+        const int64_t rows = (offsets_host[b + 1] - offsets_host[b]) * G;
+        if (rows > kFewRows) many = true;
+        else few = rows > few ? (int)rows : few;
+    }
     WeightArgs a{};
     static_cast<ContextArgs &>(a) = context_args(*desc, q_dev, offsets_dev, lens_dev, max_len, block_table_dev, table_stride, k_pool_dev, k_pool_dev,
                                                  k_scale_dev, k_scale_dev, scale, causal, window, B);
@@ -355,10 +417,10 @@ extern "C" sp_status sp_attend_weights(const sp_cache_desc *desc, const void *q_
     a.old = old_dev;
     a.weights = weights_dev;
     a.stride = weights_stride;
-    // a wave's blocks: more of them spare queries being read again, as long as workgroups are left to fill the device
-    const int64_t blocks = sp::ceil_div(max_len, kBlock) * B * desc->n_kv_heads;
+    // pairs of blocks of a wave: more of them spare queries being read again, as long as workgroups are left to fill the device
+    const int64_t pairs = sp::ceil_div(max_len, 2 * kBlock) * B * desc->n_kv_heads;
     a.per = 1;
-    while (a.per < 16 && blocks > (int64_t)a.per * 2 * kWaves * 2048) a.per *= 2;
+    while (a.per < 8 && pairs > (int64_t)a.per * 2 * kWaves * 2048) a.per *= 2;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     return desc->head_dim == 64 ? run_kind<64>(a, desc->cache_type, few, many, st) : run_kind<128>(a, desc->cache_type, few, many, st);
 }
