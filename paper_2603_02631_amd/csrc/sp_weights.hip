@@ -13,7 +13,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kFewRows = 16;            // rows of a kv head that sp_weights_few_kernel takes at most
 constexpr int kManyRows = 32;           // rows of a tile of sp_weights_many_kernel
-constexpr int kManyKeys = 64;           // keys of a wave there
+constexpr int many_blocks(int d) { return 128 / d; }    // blocks of 32 keys of a wave there: as many as leave four waves a SIMD their registers
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
@@ -207,14 +207,15 @@ __global__ __launch_bounds__(kThreads) void sp_weights_few_kernel(WeightArgs a)
     }
 }
 
-// Requests with more rows: a wave holds 64 keys as bf16 and goes through tiles of 32 rows, which its workgroup brings to LDS. For an MX4 or E4M3 cache the
+// Requests with more rows: a wave holds 32 or 64 keys as bf16 and goes through tiles of 32 rows, which its workgroup brings to LDS. For an MX4 or E4M3 cache the
 // keys become bf16 (exact); a block's E4M3 scale goes into the factor.
 template <int D, int KIND>
-__global__ __launch_bounds__(kThreads) void sp_weights_many_kernel(WeightArgs a)
+__global__ __launch_bounds__(kThreads, 4) void sp_weights_many_kernel(WeightArgs a)
 {
     constexpr bool E4M3 = KIND == SP_CACHE_E4M3, MX4 = KIND == SP_CACHE_MX4;
     constexpr int kSteps = D / 16, kChunks = D / 8, kLoads = kManyRows * kChunks / kThreads;     // 16-byte pieces of a row; of a thread
     constexpr int kKeyLoads = (int)sp::cache_bytes(KIND, D) / 32;                       // 16-byte loads of half a key's row
+    constexpr int W = many_blocks(D), kManyKeys = 32 * W;
     __shared__ u32x4 rows_lds[2][kManyRows * kChunks];
     __shared__ float ref_lds[2][kManyRows];
     __shared__ int first_lds[2][kManyRows], last_lds[2][kManyRows];
@@ -232,15 +233,16 @@ __global__ __launch_bounds__(kThreads) void sp_weights_many_kernel(WeightArgs a)
 
     // elements of step s of a lane's half of a key: E4M3 and MX4 loads bring more than one step's
     const auto piece = [&](int s) { return MX4 ? 8 * (s / 4) + 4 * h + s % 4 : E4M3 ? 4 * (s / 2) + 2 * h + s % 2 : 2 * s + h; };
-    bf16x8 k[2][kSteps];
-    float factor[2] = {scale2, scale2};
+    bf16x8 k[W][kSteps];
+    float factor[W];
     const Line line(a, b, kvh, KIND, D);
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
+    for (int w = 0; w < W; ++w) {
         // blocks behind the context are those of its last token: what they give is not stored
         const int blk = min(key0 + 32 * w, rg.len - 1) / kBlock;
         const Place at = Entry(a, line, blk).place(a, line);
         const uint8_t *src = line.k + at.off + (int64_t)c * line.row_bytes + 16 * h;
+        factor[w] = scale2;
         if constexpr (E4M3) factor[w] = factor_of(scale2, line.ks[at.scale]);
 #pragma unroll
         for (int i = 0; i < kKeyLoads; ++i) {
@@ -298,7 +300,7 @@ __global__ __launch_bounds__(kThreads) void sp_weights_many_kernel(WeightArgs a)
             last_lds[buf][tid] = next_seen.last;
         }
     };
-    float sum[2] = {0.f, 0.f};
+    float sum[W] = {};
     if (tile0 < tiles) {
         fetch(tile0);
         put(0);
@@ -307,16 +309,16 @@ __global__ __launch_bounds__(kThreads) void sp_weights_many_kernel(WeightArgs a)
     for (int tile = tile0; tile < tiles; ++tile) {
         const int buf = (tile - tile0) & 1;
         if (tile + 1 < tiles) fetch(tile + 1);
-        f32x16 x[2];
+        f32x16 x[W];
 #pragma unroll
-        for (int w = 0; w < 2; ++w)
+        for (int w = 0; w < W; ++w)
 #pragma unroll
             for (int e = 0; e < 16; ++e) x[w][e] = 0.f;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             const bf16x8 q = __builtin_bit_cast(bf16x8, rows_lds[buf][slot(c, piece(s))]);
 #pragma unroll
-            for (int w = 0; w < 2; ++w) x[w] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, k[w][s], x[w], 0, 0, 0);
+            for (int w = 0; w < W; ++w) x[w] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, k[w][s], x[w], 0, 0, 0);
         }
         // rows of a tile are in order: those in between see what its first and last row both see
         const int t_lo = tile * kManyRows / G, t_hi = min(tile * kManyRows + kManyRows - 1, rows - 1) / G;
@@ -330,13 +332,13 @@ __global__ __launch_bounds__(kThreads) void sp_weights_many_kernel(WeightArgs a)
                 for (int e = 0; e < 4; ++e) {
                     const int r = 8 * e4 + 4 * h + e, first = first_lds[buf][r], last = last_lds[buf][r];
 #pragma unroll
-                    for (int w = 0; w < 2; ++w) {
+                    for (int w = 0; w < W; ++w) {
                         const int key = key0 + 32 * w + c;
                         if (key < first || key >= last) x[w][4 * e4 + e] = neg_inf();
                     }
                 }
 #pragma unroll
-            for (int w = 0; w < 2; ++w) {
+            for (int w = 0; w < W; ++w) {
                 float p[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) p[e] = exp2_(x[w][4 * e4 + e] * factor[w] - ref[e]);
@@ -347,9 +349,9 @@ __global__ __launch_bounds__(kThreads) void sp_weights_many_kernel(WeightArgs a)
         __syncthreads();
     }
 #pragma unroll
-    for (int w = 0; w < 2; ++w) sum[w] += __shfl_xor(sum[w], 32);
-    const int key = key0 + 32 * h + c;
-    if (key < rg.len) store_weight(a, line_at, key, older, h ? sum[1] : sum[0]);
+    for (int w = 0; w < W; ++w) sum[w] += __shfl_xor(sum[w], 32);
+    const int key = key0 + 32 * (W == 2 ? h : 0) + c;
+    if (key < rg.len && (W == 2 || h == 0)) store_weight(a, line_at, key, older, W == 2 && h ? sum[W - 1] : sum[0]);
 }
 
 // few: rows of a kv head of the largest request that has few, -1 if none has
@@ -365,7 +367,7 @@ sp_status run(const WeightArgs &a, int few, bool many, hipStream_t st)
         SP_HIP_CHECK(hipGetLastError());
     }
     if (many) {
-        hipLaunchKernelGGL((sp_weights_many_kernel<D, KIND>), dim3((unsigned)sp::ceil_div(a.max_len, kManyKeys * kWaves), lines), dim3(kThreads), 0, st, a);
+        hipLaunchKernelGGL((sp_weights_many_kernel<D, KIND>), dim3((unsigned)sp::ceil_div(a.max_len, 32 * many_blocks(D) * kWaves), lines), dim3(kThreads), 0, st, a);
         SP_HIP_CHECK(hipGetLastError());
     }
     return SP_OK;

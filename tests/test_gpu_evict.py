@@ -279,6 +279,30 @@ def test_evict_ties_go_to_the_earlier_token(seed):
         check_evict("mx4", 2, 64, [3000, 1100], [700, 500], 4, 20, weights=w, seed=seed)
 
 
+@pytest.mark.parametrize("L,m", [(20000, 5000), (20000, 19999), (6000, 40), (3000, 700)])
+def test_evict_by_weights_that_are_near_each_other(L, m):
+    """More contenders than are listed at a time share the first digits, with and without equal weights among them."""
+    rng = np.random.default_rng(L + m)
+    check_evict("mx4", 1, 64, [L], [m], 4, 32, page=4096, weights=1 + rng.random((1, 1, L)) * 0.2)
+    check_evict("mx4", 1, 64, [L], [m], 4, 32, page=4096, weights=1 + rng.integers(0, 7, (1, 1, L)) * 2.0 ** -23)
+    check_evict("mx4", 1, 64, [L], [m], 0, 0, page=4096, weights=rng.integers(0, 1 << 24, (1, 1, L)).astype(np.float64))
+
+
+def test_evict_orders_nan_and_infinity():
+    """A positive NaN above, a negative one below everything, infinities as numbers."""
+    L, m = 40, 9
+    w = np.arange(L, dtype=np.float32)[None, None] * -1.0
+    bits = w.view(np.uint32)
+    bits[0, 0, 30], bits[0, 0, 20], bits[0, 0, 0], bits[0, 0, 12] = 0x7FC00000, 0x7F800000, 0xFFFFFFFF, 0x7FFFFFFF
+    bits[0, 0, 1], bits[0, 0, 2] = 0xFFC00000, 0xFF800000
+    c, _, _, _ = filled("mx4", 2, 1, 64, [0], [L], 64, spare=3)
+    dst = np.array([[p for p in range(c.n_pages) if p != c.table[0, 0]][:1]], dtype=np.int32)
+    for m in (1, 2, 3, 6, 37, 38, 39):
+        want = sorted([30, 12, 20, *range(3, 12), *range(13, 20), *range(21, 30), *range(31, 40), 2, 1, 0][:m] if m > 2 else [30, 12][:m] if m == 2 else [12])
+        _, _, kept, _ = evict("mx4", c, 2, [L], [m], 0, 0, w, dst)
+        np.testing.assert_array_equal(kept[0, 0], want)
+
+
 @pytest.mark.parametrize("L,m", [(40000, 9000), (70001, 70000), (65536, 64), (5000, 4097)])
 def test_evict_from_long_contexts(L, m):
     check_evict("mx4", 1, 64, [L, 3], [m, 2], 4, 32, page=4096)
