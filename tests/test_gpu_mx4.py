@@ -111,7 +111,7 @@ def verify(got, a, sa, w, sw, bf16):
 
 SIZES = [(1, 1, 32), (1, 33, 64), (2, 16, 96), (16, 16, 128), (17, 31, 160), (5, 1000, 2048), (1, 4096, 4096), (31, 257, 544), (48, 130, 4128), (64, 64, 512),
          (65, 300, 256), (128, 128, 1024), (130, 515, 288), (257, 256, 2048), (300, 77, 32), (513, 641, 352), (1, 5, 8192), (1025, 31, 768), (1030, 2100, 352),
-         (3090, 4110, 544)]
+         (3090, 4110, 544), (3090, 4110, 640), (3090, 4110, 128), (1030, 2100, 384), (1030, 2100, 256)]
 
 
 @pytest.mark.parametrize("bf16", [True, False])
