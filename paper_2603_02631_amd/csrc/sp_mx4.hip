@@ -105,8 +105,23 @@ __device__ __forceinline__ uint32_t scales4(const uint8_t *row, int64_t k, int64
 
 // ---- few rows: the weights are read once ------------------------------------------------------------------------------
 
-// Sixteen weight rows and 16 MT activation rows a workgroup. Its waves take stretches of 512 elements of the rows in turn, a lane four neighbouring groups of
-// one (64 bytes, and one word of scales), and add up in LDS.
+// The scales of a lane for sixteen groups of a row from group k on: of group k + 4 s + g in the lowest byte of word s.
+struct Scales16 {
+    uint32_t w[4];
+
+    __device__ __forceinline__ void load(const uint8_t *row, int64_t k, int64_t groups, int g)
+    {
+        if (k + 16 <= groups) __builtin_memcpy(w, row + k, 16);         // at any address
+        else
+#pragma unroll
+            for (int s = 0; s < 4; ++s) w[s] = scales4(row, k + 4 * s, groups);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) w[s] >>= 8 * g;
+    }
+};
+
+// Sixteen weight rows and 16 MT activation rows a workgroup. Its waves take stretches of 512 elements of the rows in turn, four instructions of 128 (of a row a lane has
+// one group in each, so that a load takes 64 neighbouring bytes of sixteen rows), and add up in LDS.
 template <bool BF16, int MT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void sp_mx4_few_kernel(MatmulArgs p)
 {
@@ -117,30 +132,31 @@ __global__ __launch_bounds__(64 * WAVES) void sp_mx4_few_kernel(MatmulArgs p)
     f32x4 acc[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int64_t k = 16 * wave + 4 * g; k - 4 * g < groups; k += 16 * WAVES) {
-        const uint8_t *w = p.w + (n * groups + k) * 16;
+    for (int64_t k = 16 * wave; k < groups; k += 16 * WAVES) {
+        const u32x4 *w = reinterpret_cast<const u32x4 *>(p.w) + n * groups + k + g;
         u32x4 u[4];
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             u[s] = u32x4{0, 0, 0, 0};
-            if (k + s < groups) u[s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(w) + s);
+            if (k + 4 * s + g < groups) u[s] = MT == 1 ? __builtin_nontemporal_load(w + 4 * s) : w[4 * s];
         }
-        const uint32_t su = scales4(p.ws + n * groups, k, groups);
+        Scales16 su;
+        su.load(p.ws + n * groups, k, groups, g);
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
             const int64_t m = min(m0 + 16 * t + c, p.M - 1);
-            const uint8_t *a = p.a + (m * groups + k) * 16;
+            const u32x4 *a = reinterpret_cast<const u32x4 *>(p.a) + m * groups + k + g;
             u32x4 v[4];
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 v[s] = u32x4{0, 0, 0, 0};
-                if (k + s < groups) v[s] = reinterpret_cast<const u32x4 *>(a)[s];
+                if (k + 4 * s + g < groups) v[s] = a[4 * s];
             }
-            const uint32_t sv = scales4(p.as + m * groups, k, groups);
-            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(u[0]), operand(v[0]), acc[t], 4, 4, 0, (int)su, 0, (int)sv);
-            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(u[1]), operand(v[1]), acc[t], 4, 4, 1, (int)su, 1, (int)sv);
-            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(u[2]), operand(v[2]), acc[t], 4, 4, 2, (int)su, 2, (int)sv);
-            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(u[3]), operand(v[3]), acc[t], 4, 4, 3, (int)su, 3, (int)sv);
+            Scales16 sv;
+            sv.load(p.as + m * groups, k, groups, g);
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(u[s]), operand(v[s]), acc[t], 4, 4, 0, (int)su.w[s], 0, (int)sv.w[s]);
         }
     }
     if (WAVES > 1) {
@@ -174,11 +190,6 @@ __device__ __forceinline__ void load_to_lds(const uint8_t *base, uint32_t off, u
 {
     __asm__ volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(to) : "memory", "m0");
 }
-// The same with four bytes a lane.
-__device__ __forceinline__ void load_word_to_lds(const uint8_t *base, uint32_t off, uint32_t to)
-{
-    __asm__ volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" : : "v"(off), "s"(base), "s"(to) : "memory", "m0");
-}
 #pragma clang diagnostic pop
 
 // WM x WN waves, each with FM x FN blocks of 32 x 32 results: columns are activation rows m, rows weight rows n.
@@ -194,16 +205,16 @@ struct Tiled {
 };
 
 // The codes that a wave multiplies at a time: groups of 32 elements of its rows, one for each half of the wave.
-template <int FM, int FN, int ROW>
+template <int FM, int FN>
 struct Codes {
     u32x4 x[FM], y[FN];
 
     __device__ __forceinline__ void read(const uint8_t *a, const uint8_t *w, uint32_t lane)
     {
 #pragma unroll
-        for (int i = 0; i < FM; ++i) x[i] = *reinterpret_cast<const u32x4 *>(a + 32 * i * ROW + lane);
+        for (int i = 0; i < FM; ++i) x[i] = *reinterpret_cast<const u32x4 *>(a + 32 * i * kRowBytes + lane);
 #pragma unroll
-        for (int j = 0; j < FN; ++j) y[j] = *reinterpret_cast<const u32x4 *>(w + 32 * j * ROW + lane);
+        for (int j = 0; j < FN; ++j) y[j] = *reinterpret_cast<const u32x4 *>(w + 32 * j * kRowBytes + lane);
     }
 
     template <int S>
@@ -217,131 +228,18 @@ struct Codes {
     }
 };
 
-// A wave's results from (m0, n0) on go through LDS (32 rows of `mine` at a time), so that rows leave in pieces of 128 bytes and more.
-template <bool BF16, int FM, int FN>
-__device__ __forceinline__ void store_tile(const MatmulArgs &p, const f32x16 (&acc)[FM][FN], float *mine, int64_t m0, int64_t n0)
-{
-    constexpr int kPad = 32 * FN + 4;
-    const int lane = threadIdx.x & 63, h = lane >> 5, c = lane & 31;
-    constexpr int kLanes = 8 * FN;                          // of a row, four results each
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; e += 4)
-                *reinterpret_cast<f32x4 *>(mine + c * kPad + 32 * j + 2 * e + 4 * h) = f32x4{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int r = 0; r < 32; r += 64 / kLanes) {
-            const int row = r + lane / kLanes, col = 4 * (lane % kLanes);
-            const f32x4 y = *reinterpret_cast<const f32x4 *>(mine + row * kPad + col);
-            const int64_t m = m0 + 32 * i + row, n = n0 + col;
-            if (m < p.M && n < p.N) store4<BF16>(p, m, n, y);
-        }
-        __builtin_amdgcn_wave_barrier();
-    }
-}
-
-// Where a workgroup's tile begins: neighbouring tiles on one die, eight rows of tiles at a time.
-template <int TM, int TN>
-__device__ __forceinline__ void tile_of(const MatmulArgs &p, int64_t *m0, int64_t *n0)
-{
-    int x = blockIdx.x;
-    const int total = p.tiles_m * p.tiles_n, per = total / 8;
-    if (x < 8 * per) x = x % 8 * per + x / 8;
-    const int band = 8 * p.tiles_n, first = x / band * 8, deep = min(8, p.tiles_m - first);
-    *m0 = (int64_t)(first + x % band % deep) * TM;
-    *n0 = (int64_t)(x % band / deep) * TN;
-}
-
-// The same with four buffers of 128 elements of a row, three of them under way, where scales come four at a time (K a multiple of 128): the loads of a tile never run dry, while with two
-// buffers they begin anew with every step. 8192 x 8192 x 4096: PIPED_NOTE.
-template <bool BF16, int WM, int WN, int FM, int FN>
-__global__ __launch_bounds__(64 * WM * WN) void sp_mx4_piped_kernel(MatmulArgs p)
-{
-    using T = Tiled<BF16, WM, WN, FM, FN>;
-    constexpr int kBuffers = 4, kBytes = 64, kPlaces = 4, kRowsALoad = T::kThreadsT / kPlaces, kLoads = T::kRows / kRowsALoad;
-    constexpr int kCodes = T::kRows * kBytes, kScales = T::kRows * 4, kUnder = kLoads + 1;       // loads of a thread for a buffer
-    constexpr int kLds = kBuffers * (kCodes + kScales) > T::kStaged ? kBuffers * (kCodes + kScales) : T::kStaged;
-    static_assert(T::TM % kRowsALoad == 0 && T::TM % 64 == 0, "a load is of activations or of weights");
-    __shared__ alignas(16) uint8_t lds[kLds];
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = lane >> 5, c = lane & 31;
-    int64_t m0, n0;
-    tile_of<T::TM, T::TN>(p, &m0, &n0);
-    const int64_t row_bytes = p.K / 2, groups = p.K / kGroup;
-    const int steps = (int)(p.K / 128);
-
-    uint32_t off[kLoads];
-    const int piece = tid % kPlaces ^ (tid / kPlaces >> 2 & 3);          // swapped about so that sixteen lanes read sixteen places
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        const int r = tid / kPlaces + i * kRowsALoad;
-        const int64_t row = r < T::TM ? min((int64_t)r, p.M - 1 - m0) : min((int64_t)(r - T::TM), p.N - 1 - n0);
-        off[i] = (uint32_t)(row * row_bytes + 16 * piece);
-    }
-    const bool scales_of_a = 64 * wave < T::TM;
-    const uint32_t scale_off = (uint32_t)((scales_of_a ? min((int64_t)tid, p.M - 1 - m0) : min((int64_t)tid - T::TM, p.N - 1 - n0)) * groups);
-    const uint8_t *a_base = p.a + m0 * row_bytes, *w_base = p.w + n0 * row_bytes, *s_base = scales_of_a ? p.as + m0 * groups : p.ws + n0 * groups;
-    const uint32_t lds_at = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t *)lds);
-    uint8_t *const scale_lds = lds + kBuffers * kCodes;
-    const auto load = [&](int step) {
-        const int buf = step % kBuffers;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-            load_to_lds((i * kRowsALoad < T::TM ? a_base : w_base) + (int64_t)step * kBytes, off[i], lds_at + buf * kCodes + i * T::kThreadsT * 16 + wave * 1024);
-        load_word_to_lds(s_base + (int64_t)step * 4, scale_off, lds_at + kBuffers * kCodes + buf * kScales + wave * 256);
-    };
-
-    f32x16 acc[FM][FN];
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    const int wm = wave / WN, wn = wave % WN;
-    const int row_a = 32 * FM * wm + c, row_w = T::TM + 32 * FN * wn + c;
-    uint32_t at[2];             // a lane's place in its row: half h takes groups 2h and 2h + 1 of a step
-#pragma unroll
-    for (int s = 0; s < 2; ++s) at[s] = 16 * ((2 * h + s) ^ (c >> 2 & 3));
-
-    for (int step = 0; step < min(kBuffers - 1, steps); ++step) load(step);
-    for (int step = 0; step < steps; ++step) {
-        // this step's loads of this wave are there, then those of all waves, who are done with the buffer before it
-        if (step + 2 < steps) __asm__ volatile("s_waitcnt vmcnt(%0)" : : "i"(2 * kUnder) : "memory");
-        else if (step + 1 < steps) __asm__ volatile("s_waitcnt vmcnt(%0)" : : "i"(kUnder) : "memory");
-        else __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        __asm__ volatile("" ::: "memory");
-        if (step + kBuffers - 1 < steps) load(step + kBuffers - 1);
-        const int buf = step % kBuffers;
-        const uint8_t *a = lds + buf * kCodes + row_a * kBytes, *w = lds + buf * kCodes + row_w * kBytes;
-        uint32_t sa[FM], sw[FN];
-        Codes<FM, FN, kBytes> even, odd;
-        even.read(a, w, at[0]);
-#pragma unroll
-        for (int i = 0; i < FM; ++i) sa[i] = *reinterpret_cast<const uint32_t *>(scale_lds + buf * kScales + (row_a + 32 * i) * 4) >> (16 * h);
-#pragma unroll
-        for (int j = 0; j < FN; ++j) sw[j] = *reinterpret_cast<const uint32_t *>(scale_lds + buf * kScales + (row_w + 32 * j) * 4) >> (16 * h);
-        odd.read(a, w, at[1]);
-        __builtin_amdgcn_sched_barrier(0);
-        even.template multiply<0>(acc, sa, sw);
-        odd.template multiply<1>(acc, sa, sw);
-        __builtin_amdgcn_sched_barrier(0);                  // products before the wait
-    }
-    __syncthreads();
-    store_tile<BF16, FM, FN>(p, acc, reinterpret_cast<float *>(lds) + wave * 32 * T::kPad, m0 + 32 * FM * wm, n0 + 32 * FN * wn);
-}
-
 template <bool BF16, int WM, int WN, int FM, int FN>
 __global__ __launch_bounds__(64 * WM * WN) void sp_mx4_tiled_kernel(MatmulArgs p)
 {
     using T = Tiled<BF16, WM, WN, FM, FN>;
     __shared__ alignas(16) uint8_t lds[T::kLds];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = lane >> 5, c = lane & 31;
-    int64_t m0, n0;
-    tile_of<T::TM, T::TN>(p, &m0, &n0);
+    // neighbouring tiles on one die: eight rows of tiles at a time
+    int x = blockIdx.x;
+    const int total = p.tiles_m * p.tiles_n, per = total / 8;
+    if (x < 8 * per) x = x % 8 * per + x / 8;
+    const int band = 8 * p.tiles_n, first = x / band * 8, deep = min(8, p.tiles_m - first);
+    const int64_t m0 = (int64_t)(first + x % band % deep) * T::TM, n0 = (int64_t)(x % band / deep) * T::TN;
     const int64_t row_bytes = p.K / 2, groups = p.K / kGroup;
     const int steps = (int)((p.K + kStep - 1) / kStep), rest = (int)(p.K % kStep);       // elements of the last step, 0: all
 
@@ -407,7 +305,7 @@ __global__ __launch_bounds__(64 * WM * WN) void sp_mx4_tiled_kernel(MatmulArgs p
 #pragma unroll
         for (int j = 0; j < FN; ++j) sw[j] = *reinterpret_cast<const uint32_t *>(scale_lds + buf * T::kScales + (row_w + 32 * j) * kStepGroups + 4 * h);
         // codes are read one group of products ahead; the scheduling barriers keep them from being read later, or further ahead, for which there are no registers
-        Codes<FM, FN, kRowBytes> even, odd;
+        Codes<FM, FN> even, odd;
         even.read(a, w, at[0]);
         odd.read(a, w, at[1]);
         __builtin_amdgcn_sched_barrier(0);
@@ -426,7 +324,26 @@ __global__ __launch_bounds__(64 * WM * WN) void sp_mx4_tiled_kernel(MatmulArgs p
         __syncthreads();
     }
 
-    store_tile<BF16, FM, FN>(p, acc, reinterpret_cast<float *>(lds) + wave * 32 * T::kPad, m0 + 32 * FM * wm, n0 + 32 * FN * wn);
+    // A wave's results go through LDS, 32 rows at a time, so that rows leave in pieces of 128 bytes and more.
+    float *mine = reinterpret_cast<float *>(lds) + wave * 32 * T::kPad;
+    constexpr int kLanes = 8 * FN;                          // of a row, four results each
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<f32x4 *>(mine + c * T::kPad + 32 * j + 2 * e + 4 * h) = f32x4{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int r = 0; r < 32; r += 64 / kLanes) {
+            const int row = r + lane / kLanes, col = 4 * (lane % kLanes);
+            const f32x4 y = *reinterpret_cast<const f32x4 *>(mine + row * T::kPad + col);
+            const int64_t m = m0 + 32 * (FM * wm + i) + row, n = n0 + 32 * FN * wn + col;
+            if (m < p.M && n < p.N) store4<BF16>(p, m, n, y);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
 }
 
 template <bool BF16, int WM, int WN, int FM, int FN>
@@ -435,9 +352,7 @@ sp_status tiled(MatmulArgs p, hipStream_t st)
     using T = Tiled<BF16, WM, WN, FM, FN>;
     p.tiles_m = (int32_t)sp::ceil_div(p.M, T::TM);
     p.tiles_n = (int32_t)sp::ceil_div(p.N, T::TN);
-    const dim3 grid((unsigned)(p.tiles_m * p.tiles_n));
-    if (p.K % 128 == 0) hipLaunchKernelGGL((sp_mx4_piped_kernel<BF16, WM, WN, FM, FN>), grid, dim3(T::kThreadsT), 0, st, p);
-    else hipLaunchKernelGGL((sp_mx4_tiled_kernel<BF16, WM, WN, FM, FN>), grid, dim3(T::kThreadsT), 0, st, p);
+    hipLaunchKernelGGL((sp_mx4_tiled_kernel<BF16, WM, WN, FM, FN>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(T::kThreadsT), 0, st, p);
     SP_HIP_CHECK(hipGetLastError());
     return SP_OK;
 }
@@ -457,9 +372,11 @@ sp_status run(const MatmulArgs &p, hipStream_t st)
 {
     if (p.M <= 16) return few<BF16, 1>(p, st);
     if (p.M <= 32) return few<BF16, 2>(p, st);
+    // Tiles take as long however few they are (0.45 us for 128 elements of K), the workgroups for few rows as long as what they read from L2, by turns (us, few rows' and tiles'):
+    // 128 x 4096 x 4096 (32 tiles) 14 and 17, 700 x 300 x 4000 (18) 9 and 22; 2048 x 500 x 2048 (64) 13 and 11, 256 x 4096 x 4096 (64) 25 and 18, 632 x 2025 x 224 (80) 12 and 7
     if (p.K <= kMostTiledK) {
         if (sp::ceil_div(p.M, 256) * sp::ceil_div(p.N, 256) >= 192) return tiled<BF16, 2, 4, 4, 2>(p, st);
-        if (sp::ceil_div(p.M, 128) * sp::ceil_div(p.N, 128) >= 128) return tiled<BF16, 2, 2, 2, 2>(p, st);
+        if (sp::ceil_div(p.M, 128) * sp::ceil_div(p.N, 128) >= 48) return tiled<BF16, 2, 2, 2, 2>(p, st);
     }
     return few<BF16, 4>(p, st);
 }
