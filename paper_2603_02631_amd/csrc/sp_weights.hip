@@ -85,13 +85,14 @@ __global__ __launch_bounds__(kThreads) void sp_weights_few_kernel(WeightArgs a)
     // this lane's part of row c for the products, and what it needs of the rows whose results it holds: 4 (g % LIVE) .. + 3
     bf16x8 q[kSteps];
     {
-        const int token = c / G, head = kvh * G + c % G;
-        const uint16_t *src = a.q + ((a.off[b] + token) * a.c.n_q_heads + head) * D;
+        // rows that are not there are copies of row 0: a key that makes its logit minus infinity makes theirs no NaN
+        const int r = c < rows ? c : 0;
+        const uint16_t *src = a.q + ((a.off[b] + r / G) * a.c.n_q_heads + kvh * G + r % G) * D;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             const int e = MX4 ? D / 4 * g + 8 * s : E4M3 ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;
             u32x4 w = {0, 0, 0, 0};
-            if (c < rows) w = *reinterpret_cast<const u32x4 *>(src + e);
+            if (rows > 0) w = *reinterpret_cast<const u32x4 *>(src + e);
             q[s] = __builtin_bit_cast(bf16x8, w);
         }
     }
@@ -106,9 +107,9 @@ __global__ __launch_bounds__(kThreads) void sp_weights_few_kernel(WeightArgs a)
         ref[j] = __builtin_huge_valf();
         if (r < rows) ref[j] = reference(a.lse[(a.off[b] + r / G) * a.c.n_q_heads + kvh * G + r % G]);
     }
-    // every row sees the keys of [all_lo, all_hi)
+    // every row sees the keys of [all_lo, all_hi); a request without rows has none that does
     const int all_lo = a.causal && a.window > 0 && rg.len - a.window > 0 ? rg.len - a.window : 0;
-    const int all_hi = a.causal ? rg.len - rg.n + 1 : rg.len;
+    const int all_hi = rows == 0 ? 0 : a.causal ? rg.len - rg.n + 1 : rg.len;
 
     const Line line(a, b, kvh, KIND, D);
     const uint32_t k_lane = MX4 ? 2 * c * line.row_bytes + D / 8 * g : c * line.row_bytes + 16 * g;
@@ -163,8 +164,9 @@ __global__ __launch_bounds__(kThreads) void sp_weights_few_kernel(WeightArgs a)
             float p[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (!whole && (key < first[j] || key >= last[j])) y[j] = neg_inf();
-                p[j] = exp2_(y[j] * f - ref[j]);
+                float x = y[j] * f - ref[j];
+                if (!whole && (key < first[j] || key >= last[j])) x = neg_inf();        // whatever the key and its block's scale are
+                p[j] = exp2_(x);
             }
             return (p[0] + p[1]) + (p[2] + p[3]);
         };
@@ -276,10 +278,9 @@ __global__ __launch_bounds__(kThreads, 4) void sp_weights_many_kernel(WeightArgs
     const auto fetch = [&](int tile) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int x = tid + i * kThreads, r = tile * kManyRows + x / kChunks;
-            next[i] = u32x4{0, 0, 0, 0};
-            if (r < rows)
-                next[i] = reinterpret_cast<const u32x4 *>(a.q + ((a.off[b] + r / G) * a.c.n_q_heads + kvh * G + r % G) * D)[x % kChunks];
+            // behind the last row copies of it, which add nothing
+            const int x = tid + i * kThreads, r = min(tile * kManyRows + x / kChunks, rows - 1);
+            next[i] = reinterpret_cast<const u32x4 *>(a.q + ((a.off[b] + r / G) * a.c.n_q_heads + kvh * G + r % G) * D)[x % kChunks];
         }
         if (tid < kManyRows) {
             const int r = tile * kManyRows + tid;
@@ -324,6 +325,9 @@ __global__ __launch_bounds__(kThreads, 4) void sp_weights_many_kernel(WeightArgs
         const int t_lo = tile * kManyRows / G, t_hi = min(tile * kManyRows + kManyRows - 1, rows - 1) / G;
         const int all_hi = a.causal ? rg.len - rg.n + t_lo + 1 : rg.len, all_lo = a.causal && a.window > 0 ? rg.len - rg.n + t_hi + 1 - a.window : 0;
         const bool whole = key0 >= all_lo && key0 + kManyKeys <= all_hi;
+        float f[W];
+#pragma unroll
+        for (int w = 0; w < W; ++w) f[w] = whole ? factor[w] : 1.f;
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) {                                // rows 8 e4 + 4 h + e
             const f32x4 ref = *reinterpret_cast<const f32x4 *>(&ref_lds[buf][8 * e4 + 4 * h]);
@@ -334,14 +338,14 @@ __global__ __launch_bounds__(kThreads, 4) void sp_weights_many_kernel(WeightArgs
 #pragma unroll
                     for (int w = 0; w < W; ++w) {
                         const int key = key0 + 32 * w + c;
-                        if (key < first || key >= last) x[w][4 * e4 + e] = neg_inf();
+                        x[w][4 * e4 + e] = key < first || key >= last ? neg_inf() : x[w][4 * e4 + e] * factor[w];    // whatever the key and its block's scale are
                     }
                 }
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 float p[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) p[e] = exp2_(x[w][4 * e4 + e] * factor[w] - ref[e]);
+                for (int e = 0; e < 4; ++e) p[e] = exp2_(x[w][4 * e4 + e] * f[w] - ref[e]);
                 sum[w] += (p[0] + p[1]) + (p[2] + p[3]);
             }
         }

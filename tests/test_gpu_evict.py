@@ -160,6 +160,73 @@ def test_a_nan_in_an_lse_gets_out(kind, n):
     assert np.isnan(got[0, 0, :101 - n]).all() and np.isfinite(got[0, 1]).all() and np.isfinite(got[1]).all()
 
 
+@pytest.mark.parametrize("H,kv,d", [(3, 1, 64), (6, 2, 128), (5, 1, 64)])
+@pytest.mark.parametrize("n", [1, 3, 15])
+def test_weights_where_a_logit_is_minus_infinity(H, kv, d, n):
+    """Such a key draws nothing from any row; rows that fill up a tile of them must not make NaN of it."""
+    c, held, off, q = filled("bf16", H, kv, d, [n], [300], 64)
+    q[..., 0] = -np.abs(q[..., 0]) - 1
+    at = [0, 37, 128, 250]
+    pool = c.k.copy()
+    for j in at:
+        for h in range(kv):
+            pool[c.at(0, h, j)] = 0x7f80
+    lse = np.zeros((n, H), dtype=np.float32)
+    old, got = torch.rand(1, kv, 300, device=DEV), []
+    for keys in (c.k, pool):
+        w = torch.full((1, kv, 300), 7.5, device=DEV)
+        sp.sp_attend_weights(desc_of(c, H, "bf16"), dev(ou.bf16_bits(q)), [0, n], dev(off), dev(np.array([300], dtype=np.int32)), 300, dev(c.table), dev(keys), None,
+                             0.125, dev(lse), old, w, causal=0)
+        got.append(w.cpu())
+    want = got[0].clone()
+    want[:, :, at] = old.cpu()[:, :, at]
+    assert torch.equal(got[1], want)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("other", [1, 40])
+def test_a_request_without_rows_keeps_its_weights_whatever_its_keys(kind, other):
+    c, held, off, q = filled(kind, 4, 2, 64, [0, other, 0], [130, 90, 64], 32)
+    if kind == "bf16":
+        keys, scales = c.k.copy(), None
+        for b, L in ((0, 130), (2, 64)):
+            for j in range(L):
+                for h in range(2):
+                    keys[c.at(b, h, j):c.at(b, h, j) + 64] = 0x7fc0
+    else:
+        keys, scales = c.k, c.ks.copy()
+        for b, L in ((0, 130), (2, 64)):
+            scales[c.table[b, :-(-L // 32)]] = 255 if kind == "mx4" else np.nan
+    before = torch.rand(3, 2, 130, device=DEV)
+    w = before.clone()
+    sp.sp_attend_weights(desc_of(c, 4, kind), dev(ou.bf16_bits(q)), off.tolist(), dev(off), dev(np.array([130, 90, 64], dtype=np.int32)), 130, dev(c.table), dev(keys),
+                         None if scales is None else dev(scales), 0.125, dev(np.zeros((other, 4), dtype=np.float32)), w, w)
+    assert torch.equal(w[0], before[0]) and torch.equal(w[2], before[2]) and bool(torch.isfinite(w).all()) and not torch.equal(w[1], before[1])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n", [1, 40])
+def test_weights_of_keys_behind_a_window_whose_pages_hold_anything(kind, n):
+    """A window's caller may have given their pages away: nothing of them gets into the weights, which stay what they were."""
+    c, held, off, q = filled(kind, 4, 2, 64, [n], [300], 32)
+    keys, scales = c.k.copy(), None if kind == "bf16" else c.ks.copy()
+    lse, before, got = dev(np.zeros((n, 4), dtype=np.float32)), torch.rand(1, 2, 300, device=DEV), []
+    for spoilt in (False, True):
+        if spoilt:
+            for page in range(5):                       # tokens before 160; the first row sees tokens from 300 - n - 50 + 1 > 200 on
+                if kind == "bf16":
+                    for j in range(32 * page, 32 * page + 32):
+                        for h in range(2):
+                            keys[c.at(0, h, j):c.at(0, h, j) + 64] = 0x7fc0
+                else:
+                    scales[c.table[0, page]] = 255 if kind == "mx4" else np.nan
+        w = before.clone()
+        sp.sp_attend_weights(desc_of(c, 4, kind), dev(ou.bf16_bits(q)), [0, n], dev(off), dev(np.array([300], dtype=np.int32)), 300, dev(c.table), dev(keys),
+                             None if scales is None else dev(scales), 0.125, lse, w, w, causal=1, window=50)
+        got.append(w)
+    assert torch.equal(got[0], got[1]) and torch.equal(got[1][..., :160], before[..., :160]) and not torch.equal(got[1], before)
+
+
 # ---- eviction --------------------------------------------------------------------------------------------------------
 
 def choice(w, L, m, sinks, recent):
