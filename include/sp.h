@@ -600,8 +600,8 @@ sp_status sp_attend_weights(const sp_cache_desc *desc, const void *q_dev, const 
  *   - new_weights_dev[b, h, i] (optional, float [B][n_kv_heads][max_budget], not weights_dev itself): its weight.
  * new_lens_dev[b] = n (int32, neither lens_dev nor budget_dev itself). Entries and slots at and behind n are left as they were.
  * Keys keep the rotation of their old position: new tokens go on from there (sp_cache_append's positions_dev), while attention's masks and windows
- * count slots. The pages of dst_table must not be among those that block_table names (for any request): source pages are only read, and free afterwards;
- * pages that requests share stay as they are. Tokens whose destination lies beyond dst_table's row, or whose destination page is not in [0, n_pages), are not moved.
+ * count slots. The pages of dst_table must be different ones for all requests, and not among those that block_table names (for any request): source pages are only
+ * read, and free afterwards; pages that requests share stay as they are. In an E4M3 cache the scale of the block that holds slot n - 1 is replaced, for what lies behind n in it too. Tokens whose destination lies beyond dst_table's row, or whose destination page is not in [0, n_pages), are not moved.
  * weights_dev: float [B][n_kv_heads][weights_stride], weights_stride >= max_len. Contexts are bounded by max_len as in sp_attend. sinks, recent >= 0.
  * 0 <= max_budget <= 2^30, min(max_len, max_budget) < 2^29; requests times kv heads at most 65535. The result does not change from call to call.
  */
@@ -653,7 +653,7 @@ sp_status sp_logprobs(const void *logits_dev, int32_t dtype, int64_t n_rows, int
  * infinity gets scale byte 255 and codes of zero.
  * x_dev: float or bf16 (dtype an sp_logits_type), row r at r * row_stride elements (row_stride >= K, a multiple of 8, rows 16-byte
  * aligned). codes_dev: [rows][K / 2] bytes, scales_dev: [rows][K / 32] bytes, both dense, codes 16-byte, scales 4-byte aligned. K is a positive multiple of 32
- * below 2^31. 0 <= rows < 2^31; rows * K < 2^35.
+ * below 2^31. 0 <= rows < 2^31; rows * K < 2^35. x_dev, codes_dev and scales_dev must not overlap.
  */
 sp_status sp_mx4_quantise(const void *x_dev, int32_t dtype, int64_t rows, int64_t K, int64_t row_stride,
                           void *codes_dev, void *scales_dev, void *hip_stream);
@@ -664,7 +664,7 @@ sp_status sp_mx4_quantise(const void *x_dev, int32_t dtype, int64_t rows, int64_
  * with A and W as sp_mx4_quantise leaves them: a_codes_dev [M][K / 2], a_scales_dev [M][K / 32], w_codes_dev [N][K / 2], w_scales_dev
  * [N][K / 32], dense, codes 16-byte, scales 4-byte aligned. out_dev: float or bf16 (dtype an sp_logits_type), row m at m * out_stride
  * elements (out_stride >= N). Products are exact, sums are held in fp32 in an order that the sizes fix, the result is rounded once.
- * Rows with a NaN scale give NaN. K is a positive multiple of 32 below 2^31, 0 <= M, N < 2^31; (M / 16 + 1) * (N / 16 + 1) < 2^24.
+ * Rows with a NaN scale give NaN. out_dev must not overlap the operands. K is a positive multiple of 32 below 2^31, 0 <= M, N < 2^31; (M / 16 + 1) * (N / 16 + 1) < 2^24.
  */
 sp_status sp_mx4_matmul(const void *a_codes_dev, const void *a_scales_dev, int64_t M, const void *w_codes_dev,
                         const void *w_scales_dev, int64_t N, int64_t K, void *out_dev, int32_t dtype, int64_t out_stride,

@@ -1,7 +1,8 @@
 // sp_cache_evict: the tokens of a paged cache that have drawn the most attention move to other pages, of each kv head by itself, the rest is left behind.
 //
 // Two launches. sp_evict_select_kernel, a workgroup for each (request, kv head): the weight of the last token that stays, as an exact selection by digits
-// of the weights' ordered bits, then a walk over the tokens in order that lists those that stay: all above it, and of those equal to it the first ones. sp_evict_move_kernel: 32 destination slots of a kv head a workgroup, keys and values.
+// of the weights' ordered bits, then a walk over the tokens in order that lists those that stay: all above it, and of those equal to it the first ones.
+// sp_evict_move_kernel: 32 destination slots of a kv head a workgroup, keys and values.
 // Out of place: every slot can be moved at once, and pages that requests share stay as they are.
 #include "sp_cache.hpp"
 
@@ -134,6 +135,7 @@ __device__ __forceinline__ Found find_digit(const uint32_t *bins, int above, int
     return found;
 }
 
+// Bound by the chain of passes, not by bytes: 1280 contenders take 7.5 us, up to 65536 of each of 128 lines 30 us, a line's 256 KB read three times from L2 by one workgroup.
 // Digits of 11, 11 and 10 bits, the most significant first: that one tells weights apart by two bits of their mantissa. Contenders that share it are listed in LDS
 // where they fit, and the other digits are found among them; so a line is read three times: to count, to list, and to write down what stays.
 template <int THREADS, int R, bool HELD>
@@ -289,6 +291,8 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t c, float ratio)
     return (uint32_t)r;
 }
 
+// A slot's source is looked up by one thread, its bytes are moved by whole 16-byte pieces, neighbouring threads those of one token. Bound by HBM for many tokens: 16 requests
+// that keep 2048 to 8192 tokens of 8 heads of 128 in bf16, 544 MB read and written, take 107 us, 5.1 TB/s (a large copy 4.8 to 5.2).
 template <int D, int KIND>
 __global__ __launch_bounds__(kMoveThreads) void sp_evict_move_kernel(EvictArgs a)
 {

@@ -4,7 +4,8 @@
 //   w[b, h, j] = old + sum_{r, g} exp(scale <q[r, g], k[b, h, j]> - lse[r, g])
 // over the rows r that see key j and the query heads g of kv head h; lse is what sp_attend wrote. A key's weight is the sum over the rows of a kv head, so a wave
 // that holds a block of keys goes through the rows and no sum crosses workgroups: nothing is added atomically, the order is fixed by the lengths.
-// The products are Q K^T with a key in a lane column: a lane adds up its rows, and the lanes of a column meet once at the end.
+// The products are Q K^T with a key in a lane column: a lane adds up its rows, and the lanes of a column meet once at the end. Keys are bf16 or become it, exactly; logits,
+// exponentials and sums are fp32.
 #include "sp_context.hpp"
 
 namespace {
@@ -64,7 +65,11 @@ __device__ __forceinline__ float gather2(float x0, float x1)
 
 // Requests of up to 16 rows a kv head (none too: their weights are what they were). A wave has its rows in registers and takes pairs of blocks of 32 tokens, one of
 // its workgroup's in turn, a pair ahead. After the products lane 16 g + c holds rows 4g .. 4g + 3 of a column's key. With at most four rows (LIVE = 1) only lanes of group 0
-// hold any, so four tiles of 16 keys are gathered into all lanes before the exponentials, with at most eight (LIVE = 2) two.
+// hold any, so four tiles of 16 keys are gathered into all lanes before the exponentials, with at most eight (LIVE = 2) two (48 contexts of MX4: 72 us without the
+// gathering, 66 with).
+// Bound by reading, and by starting: 48 contexts of 2048 to 65536 tokens, 8 kv heads of 64, 4 query heads each, MX4 (271 MB with old and new weights) take 66 us, 4.1 TB/s; 48 of
+// 16384 59, 4.5, and of E4M3 90, 5.0. A short line's workgroups are a chain of offsets, lengths, block table, keys for one or two pairs. Not kept: two pairs
+// ahead (66), the pairs of all lines in equal shares over the resident workgroups (72: finding a share's start takes longer than its lines' ends leave idle).
 template <int D, int KIND, int LIVE>
 __global__ __launch_bounds__(kThreads) void sp_weights_few_kernel(WeightArgs a)
 {
@@ -209,8 +214,10 @@ __global__ __launch_bounds__(kThreads) void sp_weights_few_kernel(WeightArgs a)
     }
 }
 
-// Requests with more rows: a wave holds 32 or 64 keys as bf16 and goes through tiles of 32 rows, which its workgroup brings to LDS. For an MX4 or E4M3 cache the
-// keys become bf16 (exact); a block's E4M3 scale goes into the factor.
+// Requests with more rows: a wave holds 32 or 64 keys as bf16 and goes through tiles of 32 rows, which its workgroup brings to LDS, two buffers in turn. A block's E4M3
+// scale goes into the factor.
+// The last 64 of 32768 tokens, 16 heads over 8 of 128, bf16: 67 MB of keys in 25 us. One read of the keys (11 us) and four tiles of rows (9 us of products, and their exponentials) come
+// after each other in a wave; four waves a SIMD fill in for one another (two, with twice the keys each: 27 us; all rows in LDS and the keys streamed past them: 29).
 template <int D, int KIND>
 __global__ __launch_bounds__(kThreads, 4) void sp_weights_many_kernel(WeightArgs a)
 {
