@@ -537,15 +537,15 @@ def _rows(t, what: str, rows: int, width: int, stride: Optional[int], known: set
     return t.data_ptr(), (strides[0] if rows > 1 else (width + 7) & ~7)
 
 
-def _table(block_table, B: int, table_stride: Optional[int]):
+def _table(block_table, B: int, table_stride: Optional[int], what: str = "block_table"):
     """(address, entries of a request) of a dense [B][table_stride] int32 block table."""
     if isinstance(block_table, int) or block_table is None:
         return block_table, 0 if table_stride is None else table_stride
     if table_stride is None:
         if block_table.dim() != 2:
-            raise SpError(1, "block_table has to be [requests][entries]")
+            raise SpError(1, f"{what} has to be [requests][entries]")
         table_stride = block_table.shape[1]
-    return _typed(block_table, "block_table", 4 * B * table_stride, _INT32), table_stride
+    return _typed(block_table, what, 4 * B * table_stride, _INT32), table_stride
 
 
 _desc_fields = struct.Struct("4i5q").unpack_from        # all fields at once: half of what reading them one by one takes
@@ -697,7 +697,7 @@ def sp_cache_evict(desc: CacheDesc, lens, max_len: int, budget, max_budget: int,
         B = lens.numel()
     n = max(B, 0)
     tab, width = _table(block_table, n, table_stride)
-    dst, dst_width = _table(dst_table, n, dst_stride)
+    dst, dst_width = _table(dst_table, n, dst_stride, "dst_table")
     _, kv, _, elems, of_scales, pool, scales = _cache_bytes(desc)
     entries = _line_stride(weights, "weights", n * kv, max_len, weights_stride)
     held = 4 * n * kv * max(max_budget, 0)

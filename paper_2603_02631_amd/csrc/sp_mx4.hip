@@ -244,7 +244,8 @@ __global__ __launch_bounds__(64 * WM * WN) void sp_mx4_tiled_kernel(MatmulArgs p
     const int total = p.tiles_m * p.tiles_n, per = total / 8;
     if (x < 8 * per) x = x % 8 * per + x / 8;
     const int band = 8 * p.tiles_n, first = x / band * 8, deep = min(8, p.tiles_m - first);
-    const int64_t m0 = (int64_t)(first + x % band % deep) * T::TM, n0 = (int64_t)(x % band / deep) * T::TN;
+    // the quotients come from vector operations: as scalars, so that the addresses made of them are scalars however little is optimised
+    const int64_t m0 = (int64_t)__builtin_amdgcn_readfirstlane(first + x % band % deep) * T::TM, n0 = (int64_t)__builtin_amdgcn_readfirstlane(x % band / deep) * T::TN;
     const int64_t row_bytes = p.K / 2, groups = p.K / kGroup;
     const int steps = (int)((p.K + kStep - 1) / kStep), rest = (int)(p.K % kStep);       // elements of the last step, 0: all
 
