@@ -574,7 +574,7 @@ sp_status sp_attend(const sp_cache_desc *desc, const void *q_dev,
  * weights_stride >= max_len. old = old_dev[b, h, j] (the same layout; may be weights_dev itself, else they must not overlap) for
  * tokens that were there before the rows' own: j < lens[b] - n_b with causal = 1, all with causal = 0; 0 for the others
  * and where old_dev is null. A request without rows keeps its old weights. Rows with an lse of minus infinity add nothing.
- * Arithmetic is in fp32, in an order that is fixed by the lengths.
+ * Arithmetic is in fp32, in an order that is fixed by the offsets, the lengths and max_len.
  * A row that sees a NaN, or whose lse is NaN, makes NaN of the weights that it adds to, and of others of its request.
  * Limits as in sp_attend; requests times kv heads at most 65535.
  */

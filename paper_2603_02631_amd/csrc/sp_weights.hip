@@ -14,6 +14,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kFewRows = 16;            // rows of a kv head that sp_weights_few_kernel takes at most
 constexpr int kManyRows = 32;           // rows of a tile of sp_weights_many_kernel
+constexpr int64_t kUnits = 256;         // compute units
 constexpr int many_blocks(int d) { return 128 / d; }    // blocks of 32 keys of a wave there: as many as leave four waves a SIMD their registers
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
@@ -215,19 +216,20 @@ __global__ __launch_bounds__(kThreads) void sp_weights_few_kernel(WeightArgs a)
 }
 
 // Requests with more rows: a wave holds 32 or 64 keys as bf16 and goes through tiles of 32 rows, which its workgroup brings to LDS, two buffers in turn. A block's E4M3
-// scale goes into the factor.
+// scale goes into the factor. R fours of waves have the same keys and take the tiles in turn; their sums are added in their order.
 // The last 64 of 32768 tokens, 16 heads over 8 of 128, bf16: 67 MB of keys in 25 us. One read of the keys (11 us) and four tiles of rows (9 us of products, and their exponentials) come
 // after each other in a wave; four waves a SIMD fill in for one another (two, with twice the keys each: 27 us; all rows in LDS and the keys streamed past them: 29).
-template <int D, int KIND>
-__global__ __launch_bounds__(kThreads, 4) void sp_weights_many_kernel(WeightArgs a)
+template <int D, int KIND, int R>
+__global__ __launch_bounds__(kThreads * R, 4) void sp_weights_many_kernel(WeightArgs a)
 {
     constexpr bool E4M3 = KIND == SP_CACHE_E4M3, MX4 = KIND == SP_CACHE_MX4;
     constexpr int kSteps = D / 16, kChunks = D / 8, kLoads = kManyRows * kChunks / kThreads;     // 16-byte pieces of a row; of a thread
     constexpr int kKeyLoads = (int)sp::cache_bytes(KIND, D) / 32;                       // 16-byte loads of half a key's row
     constexpr int W = many_blocks(D), kManyKeys = 32 * W;
-    __shared__ u32x4 rows_lds[2][kManyRows * kChunks];
-    __shared__ float ref_lds[2][kManyRows];
-    __shared__ int first_lds[2][kManyRows], last_lds[2][kManyRows];
+    __shared__ u32x4 rows_lds[2][R][kManyRows * kChunks];
+    __shared__ float ref_lds[2][R][kManyRows];
+    __shared__ int first_lds[2][R][kManyRows], last_lds[2][R][kManyRows];
+    __shared__ float sum_lds[R][kWaves][kManyKeys];
 
     const int b = blockIdx.y / a.c.n_kv_heads, kvh = blockIdx.y % a.c.n_kv_heads, G = a.c.group;
     const Range rg = range_of(a, b);
@@ -235,7 +237,9 @@ __global__ __launch_bounds__(kThreads, 4) void sp_weights_many_kernel(WeightArgs
     const int key_wg = blockIdx.x * kWaves * kManyKeys;
     if (rows64 <= kFewRows || key_wg >= rg.len) return;
     const int rows = (int)rows64;
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = lane >> 5, c = lane & 31;
+    // four waves have the keys, R fours of them a tile of rows each
+    const int tid = threadIdx.x % kThreads, wave = __builtin_amdgcn_readfirstlane(tid >> 6), four = __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+    const int lane = tid & 63, h = lane >> 5, c = lane & 31;
     const int key0 = key_wg + wave * kManyKeys, older = older_of(a, rg);
     const int64_t line_at = ((int64_t)b * a.c.n_kv_heads + kvh) * a.stride;
     const float scale2 = a.scale * kLog2e;
@@ -300,23 +304,16 @@ __global__ __launch_bounds__(kThreads, 4) void sp_weights_many_kernel(WeightArgs
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int x = tid + i * kThreads;
-            rows_lds[buf][slot(x / kChunks, x % kChunks)] = next[i];
+            rows_lds[buf][four][slot(x / kChunks, x % kChunks)] = next[i];
         }
         if (tid < kManyRows) {
-            ref_lds[buf][tid] = next_ref;
-            first_lds[buf][tid] = next_seen.first;
-            last_lds[buf][tid] = next_seen.last;
+            ref_lds[buf][four][tid] = next_ref;
+            first_lds[buf][four][tid] = next_seen.first;
+            last_lds[buf][four][tid] = next_seen.last;
         }
     };
     float sum[W] = {};
-    if (tile0 < tiles) {
-        fetch(tile0);
-        put(0);
-        __syncthreads();
-    }
-    for (int tile = tile0; tile < tiles; ++tile) {
-        const int buf = (tile - tile0) & 1;
-        if (tile + 1 < tiles) fetch(tile + 1);
+    const auto multiply = [&](int tile, int buf) {
         f32x16 x[W];
 #pragma unroll
         for (int w = 0; w < W; ++w)
@@ -324,7 +321,7 @@ __global__ __launch_bounds__(kThreads, 4) void sp_weights_many_kernel(WeightArgs
             for (int e = 0; e < 16; ++e) x[w][e] = 0.f;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-            const bf16x8 q = __builtin_bit_cast(bf16x8, rows_lds[buf][slot(c, piece(s))]);
+            const bf16x8 q = __builtin_bit_cast(bf16x8, rows_lds[buf][four][slot(c, piece(s))]);
 #pragma unroll
             for (int w = 0; w < W; ++w) x[w] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, k[w][s], x[w], 0, 0, 0);
         }
@@ -337,11 +334,11 @@ __global__ __launch_bounds__(kThreads, 4) void sp_weights_many_kernel(WeightArgs
         for (int w = 0; w < W; ++w) f[w] = whole ? factor[w] : 1.f;
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) {                                // rows 8 e4 + 4 h + e
-            const f32x4 ref = *reinterpret_cast<const f32x4 *>(&ref_lds[buf][8 * e4 + 4 * h]);
+            const f32x4 ref = *reinterpret_cast<const f32x4 *>(&ref_lds[buf][four][8 * e4 + 4 * h]);
             if (!whole)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int r = 8 * e4 + 4 * h + e, first = first_lds[buf][r], last = last_lds[buf][r];
+                    const int r = 8 * e4 + 4 * h + e, first = first_lds[buf][four][r], last = last_lds[buf][four][r];
 #pragma unroll
                     for (int w = 0; w < W; ++w) {
                         const int key = key0 + 32 * w + c;
@@ -356,18 +353,39 @@ __global__ __launch_bounds__(kThreads, 4) void sp_weights_many_kernel(WeightArgs
                 sum[w] += (p[0] + p[1]) + (p[2] + p[3]);
             }
         }
-        if (tile + 1 < tiles) put(buf ^ 1);
+    };
+    if (tile0 + four < tiles) {
+        fetch(tile0 + four);
+        put(0);
+    }
+    __syncthreads();
+    for (int at = tile0, buf = 0; at < tiles; at += R, buf ^= 1) {
+        const int tile = at + four;
+        if (tile + R < tiles) fetch(tile + R);
+        if (tile < tiles) multiply(tile, buf);
+        if (tile + R < tiles) put(buf ^ 1);
         __syncthreads();
     }
 #pragma unroll
     for (int w = 0; w < W; ++w) sum[w] += __shfl_xor(sum[w], 32);
+    if constexpr (R > 1) {                                  // the fours' sums, in their order
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+            if (h == 0) sum_lds[four][wave][32 * w + c] = sum[w];
+        __syncthreads();
+        if (four != 0) return;
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+#pragma unroll
+            for (int i = 1; i < R; ++i) sum[w] += sum_lds[i][wave][32 * w + c];
+    }
     const int key = key0 + 32 * (W == 2 ? h : 0) + c;
     if (key < rg.len && (W == 2 || h == 0)) store_weight(a, line_at, key, older, W == 2 && h ? sum[W - 1] : sum[0]);
 }
 
-// few: rows of a kv head of the largest request that has few, -1 if none has
+// few: rows of a kv head of the largest request that has few, -1 if none has; fours: of waves of a workgroup for many rows, 0 if none has many
 template <int D, int KIND>
-sp_status run(const WeightArgs &a, int few, bool many, hipStream_t st)
+sp_status run(const WeightArgs &a, int few, int fours, hipStream_t st)
 {
     const unsigned lines = (unsigned)(a.B * a.c.n_kv_heads);
     if (few >= 0) {
@@ -377,18 +395,21 @@ sp_status run(const WeightArgs &a, int few, bool many, hipStream_t st)
         else hipLaunchKernelGGL((sp_weights_few_kernel<D, KIND, 4>), grid, dim3(kThreads), 0, st, a);
         SP_HIP_CHECK(hipGetLastError());
     }
-    if (many) {
-        hipLaunchKernelGGL((sp_weights_many_kernel<D, KIND>), dim3((unsigned)sp::ceil_div(a.max_len, 32 * many_blocks(D) * kWaves), lines), dim3(kThreads), 0, st, a);
+    if (fours) {
+        const dim3 grid((unsigned)sp::ceil_div(a.max_len, 32 * many_blocks(D) * kWaves), lines);
+        if (fours == 4) hipLaunchKernelGGL((sp_weights_many_kernel<D, KIND, 4>), grid, dim3(4 * kThreads), 0, st, a);
+        else if (fours == 2) hipLaunchKernelGGL((sp_weights_many_kernel<D, KIND, 2>), grid, dim3(2 * kThreads), 0, st, a);
+        else hipLaunchKernelGGL((sp_weights_many_kernel<D, KIND, 1>), grid, dim3(kThreads), 0, st, a);
         SP_HIP_CHECK(hipGetLastError());
     }
     return SP_OK;
 }
 
 template <int D>
-sp_status run_kind(const WeightArgs &a, int kind, int few, bool many, hipStream_t st)
+sp_status run_kind(const WeightArgs &a, int kind, int few, int fours, hipStream_t st)
 {
-    if (kind == SP_CACHE_MX4) return run<D, SP_CACHE_MX4>(a, few, many, st);
-    return kind == SP_CACHE_E4M3 ? run<D, SP_CACHE_E4M3>(a, few, many, st) : run<D, SP_CACHE_BF16>(a, few, many, st);
+    if (kind == SP_CACHE_MX4) return run<D, SP_CACHE_MX4>(a, few, fours, st);
+    return kind == SP_CACHE_E4M3 ? run<D, SP_CACHE_E4M3>(a, few, fours, st) : run<D, SP_CACHE_BF16>(a, few, fours, st);
 }
 
 }  // namespace
@@ -417,12 +438,21 @@ extern "C" sp_status sp_attend_weights(const sp_cache_desc *desc, const void *q_
 
     const int64_t G = desc->n_q_heads / desc->n_kv_heads;
     int few = -1;
-    bool many = false;
+    int64_t tiles = 0, longest_tiles = 0;       // of rows, of the requests with many
     for (int32_t b = 0; b < B; ++b) {
-        const int64_t rows = (offsets_host[b + 1] - offsets_host[b]) * G;
-        if (rows > kFewRows) many = true;
-        else few = rows > few ? (int)rows : few;
+        const int64_t rows = (offsets_host[b + 1] - offsets_host[b]) * G, n = sp::ceil_div(rows, kManyRows);
+        if (rows <= kFewRows) {
+            few = rows > few ? (int)rows : few;
+            continue;
+        }
+        tiles += n;
+        longest_tiles = n > longest_tiles ? n : longest_tiles;
     }
+    // A workgroup goes through the tiles of its line's rows, 1.1 us each; several fours of waves share them. That pays where the longest line, and not the work of a compute unit, takes the
+    // time, and costs where there is work for all, since each four loads the keys. One, two, four fours in us, at one longest line a unit's work: 8192 rows by 8192 keys, 8 heads of 64 284, 182, 132; at half of
+    // it: 4096 rows, 8 of 128 160, 118, 128; at a quarter: 16 requests of 2048 rows by 2000 keys 142, 145, 160; few rows (128 by 32768, 8 of 128) 25, 32, 56.
+    const int64_t unit = sp::ceil_div(max_len, 32 * many_blocks(desc->head_dim) * kWaves) * desc->n_kv_heads * tiles / kUnits;
+    const int fours = tiles == 0 ? 0 : longest_tiles < 16 || 3 * longest_tiles < unit ? 1 : 4 * longest_tiles < 3 * unit ? 2 : 4;
     WeightArgs a{};
     static_cast<ContextArgs &>(a) = context_args(*desc, q_dev, offsets_dev, lens_dev, max_len, block_table_dev, table_stride, k_pool_dev, k_pool_dev,
                                                  k_scale_dev, k_scale_dev, scale, causal, window, B);
@@ -435,5 +465,5 @@ extern "C" sp_status sp_attend_weights(const sp_cache_desc *desc, const void *q_
     a.per = 1;
     while (a.per < 8 && pairs > (int64_t)a.per * 2 * kWaves * 2048) a.per *= 2;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    return desc->head_dim == 64 ? run_kind<64>(a, desc->cache_type, few, many, st) : run_kind<128>(a, desc->cache_type, few, many, st);
+    return desc->head_dim == 64 ? run_kind<64>(a, desc->cache_type, few, fours, st) : run_kind<128>(a, desc->cache_type, few, fours, st);
 }

@@ -147,6 +147,15 @@ def test_weights_of_long_contexts(kind):
     check_weights(kind, 8, 4, 128, [20, 1], [5000, 9000])
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("causal,window", [(1, 0), (0, 0), (1, 100)])
+def test_weights_of_rows_that_waves_share(kind, causal, window):
+    """Enough rows for several fours of waves: four of them for one long line, two where the work of the device is twice the longest line's."""
+    check_weights(kind, 16, 1, 64, [45, 3, 70], [300, 40, 500], causal=causal, window=window)
+    check_weights(kind, 8, 1, 128, [101, 1, 64], [300, 40, 700], causal=causal, window=window)
+    check_weights(kind, 64, 16, 128, [128, 130, 131, 127, 1], [1000, 1000, 900, 1000, 30], causal=causal, window=window)
+
+
 @pytest.mark.parametrize("n", [1, 30])
 @pytest.mark.parametrize("kind", KINDS)
 def test_a_nan_in_an_lse_gets_out(kind, n):
