@@ -597,13 +597,13 @@ sp_status sp_attend_weights(const sp_cache_desc *desc, const void *q_dev, const 
  *     largest scale s among those of its tokens (a NaN counts as the largest), codes are brought to it, E4M3(code * (scale / s)): exactly where scales are powers of
  *     two, but for what falls among the subnormals;
  *   - kept_dev[b, h, i] (int32 [B][n_kv_heads][max_budget]): which token it was;
- *   - new_weights_dev[b, h, i] (optional, float [B][n_kv_heads][max_budget], not weights_dev itself): its weight.
+ *   - new_weights_dev[b, h, i] (optional, float [B][n_kv_heads][max_budget], not overlapping weights_dev): its weight.
  * new_lens_dev[b] = n (int32, neither lens_dev nor budget_dev itself). Entries and slots at and behind n are left as they were.
  * Keys keep the rotation of their old position: new tokens go on from there (sp_cache_append's positions_dev), while attention's masks and windows
  * count slots. The pages of dst_table must be different ones for all requests, and not among those that block_table names (for any request): source pages are only
  * read, and free afterwards; pages that requests share stay as they are. In an E4M3 cache the scale of the block that holds slot n - 1 is replaced, for what lies behind n in it too. Tokens whose destination lies beyond dst_table's row, or whose destination page is not in [0, n_pages), are not moved.
  * weights_dev: float [B][n_kv_heads][weights_stride], weights_stride >= max_len. Contexts are bounded by max_len as in sp_attend. sinks, recent >= 0.
- * 0 <= max_budget <= 2^30, min(max_len, max_budget) < 2^29; requests times kv heads at most 65535. The result does not change from call to call.
+ * 0 <= max_budget <= 2^30, min(max_len, max_budget) <= 2^29 - 32; requests times kv heads at most 65535. The result does not change from call to call.
  */
 sp_status sp_cache_evict(const sp_cache_desc *desc, int32_t B, const int32_t *lens_dev, int64_t max_len,
                          const int32_t *budget_dev, int64_t max_budget, int64_t sinks, int64_t recent,

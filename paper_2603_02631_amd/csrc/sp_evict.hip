@@ -12,7 +12,7 @@ constexpr int kBins = 2048;             // counters of the selection
 constexpr int kMoveThreads = 256;
 constexpr int kBlock = sp::kCacheBlock;
 constexpr int64_t kMaxLen = int64_t(1) << 30;
-constexpr int64_t kMaxKept = int64_t(1) << 29;      // a launch's threads fit 32 bits
+constexpr int64_t kMaxKept = (int64_t(1) << 29) - kBlock;      // a launch's threads fit 32 bits
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
@@ -408,7 +408,7 @@ extern "C" sp_status sp_cache_evict(const sp_cache_desc *desc, int32_t B, const 
     const int64_t most = max_len < max_budget ? max_len : max_budget;       // tokens that a request keeps at most
     if (max_len > 0 && !weights_dev) return sp::fail(SP_ERR_INVALID_ARG, "weights_dev is null");
     if (most > 0 && !kept_dev) return sp::fail(SP_ERR_INVALID_ARG, "kept_dev is null");
-    if (most >= kMaxKept) return sp::fail(SP_ERR_UNSUPPORTED, "%lld kept tokens are more than a launch holds", (long long)most);
+    if (most > kMaxKept) return sp::fail(SP_ERR_UNSUPPORTED, "%lld kept tokens are more than a launch holds", (long long)most);
     if (sp_status rc = sp::check_pools(*desc, k_pool_dev, v_pool_dev, k_scale_dev, v_scale_dev)) return rc;
     if (new_weights_dev && new_weights_dev == weights_dev) return sp::fail(SP_ERR_INVALID_ARG, "new_weights_dev must not be weights_dev");
 
