@@ -88,7 +88,8 @@ __device__ __forceinline__ void store4(const MatmulArgs &p, int64_t m, int64_t n
 
 __device__ __forceinline__ i32x8 operand(u32x4 x) { return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], 0, 0, 0, 0}; }
 
-// Up to four scale bytes of a row from group k on, as they lie there (at any address); 1 for groups that the row does not have.
+// Up to four scale bytes of a row from group k on, as they lie there (at any address). For groups that the row does not have 0: with the other operand's, which are 0 too, a factor
+// of 2^-254, under which any codes vanish.
 __device__ __forceinline__ uint32_t scales4(const uint8_t *row, int64_t k, int64_t groups)
 {
     if (k + 4 <= groups) {
@@ -96,10 +97,10 @@ __device__ __forceinline__ uint32_t scales4(const uint8_t *row, int64_t k, int64
         __builtin_memcpy(&w, row + k, 4);
         return w;
     }
-    uint32_t w = 0x7f7f7f7fu;
+    uint32_t w = 0;
 #pragma unroll
     for (int i = 0; i < 3; ++i)
-        if (k + i < groups) w = (w & ~(255u << (8 * i))) | (uint32_t)row[k + i] << (8 * i);
+        if (k + i < groups) w |= (uint32_t)row[k + i] << (8 * i);
     return w;
 }
 
@@ -230,9 +231,10 @@ struct Codes {
     }
 };
 
-// 8192 x 8192 x 4096 takes 190 to 225 us by the clock that the power leaves, 2.4 to 2.9 PFLOP/s, where the instructions alone run at 6.7 on random data and a large bf16 product
-// reaches 1.3. Bound by bringing tiles from L2 to LDS, 1.1 GB at some 9 TB/s, beside the products, which start after it again and again: of a SIMD's time 34 % are products. Buffers for four steps
-// (192), steps taken in another order by each workgroup and 128 x 128 results a wave gained nothing; 256 x 256 results a workgroup are what its registers hold.
+// 8192 x 8192 x 4096 takes 172 to 195 us by the clock that the power leaves, 2.8 to 3.2 PFLOP/s, where the instructions alone run at 6.7 on random data and a large bf16 product
+// reaches 1.3. Copies without loads take 150, without products 136, without results 176: products, operands from LDS and tiles to LDS share the time, and the first operands of a step come after a
+// barrier. The next step's loads are requested behind the first products, whose issue they would hold up (181 to 174). Not kept: buffers for four steps, steps in another order for each workgroup,
+// 128 x 128 results a wave (the same or slower); operands requested across the barrier, which takes all registers (168, but 128 x 128 tiles 15.4 to 16.3).
 template <bool BF16, int WM, int WN, int FM, int FN>
 __global__ __launch_bounds__(64 * WM * WN) void sp_mx4_tiled_kernel(MatmulArgs p)
 {
@@ -250,28 +252,28 @@ __global__ __launch_bounds__(64 * WM * WN) void sp_mx4_tiled_kernel(MatmulArgs p
     const int steps = (int)((p.K + kStep - 1) / kStep), rest = (int)(p.K % kStep);       // elements of the last step, 0: all
 
     // this thread's pieces: row (of the activations, then of the weights) and place in it, swapped about so that sixteen lanes read sixteen places of 16 bytes
+    const int most_m = (int)min(p.M - 1 - m0, (int64_t)T::TM), most_n = (int)min(p.N - 1 - n0, (int64_t)T::TN);
     uint32_t off[T::kLoads];
     const int slot = tid % kPieces, piece = slot ^ (tid / kPieces >> 1 & 7);
 #pragma unroll
     for (int i = 0; i < T::kLoads; ++i) {
         const int r = tid / kPieces + i * (T::kThreadsT / kPieces);
-        const int64_t row = r < T::TM ? min((int64_t)r, p.M - 1 - m0) : min((int64_t)(r - T::TM), p.N - 1 - n0);
-        off[i] = (uint32_t)(row * row_bytes + 16 * piece);
+        const int row = r < T::TM ? min(r, most_m) : min(r - T::TM, most_n);
+        off[i] = __umul24((uint32_t)row, (uint32_t)row_bytes) + 16 * piece;      // fewer than 2^9 rows of less than 2^22 bytes
     }
     const uint8_t *a_base = p.a + m0 * row_bytes, *w_base = p.w + n0 * row_bytes;
     const uint8_t *scale_row = tid < T::TM ? p.as + min(m0 + tid, p.M - 1) * groups : p.ws + min(n0 + tid - T::TM, p.N - 1) * groups;
     const uint32_t lds_at = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t *)lds);
     uint8_t *const scale_lds = lds + 2 * T::kCodes;
 
+    // behind a row's end a thread takes the last step's first piece, whose product with the scales there vanishes
+    const uint32_t past = rest != 0 && 32 * piece >= rest ? 16 * piece : 0;
     const auto load_codes = [&](int step, int buf) {
-        const bool tail = rest != 0 && step == steps - 1;
+        const uint32_t back = step == steps - 1 ? past : 0;
 #pragma unroll
-        for (int i = 0; i < T::kLoads; ++i) {
-            const bool of_a = i * (T::kThreadsT / kPieces) < T::TM;
-            const uint32_t to = buf * T::kCodes + i * T::kThreadsT * 16;
-            if (!tail || 32 * piece < rest) load_to_lds((of_a ? a_base : w_base) + (int64_t)step * kRowBytes, off[i], lds_at + to + wave * 1024);
-            else *reinterpret_cast<u32x4 *>(lds + to + tid * 16) = u32x4{0, 0, 0, 0};
-        }
+        for (int i = 0; i < T::kLoads; ++i)
+            load_to_lds((i * (T::kThreadsT / kPieces) < T::TM ? a_base : w_base) + (int64_t)step * kRowBytes, off[i] - back,
+                        lds_at + buf * T::kCodes + i * T::kThreadsT * 16 + wave * 1024);
     };
     const auto load_scales = [&](int step) {
         const int64_t k = (int64_t)step * kStepGroups;
@@ -302,7 +304,6 @@ __global__ __launch_bounds__(64 * WM * WN) void sp_mx4_tiled_kernel(MatmulArgs p
         put_scales(scales, buf ^ 1);                        // of the next step, loaded in the one before
         if (step + 1 < steps) {
             scales = load_scales(step + 2);
-            load_codes(step + 1, buf ^ 1);
         }
         const uint8_t *a = lds + buf * T::kCodes + row_a * kRowBytes, *w = lds + buf * T::kCodes + row_w * kRowBytes;
         uint32_t sa[FM], sw[FN];
@@ -316,6 +317,8 @@ __global__ __launch_bounds__(64 * WM * WN) void sp_mx4_tiled_kernel(MatmulArgs p
         odd.read(a, w, at[1]);
         __builtin_amdgcn_sched_barrier(0);
         even.template multiply<0>(acc, sa, sw);
+        __builtin_amdgcn_sched_barrier(0);
+        if (step + 1 < steps) load_codes(step + 1, buf ^ 1);
         __builtin_amdgcn_sched_barrier(0);
         even.read(a, w, at[2]);
         __builtin_amdgcn_sched_barrier(0);
@@ -378,10 +381,11 @@ sp_status run(const MatmulArgs &p, hipStream_t st)
 {
     if (p.M <= 16) return few<BF16, 1>(p, st);
     if (p.M <= 32) return few<BF16, 2>(p, st);
-    // Tiles take as long however few they are (0.45 us for 128 elements of K), the workgroups for few rows as long as what they read from L2, by turns (us, few rows' and tiles'):
-    // 128 x 4096 x 4096 (32 tiles) 14 and 17, 700 x 300 x 4000 (18) 9 and 22; 2048 x 500 x 2048 (64) 13 and 11, 256 x 4096 x 4096 (64) 25 and 18, 632 x 2025 x 224 (80) 12 and 7
+    // Tiles take as long however few they are (0.35 us for 128 elements of K), the workgroups for few rows as long as what they read from L2, by turns (us, few rows' and tiles'):
+    // 128 x 4096 x 4096 (32 tiles) 14.0 and 14.6, 700 x 300 x 4000 (18) 7.7 and 14.0; 384 x 2048 x 2048 (48) 10.4 and 9.4, 256 x 4096 x 4096 (64) 25 and 15, 632 x 2025 x 224 (80) 11.0 and 6.3.
+    // Large tiles need nearly one for each unit (us, of 128 x 128 and 256 x 256): 2048 x 4096 x 4096 (128 large ones) 33 and 39, 2560 x 4096 x 4096 (160) 47 and 40, 8192 x 8192 x 4096 235 and 184.
     if (p.K <= kMostTiledK) {
-        if (sp::ceil_div(p.M, 256) * sp::ceil_div(p.N, 256) >= 192) return tiled<BF16, 2, 4, 4, 2>(p, st);
+        if (sp::ceil_div(p.M, 256) * sp::ceil_div(p.N, 256) >= 160) return tiled<BF16, 2, 4, 4, 2>(p, st);
         if (sp::ceil_div(p.M, 128) * sp::ceil_div(p.N, 128) >= 48) return tiled<BF16, 2, 2, 2, 2>(p, st);
     }
     return few<BF16, 4>(p, st);
