@@ -309,8 +309,17 @@ __device__ __forceinline__ void few_stretch(const AttendArgs &a, int b, int kvh,
             load_keys(kv, there);
             bf16x8 vf[kTiles];
             if (!whole) kv.clear_values(g, key0, rg.lo, rg.hi);
-            if constexpr (MX4) kv.values(vf, c);
-            else kv.values(vf);
+            if constexpr (MX4) {
+                kv.values(vf, c);
+                // before the next block's are requested, or these would be held beside them, and copied
+#pragma unroll
+                for (int i = 0; i < kTiles; ++i) {
+                    u32x4 r = __builtin_bit_cast(u32x4, vf[i]);
+                    asm volatile("" : "+v"(r));
+                    vf[i] = __builtin_bit_cast(bf16x8, r);
+                }
+            } else
+                kv.values(vf);
             load_values(kv, there);
             soon = later;
 #pragma unroll

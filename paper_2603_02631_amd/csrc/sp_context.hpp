@@ -305,16 +305,16 @@ __device__ __forceinline__ uint32_t widen4(uint32_t w, float scale)
 // 8g .. 8g + 7, and the scales of a lane's two keys lie side by side; of a key's row a lane has elements [g D/4, (g + 1) D/4), of one group. Values: elements
 // [c D/16, (c+1) D/16) of keys 8g .. 8g + 7, each key's under its scale and then paired by keys. (The scaled matrix instruction would take keys as they are with queries as
 // sums of two E4M3 numbers, but it drops products below some 2^-13 of an instruction's largest: logits off by 2^-11 of theirs.)
-// Half the bytes of E4M3 and more operations for each: a block of 32 tokens of head_dim 64 takes a wave 154 vector operations, of which 32 widen and 16 pair, so that
-// 48 contexts of 2048 to 65536 tokens (32 query heads over 8, 439 MB) take 91 to 96 us (E4M3: 138), 4.7 TB/s, with the vector pipes issuing for two thirds of the time.
-// Not kept: five workgroups a compute unit (registers for 96: 111 us), two blocks ahead (103 to 137), loads past the caches (the same).
+// Half the bytes of E4M3 and more operations for each: 48 contexts of 2048 to 65536 tokens (32 query heads of 64 over 8, 439 MB) take 91 us (E4M3: 138), 4.8 TB/s. Bound by what
+// is under way: a block of keys and values of each of a unit's 16 waves. An eighth fewer vector operations, or all values in one load instead of eight, change that by less than 4 us; five
+// workgroups a unit (registers for 96: 112 us), two blocks ahead (103 to 137) and loads past the caches (the same) were not kept.
 template <int D, bool STREAM>
 struct Block<D, SP_CACHE_MX4, STREAM> {
     static constexpr int kBytes = D / 32;                           // of a token's scales, and of a lane's part of a token's values
     static constexpr int kWords = kBytes / 2;                       // dwords of two tokens' scales
     uint32_t k[2][2 * kWords];
     uint32_t ks[kWords];
-    uint32_t v[8];
+    u32x4 v[2];                     // a word for each key (as vectors: single ones of 16 bits would be cut to them and widened again with every use)
     u32x4 vs[kWords];
 
     __device__ __forceinline__ static int key_of(int g, int i) { return 8 * g + i; }
@@ -351,8 +351,8 @@ struct Block<D, SP_CACHE_MX4, STREAM> {
         Moving p(l.v + at.off);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if constexpr (D == 64) v[j] = p.load<uint16_t>(lane);
-            else v[j] = p.load<uint32_t>(lane);
+            if constexpr (D == 64) v[j / 4][j % 4] = p.load<uint16_t>(lane);
+            else v[j / 4][j % 4] = p.load<uint32_t>(lane);
             p.advance(l.row_bytes);
         }
         const Moving s(l.vs4 + at.scale * D);
@@ -382,8 +382,9 @@ struct Block<D, SP_CACHE_MX4, STREAM> {
                 s[i] = D == 64 ? exponent_of(vs[0][p], turn[i]) : exponent_of(vs[p / 2 % kWords][2 * (p & 1) + i], turn[0]);
 #pragma unroll
             for (int e = 0; e < D / 32; ++e) {                      // a byte: elements 2e and 2e + 1
-                const uint32_t x = e == 0 ? widen4<0>(v[2 * p], s[0]) : e == 1 ? widen4<1>(v[2 * p], s[0]) : e == 2 ? widen4<2>(v[2 * p], s[0]) : widen4<3>(v[2 * p], s[0]);
-                const uint32_t y = e == 0 ? widen4<0>(v[2 * p + 1], s[1]) : e == 1 ? widen4<1>(v[2 * p + 1], s[1]) : e == 2 ? widen4<2>(v[2 * p + 1], s[1]) : widen4<3>(v[2 * p + 1], s[1]);
+                const uint32_t a = v[p / 2][2 * p % 4], b = v[p / 2][2 * p % 4 + 1];
+                const uint32_t x = e == 0 ? widen4<0>(a, s[0]) : e == 1 ? widen4<1>(a, s[0]) : e == 2 ? widen4<2>(a, s[0]) : widen4<3>(a, s[0]);
+                const uint32_t y = e == 0 ? widen4<0>(b, s[1]) : e == 1 ? widen4<1>(b, s[1]) : e == 2 ? widen4<2>(b, s[1]) : widen4<3>(b, s[1]);
                 r[2 * e][p] = __builtin_amdgcn_perm(y, x, 0x05040100u);
                 r[2 * e + 1][p] = __builtin_amdgcn_perm(y, x, 0x07060302u);
             }
