@@ -305,9 +305,9 @@ __device__ __forceinline__ uint32_t widen4(uint32_t w, float scale)
 // 8g .. 8g + 7, and the scales of a lane's two keys lie side by side; of a key's row a lane has elements [g D/4, (g + 1) D/4), of one group. Values: elements
 // [c D/16, (c+1) D/16) of keys 8g .. 8g + 7, each key's under its scale and then paired by keys. (The scaled matrix instruction would take keys as they are with queries as
 // sums of two E4M3 numbers, but it drops products below some 2^-13 of an instruction's largest: logits off by 2^-11 of theirs.)
-// Half the bytes of E4M3 and more operations for each: 48 contexts of 2048 to 65536 tokens (32 query heads of 64 over 8, 439 MB) take 91 us (E4M3: 138), 4.8 TB/s. Bound by what
-// is under way: a block of keys and values of each of a unit's 16 waves. An eighth fewer vector operations, or all values in one load instead of eight, change that by less than 4 us; five
-// workgroups a unit (registers for 96: 112 us), two blocks ahead (103 to 137) and loads past the caches (the same) were not kept.
+// 48 contexts of 2048 to 65536 tokens (32 query heads of 64 over 8, 439 MB) take 91 us, 4.8 TB/s (E4M3, twice the bytes: 138). Not bound by operations (copies without the conversions, 60 of 137
+// vector operations fewer, take as long) nor by what is under way (keys two blocks ahead 96, both 103 and more): what is left is how memory serves pieces of 1 KB, and 64 bytes of scales.
+// Not kept either: all values in one load instead of eight (4 us, without getting them to their lanes), all keys in one load (2 us), five workgroups a unit (registers for 96: 108 us), loads past the caches (the same).
 template <int D, bool STREAM>
 struct Block<D, SP_CACHE_MX4, STREAM> {
     static constexpr int kBytes = D / 32;                           // of a token's scales, and of a lane's part of a token's values
