@@ -121,7 +121,7 @@ struct Scales16 {
     }
 };
 
-// Bound by reading the weights: one row by 32000 x 2048 (35 MB) 9 us, by 33000 x 8192 (144 MB) 37 us, 3.9 TB/s (with 64 neighbouring bytes for a
+// Bound by reading the weights: one row by 32000 x 2048 (35 MB) 8 us, by 33000 x 8192 (144 MB) 36 us, 4.0 TB/s, past the caches 9 and 38 (with 64 neighbouring bytes for a
 // lane, loaded in four pieces, 13 and 55); by launching and one chain of loads where they are few (48 x 4096 x 4096, 9 MB: 8.4 us).
 // Sixteen weight rows and 16 MT activation rows a workgroup. Its waves take stretches of 512 elements of the rows in turn, four instructions of 128 (of a row a lane has
 // one group in each, so that a load takes 64 neighbouring bytes of sixteen rows), and add up in LDS.
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(64 * WAVES) void sp_mx4_few_kernel(MatmulArgs p)
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             u[s] = u32x4{0, 0, 0, 0};
-            if (k + 4 * s + g < groups) u[s] = MT == 1 ? __builtin_nontemporal_load(w + 4 * s) : w[4 * s];
+            if (k + 4 * s + g < groups) u[s] = w[4 * s];
         }
         Scales16 su;
         su.load(p.ws + n * groups, k, groups, g);

@@ -12,7 +12,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kFewRows = 16;            // rows of a kv head that sp_weights_few_kernel takes at most
+// Rows of a kv head that sp_weights_few_kernel takes at most: what a wave's tile holds. 12 rows of 16 contexts of 16000 tokens (8 heads of 64, MX4) take 23 us there and 33 in the other kernel, of 4 (8 of 128,
+// bf16) 32 and 30.
+constexpr int kFewRows = 16;
 constexpr int kManyRows = 32;           // rows of a tile of sp_weights_many_kernel
 constexpr int64_t kUnits = 256;         // compute units
 constexpr int many_blocks(int d) { return 128 / d; }    // blocks of 32 keys of a wave there: as many as leave four waves a SIMD their registers
@@ -460,10 +462,11 @@ extern "C" sp_status sp_attend_weights(const sp_cache_desc *desc, const void *q_
     a.old = old_dev;
     a.weights = weights_dev;
     a.stride = weights_stride;
-    // pairs of blocks of a wave: more of them spare queries being read again, as long as workgroups are left to fill the device
+    // Pairs of blocks of a wave: as many as leave two waves a SIMD, at most 8. One, two, four, eight of them in us: 65536 keys, 8 heads of 64, 10.6, 8.7, 9.0, 10.5; 16 times 16000 34, 26, 22, 20; 4 times
+    // 16000, 8 of 128, 43, 35, 32, 33; 48 of up to 65536 115, 74 to 81, 66, 67, and 138 with sixteen.
     const int64_t pairs = sp::ceil_div(max_len, 2 * kBlock) * B * desc->n_kv_heads;
     a.per = 1;
-    while (a.per < 8 && pairs > (int64_t)a.per * 2 * kWaves * 2048) a.per *= 2;
+    while (a.per < 8 && pairs > (int64_t)a.per * 2048) a.per *= 2;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     return desc->head_dim == 64 ? run_kind<64>(a, desc->cache_type, few, fours, st) : run_kind<128>(a, desc->cache_type, few, fours, st);
 }
