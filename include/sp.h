@@ -435,8 +435,9 @@ sp_status sp_assemble(const int32_t *target_ids_dev, int64_t M,
  * token and the probabilities of given ones are read off the logits
  * (sp_logprobs). Projections can be products in 4 bits (sp_mx4_quantise,
  * sp_mx4_matmul), and a cache can be held to a budget: what its tokens draw is
- * added up (sp_attend_weights) and the rest is dropped (sp_cache_evict). A bf16 cache with pages of a multiple of 512 tokens is what
- * sp_score_paged reads afterwards.
+ * added up (sp_attend_weights) and the rest is dropped (sp_cache_evict). A bf16
+ * cache with pages of a multiple of 512 tokens is what sp_score_paged reads
+ * afterwards.
  */
 
 /* How a paged cache holds its elements. SP_CACHE_BF16: as they are.
@@ -546,7 +547,8 @@ sp_status sp_attend_workspace(const sp_cache_desc *desc, const int64_t *offsets_
  * context among them) may hold anything, NaN included.
  * What a row sees should be finite: logits below 2^120, values below 2^90 in magnitude, scales
  * finite and not negative (a value scale below 2^-64 may count as 2^-64: zero is in order for a block
- * of zeros); scale bytes of MX4 caches below 2^90. A row that sees a NaN becomes NaN, and other rows of its request may.
+ * of zeros); scale bytes of MX4 caches stand for less than 2^90. A row that sees a NaN becomes
+ * NaN, and other rows of its request may.
  * At most 2^26 query tokens and contexts of at most 2^30 tokens; requests times kv heads, and tiles of 256
  * query rows times kv heads, below 2^23.
  * max_len bounds the contexts from the host's side (a longer lens[b] counts as
@@ -565,17 +567,20 @@ sp_status sp_attend(const sp_cache_desc *desc, const void *q_dev,
                     void *ws_dev, size_t ws_bytes, void *hip_stream);
 
 /*
- * How much attention the tokens of a paged cache have drawn: the weight that decides which of them sp_cache_evict
- * keeps. Queries, contexts, masks and the cache's keys are those of an sp_attend call, whose lse_dev this call
- * takes; the values are not looked at:
- *   weights_dev[b, h, j] = old + sum over rows r of request b that see key j, and over the query heads g of kv head h, of
- *                          exp( scale * <q[r, g], K[b, h, j]> - lse_dev[r, g] )
- * for j < lens[b]; entries behind are left as they were. weights_dev: float [B][n_kv_heads][weights_stride],
- * weights_stride >= max_len. old = old_dev[b, h, j] (the same layout; may be weights_dev itself, else they must not overlap) for
- * tokens that were there before the rows' own: j < lens[b] - n_b with causal = 1, all with causal = 0; 0 for the others
- * and where old_dev is null. A request without rows keeps its old weights. Rows with an lse of minus infinity add nothing.
+ * How much attention the tokens of a paged cache have drawn: the weight that decides which of them
+ * sp_cache_evict keeps. Queries, contexts, masks and the cache's keys are those of an sp_attend
+ * call, whose lse_dev this call takes; the values are not looked at:
+ *   weights_dev[b, h, j] = old + sum over rows r of request b that see key j, and over the query
+ *                          heads g of kv head h, of exp( scale * <q[r, g], K[b, h, j]> - lse_dev[r, g] )
+ * for j < lens[b]; entries behind are left as they were. weights_dev: float
+ * [B][n_kv_heads][weights_stride], weights_stride >= max_len.
+ * old = old_dev[b, h, j] (the same layout; may be weights_dev itself, else they must not overlap)
+ * for tokens that were there before the rows' own: j < lens[b] - n_b with causal = 1, all with
+ * causal = 0; 0 for the others and where old_dev is null. A request without rows keeps its old
+ * weights. Rows with an lse of minus infinity add nothing.
  * Arithmetic is in fp32, in an order that is fixed by the offsets, the lengths and max_len.
- * A row that sees a NaN, or whose lse is NaN, makes NaN of the weights that it adds to, and of others of its request.
+ * A row that sees a NaN, or whose lse is NaN, makes NaN of the weights that it adds to, and of
+ * others of its request.
  * Limits as in sp_attend; requests times kv heads at most 65535.
  */
 sp_status sp_attend_weights(const sp_cache_desc *desc, const void *q_dev, const int64_t *offsets_host,
@@ -586,24 +591,35 @@ sp_status sp_attend_weights(const sp_cache_desc *desc, const void *q_dev, const 
                             int64_t weights_stride, void *hip_stream);
 
 /*
- * Eviction: the cached tokens of most weight, of each kv head by itself, into other pages. Request b has lens_dev[b] tokens
- * and a budget of budget_dev[b] (device, int32; a negative one counts as 0, one above max_budget as max_budget). With n = min(len, budget):
+ * Eviction: the cached tokens of most weight, of each kv head by itself, into other pages. Request
+ * b has lens_dev[b] tokens and a budget of budget_dev[b] (device, int32; a negative one counts as
+ * 0, one above max_budget as max_budget). With n = min(len, budget):
  *   - a context of at most the budget is kept whole;
- *   - else the first s = min(sinks, budget) tokens, the last r = min(recent, budget - s), and of those between the
- *     budget - s - r with the largest weights_dev[b, h, j], equal weights in favour of the earlier token. Weights are compared
- *     as numbers, a positive NaN above and a negative one below all others, -0 equal to 0.
- * The kept tokens of kv head h, in their order, become tokens 0 .. n - 1 of the pages that dst_table_dev names:
- *   - their keys and values (v_pool_dev and v_scale_dev as in sp_attend). bf16 and MX4 as they are, with their scales. E4M3: a block takes the
- *     largest scale s among those of its tokens (a NaN counts as the largest), codes are brought to it, E4M3(code * (scale / s)): exactly where scales are powers of
- *     two, but for what falls among the subnormals;
+ *   - else the first s = min(sinks, budget) tokens, the last r = min(recent, budget - s), and of
+ *     those between the budget - s - r with the largest weights_dev[b, h, j], equal weights in
+ *     favour of the earlier token. Weights are compared as numbers, a positive NaN above and a
+ *     negative one below all others, -0 equal to 0.
+ * The kept tokens of kv head h, in their order, become tokens 0 .. n - 1 of the pages that
+ * dst_table_dev names:
+ *   - their keys and values (v_pool_dev and v_scale_dev as in sp_attend). bf16 and MX4 as they
+ *     are, with their scales. E4M3: a block takes the largest scale s among those of its tokens (a
+ *     NaN counts as the largest), codes are brought to it, E4M3(code * (scale / s)): exactly where
+ *     scales are powers of two, but for what falls among the subnormals;
  *   - kept_dev[b, h, i] (int32 [B][n_kv_heads][max_budget]): which token it was;
- *   - new_weights_dev[b, h, i] (optional, float [B][n_kv_heads][max_budget], not overlapping weights_dev): its weight.
- * new_lens_dev[b] = n (int32, neither lens_dev nor budget_dev itself). Entries and slots at and behind n are left as they were.
- * Keys keep the rotation of their old position: new tokens go on from there (sp_cache_append's positions_dev), while attention's masks and windows
- * count slots. The pages of dst_table must be different ones for all requests, and not among those that block_table names (for any request): source pages are only
- * read, and free afterwards; pages that requests share stay as they are. In an E4M3 cache the scale of the block that holds slot n - 1 is replaced, for what lies behind n in it too. Tokens whose destination lies beyond dst_table's row, or whose destination page is not in [0, n_pages), are not moved.
- * weights_dev: float [B][n_kv_heads][weights_stride], weights_stride >= max_len. Contexts are bounded by max_len as in sp_attend. sinks, recent >= 0.
- * 0 <= max_budget <= 2^30, min(max_len, max_budget) <= 2^29 - 32; requests times kv heads at most 65535. The result does not change from call to call.
+ *   - new_weights_dev[b, h, i] (optional, float [B][n_kv_heads][max_budget], not overlapping
+ *     weights_dev): its weight.
+ * new_lens_dev[b] = n (int32, neither lens_dev nor budget_dev itself). Entries and slots at and
+ * behind n are left as they were, but for the scale of the E4M3 block that holds slot n - 1.
+ * Keys keep the rotation of their old position: new tokens go on from there (sp_cache_append's
+ * positions_dev), while attention's masks and windows count slots.
+ * The pages of dst_table must be different ones for all requests, and not among those that
+ * block_table names (for any request): source pages are only read, and free afterwards; pages that
+ * requests share stay as they are. Tokens whose destination lies beyond dst_table's row, or whose
+ * destination page is not in [0, n_pages), are not moved.
+ * weights_dev: float [B][n_kv_heads][weights_stride], weights_stride >= max_len. Contexts are
+ * bounded by max_len as in sp_attend. sinks, recent >= 0. 0 <= max_budget <= 2^30,
+ * min(max_len, max_budget) <= 2^29 - 32; requests times kv heads at most 65535. The result does
+ * not change from call to call.
  */
 sp_status sp_cache_evict(const sp_cache_desc *desc, int32_t B, const int32_t *lens_dev, int64_t max_len,
                          const int32_t *budget_dev, int64_t max_budget, int64_t sinks, int64_t recent,
@@ -647,13 +663,16 @@ sp_status sp_logprobs(const void *logits_dev, int32_t dtype, int64_t n_rows, int
                       void *hip_stream);
 
 /*
- * Rows of numbers to microscaled 4-bit elements (as in SP_CACHE_MX4 caches). Of each SP_MX4_GROUP elements x of a row the
- * largest magnitude m gives the smallest power of two s >= 2^-64 with m <= 6 s; scales_dev[r][k / 32] = log2 s + 127, and
- * codes are E2M1(x / s), rounded to nearest, halfway to the even code, the sign of zero kept. A group that holds a NaN or an
- * infinity gets scale byte 255 and codes of zero.
- * x_dev: float or bf16 (dtype an sp_logits_type), row r at r * row_stride elements (row_stride >= K, a multiple of 8, rows 16-byte
- * aligned). codes_dev: [rows][K / 2] bytes, scales_dev: [rows][K / 32] bytes, both dense, codes 16-byte, scales 4-byte aligned. K is a positive multiple of 32
- * below 2^31. 0 <= rows < 2^31; rows * K < 2^35. x_dev, codes_dev and scales_dev must not overlap.
+ * Rows of numbers to microscaled 4-bit elements (as in SP_CACHE_MX4 caches). Of each SP_MX4_GROUP
+ * elements x of a row the largest magnitude m gives the smallest power of two s >= 2^-64 with
+ * m <= 6 s; scales_dev[r][k / 32] = log2 s + 127, and codes are E2M1(x / s), rounded to nearest,
+ * halfway to the even code, the sign of zero kept. A group that holds a NaN or an infinity gets
+ * scale byte 255 and codes of zero.
+ * x_dev: float or bf16 (dtype an sp_logits_type), row r at r * row_stride elements (row_stride >=
+ * K, a multiple of 8, rows 16-byte aligned). codes_dev: [rows][K / 2] bytes, scales_dev:
+ * [rows][K / 32] bytes, both dense, codes 16-byte, scales 4-byte aligned. K is a positive multiple
+ * of 32 below 2^31. 0 <= rows < 2^31; rows * K < 2^35. x_dev, codes_dev and scales_dev must not
+ * overlap.
  */
 sp_status sp_mx4_quantise(const void *x_dev, int32_t dtype, int64_t rows, int64_t K, int64_t row_stride,
                           void *codes_dev, void *scales_dev, void *hip_stream);
@@ -661,10 +680,12 @@ sp_status sp_mx4_quantise(const void *x_dev, int32_t dtype, int64_t rows, int64_
 /*
  * Product of two microscaled 4-bit matrices, a projection's activations and weights:
  *   out_dev[m][n] = sum_k A[m][k] W[n][k],  0 <= m < M, 0 <= n < N
- * with A and W as sp_mx4_quantise leaves them: a_codes_dev [M][K / 2], a_scales_dev [M][K / 32], w_codes_dev [N][K / 2], w_scales_dev
- * [N][K / 32], dense, codes 16-byte, scales 4-byte aligned. out_dev: float or bf16 (dtype an sp_logits_type), row m at m * out_stride
- * elements (out_stride >= N). Products are exact, sums are held in fp32 in an order that the sizes fix, the result is rounded once.
- * Rows with a NaN scale give NaN. out_dev must not overlap the operands. K is a positive multiple of 32 below 2^31, 0 <= M, N < 2^31; (M / 16 + 1) * (N / 16 + 1) < 2^24.
+ * with A and W as sp_mx4_quantise leaves them: a_codes_dev [M][K / 2], a_scales_dev [M][K / 32],
+ * w_codes_dev [N][K / 2], w_scales_dev [N][K / 32], dense, codes 16-byte, scales 4-byte aligned.
+ * out_dev: float or bf16 (dtype an sp_logits_type), row m at m * out_stride elements (out_stride
+ * >= N), not overlapping the operands. Products are exact, sums are held in fp32 in an order that
+ * the sizes fix, the result is rounded once. Rows with a NaN scale give NaN. K is a positive
+ * multiple of 32 below 2^31, 0 <= M, N < 2^31; (M / 16 + 1) * (N / 16 + 1) < 2^24.
  */
 sp_status sp_mx4_matmul(const void *a_codes_dev, const void *a_scales_dev, int64_t M, const void *w_codes_dev,
                         const void *w_scales_dev, int64_t N, int64_t K, void *out_dev, int32_t dtype, int64_t out_stride,
