@@ -8,14 +8,16 @@
 //   m <= 448 s. Powers of two, because a block fills up over many calls: when a later token is larger, the older codes
 //   are brought to the larger scale by shifting exponents, exactly but for what falls among the subnormals (below
 //   2^-14 of the block's largest value), so a cache filled token by token holds what one filled at once does.
-// MX4: each 32 elements of a token's head have a scale of their own (sp_mx4.hpp). Its largest magnitude lies in up to D / 16 neighbouring threads, in which of
+// MX4: each 32 elements of a token's head have a scale of their own (sp_mx4.hpp). Its largest magnitude lies in up to D / 16 neighbouring threads,
+// in which of
 //   them the rotation's pairing decides; they meet by shuffles of the wave, and no other token is looked at.
 //
-// One workgroup owns 32 cache slots (the tokens of one scale) of one kv head: keys, values and the queries of the head's group.
-// A thread owns two vectors of eight elements of a token that the rotation pairs up, so that a pair never leaves its
-// thread and the token's cosines and sines are loaded once for the key and all query heads.
-// Bound by HBM for long inputs: 16 ragged chunks of 300 to 4096 tokens (32 query heads of 128 over 4, E4M3) 106 us, 4.9 TB/s read and written of the 5.2 that a large copy
-// reaches (MX4 104 us, 4.8 TB/s of 504 MB, most of it inputs and queries; a single token 4.5 us in the kernel); a prompt of 8192 tokens (32 heads of 64 over 8, bf16), one round of workgroups, 26 us, 4.0. By a chain of four dependent loads (offsets, block table,
+// One workgroup owns 32 cache slots (the tokens of one scale) of one kv head: keys, values and the queries of the head's group. A thread owns two
+// vectors of eight elements of a token that the rotation pairs up, so that a pair never leaves its thread and the token's cosines and sines are
+// loaded once for the key and all query heads.
+// Bound by HBM for long inputs: 16 ragged chunks of 300 to 4096 tokens (32 query heads of 128 over 4, E4M3) 106 us, 4.9 TB/s read and written of
+// the 5.2 that a large copy reaches (MX4 104 us, 4.8 TB/s of 504 MB, most of it inputs and queries; a single token 4.5 us in the kernel); a prompt
+// of 8192 tokens (32 heads of 64 over 8, bf16), one round of workgroups, 26 us, 4.0. By a chain of four dependent loads (offsets, block table,
 // inputs, old codes) and the call itself for single tokens: 13 us. With the kv heads of the same tokens far apart in the grid the chunks took 114.
 #include "sp_cache.hpp"
 #include "sp_mx4.hpp"

@@ -18,8 +18,8 @@ constexpr int kBlock = sp::kCacheBlock;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMostScale = 2.3e38f;      // of a call: times log2(e) it is finite
 
-// A block's key scale goes into its logits' factor, its value scale into the exponent (and out of the sum again): no operation for an element.
-// The factor stays above zero, so that masked logits stay minus infinity, and finite, so that a product of zero stays a logit of zero; the value scale
+// A block's key scale goes into its logits' factor, its value scale into the exponent (and out of the sum again): no operation for an element. The
+// factor stays above zero, so that masked logits stay minus infinity, and finite, so that a product of zero stays a logit of zero; the value scale
 // above 2^-64, so that exponents keep their range.
 constexpr float kLeastScale = 5.42101086e-20f, kLeastFactor = 1.17549435e-38f, kMostFactor = 3.40282347e38f;
 
@@ -194,13 +194,14 @@ struct Entry {
     }
 };
 
-// One block of 32 tokens as a wave loads it, straight into the registers that the matrix instructions take it from.
-// Lane l = 16 g + c. Keys: row c of 16-key tile t, the contraction's elements in an order that makes a lane's share of a row contiguous
-// (queries are loaded in the same order). Values: elements [c D/16, (c+1) D/16) of the eight keys 4g + j and 16 + 4g + j, j < 4: the
-// keys whose logits the lane holds after the first product.
-// Loads that take whole lines of 128 bytes pass the caches by: values, unless their rows have 64 bytes, and keys whose rows do. 32 requests of bf16, head_dim
-// 128, 172 us without and 160 with; 48 of E4M3, head_dim 64, 157 and 143 (200 of up to 4000 tokens 52 and 49, but 56 with values too). The latter only
-// for contexts that no cache would hold until the next call: 64 of up to 2000 tokens, called again and again, take 15.7 us without and 18.7 with.
+// One block of 32 tokens as a wave loads it, straight into the registers that the matrix instructions take it from. Lane l = 16 g + c. Keys: row c
+// of 16-key tile t, the contraction's elements in an order that makes a lane's share of a row contiguous (queries are loaded in the same order).
+// Values: elements [c D/16, (c+1) D/16) of the eight keys 4g + j and 16 + 4g + j, j < 4: the keys whose logits the lane holds after the first
+// product.
+// Loads that take whole lines of 128 bytes pass the caches by: values, unless their rows have 64 bytes, and keys whose rows do. 32 requests of
+// bf16, head_dim 128, 172 us without and 160 with; 48 of E4M3, head_dim 64, 157 and 143 (200 of up to 4000 tokens 52 and 49, but 56 with values
+// too). The latter only for contexts that no cache would hold until the next call: 64 of up to 2000 tokens, called again and again, take 15.7 us
+// without and 18.7 with.
 template <int D, int KIND, bool STREAM>
 struct Block {
     static constexpr bool E4M3 = KIND == SP_CACHE_E4M3;
@@ -301,13 +302,15 @@ __device__ __forceinline__ uint32_t widen4(uint32_t w, float scale)
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, BYTE));
 }
 
-// The same for an MX4 cache, widened to bf16 with its scales. Row c of tile t is key 2c + t, so that the keys whose logits a lane holds after the first product are
-// 8g .. 8g + 7, and the scales of a lane's two keys lie side by side; of a key's row a lane has elements [g D/4, (g + 1) D/4), of one group. Values: elements
-// [c D/16, (c+1) D/16) of keys 8g .. 8g + 7, each key's under its scale and then paired by keys. (The scaled matrix instruction would take keys as they are with queries as
-// sums of two E4M3 numbers, but it drops products below some 2^-13 of an instruction's largest: logits off by 2^-11 of theirs.)
-// 48 contexts of 2048 to 65536 tokens (32 query heads of 64 over 8, 439 MB) take 91 us, 4.8 TB/s (E4M3, twice the bytes: 138). Not bound by operations (copies without the conversions, 60 of 137
-// vector operations fewer, take as long) nor by what is under way (keys two blocks ahead 96, both 103 and more): what is left is how memory serves pieces of 1 KB, and 64 bytes of scales.
-// Not kept either: all values in one load instead of eight (4 us, without getting them to their lanes), all keys in one load (2 us), five workgroups a unit (registers for 96: 108 us), loads past the caches (the same).
+// The same for an MX4 cache, widened to bf16 with its scales. Row c of tile t is key 2c + t, so that the keys whose logits a lane holds after the
+// first product are 8g .. 8g + 7, and the scales of a lane's two keys lie side by side; of a key's row a lane has elements [g D/4, (g + 1) D/4), of
+// one group. Values: elements [c D/16, (c+1) D/16) of keys 8g .. 8g + 7, each key's under its scale and then paired by keys. (The scaled matrix
+// instruction would take keys as they are with queries as sums of two E4M3 numbers, but it drops products below some 2^-13 of an instruction's
+// largest: logits off by 2^-11 of theirs.) 48 contexts of 2048 to 65536 tokens (32 query heads of 64 over 8, 439 MB) take 91 us, 4.8 TB/s (E4M3,
+// twice the bytes: 138). Not bound by operations (copies without the conversions, 60 of 137 vector operations fewer, take as long) nor by what is
+// under way (keys two blocks ahead 96, both 103 and more): what is left is how memory serves pieces of 1 KB, and 64 bytes of scales. Not kept
+// either: all values in one load instead of eight (4 us, without getting them to their lanes), all keys in one load (2 us), five workgroups a unit
+// (registers for 96: 108 us), loads past the caches (the same).
 template <int D, bool STREAM>
 struct Block<D, SP_CACHE_MX4, STREAM> {
     static constexpr int kBytes = D / 32;                           // of a token's scales, and of a lane's part of a token's values

@@ -1,8 +1,9 @@
-// sp_cache_evict: the tokens of a paged cache that have drawn the most attention move to other pages, of each kv head by itself, the rest is left behind.
+// sp_cache_evict: the tokens of a paged cache that have drawn the most attention move to other pages, of each kv head by itself, the rest is left
+// behind.
 //
-// Two launches. sp_evict_select_kernel, a workgroup for each (request, kv head): the weight of the last token that stays, as an exact selection by digits
-// of the weights' ordered bits, then a walk over the tokens in order that lists those that stay: all above it, and of those equal to it the first ones.
-// sp_evict_move_kernel: 32 destination slots of a kv head a workgroup, keys and values.
+// Two launches. sp_evict_select_kernel, a workgroup for each (request, kv head): the weight of the last token that stays, as an exact selection by
+// digits of the weights' ordered bits, then a walk over the tokens in order that lists those that stay: all above it, and of those equal to it the
+// first ones. sp_evict_move_kernel: 32 destination slots of a kv head a workgroup, keys and values.
 // Out of place: every slot can be moved at once, and pages that requests share stay as they are.
 #include "sp_cache.hpp"
 
@@ -53,9 +54,9 @@ __device__ __forceinline__ uint32_t ordered(float x)
 }
 __device__ __forceinline__ float weight_of(uint32_t x) { return __uint_as_float(x & 0x80000000u ? x & 0x7fffffffu : ~x); }
 
-// A wave's stretch of a line's contenders, in order: R times 64 neighbours at a time, as their ordered bits. Stretches that have no more are read once (HELD). Places without a
-// token hold 0, which is below every weight (but for one NaN) and behind all tokens. R is small: code that is long and passed once waits for its own instructions (with lines of
-// 65536 weights held in registers, R = 64, a line of 1280 took 23 us, with R = 8 11).
+// A wave's stretch of a line's contenders, in order: R times 64 neighbours at a time, as their ordered bits. Stretches that have no more are read
+// once (HELD). Places without a token hold 0, which is below every weight (but for one NaN) and behind all tokens. R is small: code that is long
+// and passed once waits for its own instructions (with lines of 65536 weights held in registers, R = 64, a line of 1280 took 23 us, with R = 8 11).
 template <int R, bool HELD>
 struct Stretch {
     const float *w;
@@ -135,9 +136,10 @@ __device__ __forceinline__ Found find_digit(const uint32_t *bins, int above, int
     return found;
 }
 
-// Bound by the chain of passes, not by bytes: 1280 contenders take 7.5 us, up to 65536 of each of 128 lines 30 us, a line's 256 KB read three times from L2 by one workgroup.
-// Digits of 11, 11 and 10 bits, the most significant first: that one tells weights apart by two bits of their mantissa. Contenders that share it are listed in LDS
-// where they fit, and the other digits are found among them; so a line is read three times: to count, to list, and to write down what stays.
+// Bound by the chain of passes, not by bytes: 1280 contenders take 7.5 us, up to 65536 of each of 128 lines 30 us, a line's 256 KB read three times
+// from L2 by one workgroup. Digits of 11, 11 and 10 bits, the most significant first: that one tells weights apart by two bits of their mantissa.
+// Contenders that share it are listed in LDS where they fit, and the other digits are found among them; so a line is read three times: to count, to
+// list, and to write down what stays.
 template <int THREADS, int R, bool HELD>
 __global__ __launch_bounds__(THREADS) void sp_evict_select_kernel(EvictArgs a)
 {
@@ -189,7 +191,8 @@ __global__ __launch_bounds__(THREADS) void sp_evict_select_kernel(EvictArgs a)
     Found f = find_digit<THREADS>(bins, 0, want);
     const uint32_t top = f.digit;
     uint32_t least = top << 21;         // the least bits that stay, as far as their digits are known
-    // Whether all that share the known digits stay: then what stays is above `below`, and there are no ties to look at. (`least` is not 0 then: something is left behind.)
+    // Whether all that share the known digits stay: then what stays is above `below`, and there are no ties to look at. (`least` is not 0 then:
+    // something is left behind.)
     bool all = f.above + f.count == (uint32_t)want;
     uint32_t below = all ? least - 1 : 0;
     int more = 0;                       // of this wave, certain to stay
@@ -291,8 +294,9 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t c, float ratio)
     return (uint32_t)r;
 }
 
-// A slot's source is looked up by one thread, its bytes are moved by whole 16-byte pieces, neighbouring threads those of one token. Bound by HBM for many tokens: 16 requests
-// that keep 2048 to 8192 tokens of 8 heads of 128 in bf16, 544 MB read and written, take 107 us, 5.1 TB/s (a large copy 4.8 to 5.2).
+// A slot's source is looked up by one thread, its bytes are moved by whole 16-byte pieces, neighbouring threads those of one token. Bound by HBM
+// for many tokens: 16 requests that keep 2048 to 8192 tokens of 8 heads of 128 in bf16, 544 MB read and written, take 107 us, 5.1 TB/s (a large
+// copy 4.8 to 5.2).
 template <int D, int KIND>
 __global__ __launch_bounds__(kMoveThreads) void sp_evict_move_kernel(EvictArgs a)
 {

@@ -88,8 +88,8 @@ __device__ __forceinline__ void store4(const MatmulArgs &p, int64_t m, int64_t n
 
 __device__ __forceinline__ i32x8 operand(u32x4 x) { return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], 0, 0, 0, 0}; }
 
-// Up to four scale bytes of a row from group k on, as they lie there (at any address). For groups that the row does not have 0: with the other operand's, which are 0 too, a factor
-// of 2^-254, under which any codes vanish.
+// Up to four scale bytes of a row from group k on, as they lie there (at any address). For groups that the row does not have 0: with the other
+// operand's, which are 0 too, a factor of 2^-254, under which any codes vanish.
 __device__ __forceinline__ uint32_t scales4(const uint8_t *row, int64_t k, int64_t groups)
 {
     if (k + 4 <= groups) {
@@ -121,10 +121,10 @@ struct Scales16 {
     }
 };
 
-// Bound by reading the weights: one row by 32000 x 2048 (35 MB) 8 us, by 33000 x 8192 (144 MB) 36 us, 4.0 TB/s, past the caches 9 and 38 (with 64 neighbouring bytes for a
-// lane, loaded in four pieces, 13 and 55); by launching and one chain of loads where they are few (48 x 4096 x 4096, 9 MB: 8.4 us).
-// Sixteen weight rows and 16 MT activation rows a workgroup. Its waves take stretches of 512 elements of the rows in turn, four instructions of 128 (of a row a lane has
-// one group in each, so that a load takes 64 neighbouring bytes of sixteen rows), and add up in LDS.
+// Bound by reading the weights: one row by 32000 x 2048 (35 MB) 8 us, by 33000 x 8192 (144 MB) 36 us, 4.0 TB/s, past the caches 9 and 38 (with 64
+// neighbouring bytes for a lane, loaded in four pieces, 13 and 55); by launching and one chain of loads where they are few (48 x 4096 x 4096, 9 MB:
+// 8.4 us). Sixteen weight rows and 16 MT activation rows a workgroup. Its waves take stretches of 512 elements of the rows in turn, four
+// instructions of 128 (of a row a lane has one group in each, so that a load takes 64 neighbouring bytes of sixteen rows), and add up in LDS.
 template <bool BF16, int MT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void sp_mx4_few_kernel(MatmulArgs p)
 {
@@ -185,8 +185,8 @@ constexpr int kStep = 256;              // elements of a row that a tile takes a
 constexpr int kRowBytes = kStep / 2, kPieces = kRowBytes / 16, kStepGroups = kStep / kGroup;
 constexpr int64_t kMostTiledK = int64_t(1) << 22;       // offsets of a tile's rows fit 32 bits
 
-// 64 lanes x 16 bytes from base + off (each lane its own) straight into LDS from byte `to` on. asm, since the compiler would wait for all of them before it
-// reads anything else from LDS; the loop waits itself.
+// 64 lanes x 16 bytes from base + off (each lane its own) straight into LDS from byte `to` on. asm, since the compiler would wait for all of them
+// before it reads anything else from LDS; the loop waits itself.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds(const uint8_t *base, uint32_t off, uint32_t to)
@@ -231,10 +231,11 @@ struct Codes {
     }
 };
 
-// 8192 x 8192 x 4096 takes 172 to 195 us by the clock that the power leaves, 2.8 to 3.2 PFLOP/s, where the instructions alone run at 6.7 on random data and a large bf16 product
-// reaches 1.3. Copies without loads take 150, without products 136, without results 176: products, operands from LDS and tiles to LDS share the time, and the first operands of a step come after a
-// barrier. The next step's loads are requested behind the first products, whose issue they would hold up (181 to 174). Not kept: buffers for four steps, steps in another order for each workgroup,
-// 128 x 128 results a wave (the same or slower); operands requested across the barrier, which takes all registers (168, but 128 x 128 tiles 15.4 to 16.3).
+// 8192 x 8192 x 4096 takes 172 to 195 us by the clock that the power leaves, 2.8 to 3.2 PFLOP/s, where the instructions alone run at 6.7 on random
+// data and a large bf16 product reaches 1.3. Copies without loads take 150, without products 136, without results 176: products, operands from LDS
+// and tiles to LDS share the time, and the first operands of a step come after a barrier. The next step's loads are requested behind the first
+// products, whose issue they would hold up (181 to 174). Not kept: buffers for four steps, steps in another order for each workgroup, 128 x 128
+// results a wave (the same or slower); operands requested across the barrier, which takes all registers (168, but 128 x 128 tiles 15.4 to 16.3).
 template <bool BF16, int WM, int WN, int FM, int FN>
 __global__ __launch_bounds__(64 * WM * WN) void sp_mx4_tiled_kernel(MatmulArgs p)
 {
@@ -251,7 +252,8 @@ __global__ __launch_bounds__(64 * WM * WN) void sp_mx4_tiled_kernel(MatmulArgs p
     const int64_t row_bytes = p.K / 2, groups = p.K / kGroup;
     const int steps = (int)((p.K + kStep - 1) / kStep), rest = (int)(p.K % kStep);       // elements of the last step, 0: all
 
-    // this thread's pieces: row (of the activations, then of the weights) and place in it, swapped about so that sixteen lanes read sixteen places of 16 bytes
+    // this thread's pieces: row (of the activations, then of the weights) and place in it, swapped about so that sixteen lanes read sixteen places
+    // of 16 bytes
     const int most_m = (int)min(p.M - 1 - m0, (int64_t)T::TM), most_n = (int)min(p.N - 1 - n0, (int64_t)T::TN);
     uint32_t off[T::kLoads];
     const int slot = tid % kPieces, piece = slot ^ (tid / kPieces >> 1 & 7);
@@ -311,7 +313,8 @@ __global__ __launch_bounds__(64 * WM * WN) void sp_mx4_tiled_kernel(MatmulArgs p
         for (int i = 0; i < FM; ++i) sa[i] = *reinterpret_cast<const uint32_t *>(scale_lds + buf * T::kScales + (row_a + 32 * i) * kStepGroups + 4 * h);
 #pragma unroll
         for (int j = 0; j < FN; ++j) sw[j] = *reinterpret_cast<const uint32_t *>(scale_lds + buf * T::kScales + (row_w + 32 * j) * kStepGroups + 4 * h);
-        // codes are read one group of products ahead; the scheduling barriers keep them from being read later, or further ahead, for which there are no registers
+        // codes are read one group of products ahead; the scheduling barriers keep them from being read later, or further ahead, for which there
+        // are no registers
         Codes<FM, FN> even, odd;
         even.read(a, w, at[0]);
         odd.read(a, w, at[1]);
@@ -381,9 +384,10 @@ sp_status run(const MatmulArgs &p, hipStream_t st)
 {
     if (p.M <= 16) return few<BF16, 1>(p, st);
     if (p.M <= 32) return few<BF16, 2>(p, st);
-    // Tiles take as long however few they are (0.35 us for 128 elements of K), the workgroups for few rows as long as what they read from L2, by turns (us, few rows' and tiles'):
-    // 128 x 4096 x 4096 (32 tiles) 14.0 and 14.6, 700 x 300 x 4000 (18) 7.7 and 14.0; 384 x 2048 x 2048 (48) 10.4 and 9.4, 256 x 4096 x 4096 (64) 25 and 15, 632 x 2025 x 224 (80) 11.0 and 6.3.
-    // Large tiles need nearly one for each unit (us, of 128 x 128 and 256 x 256): 2048 x 4096 x 4096 (128 large ones) 33 and 39, 2560 x 4096 x 4096 (160) 47 and 40, 8192 x 8192 x 4096 235 and 184.
+    // Tiles take as long however few they are (0.35 us for 128 elements of K), the workgroups for few rows as long as what they read from L2, by
+    // turns (us, few rows' and tiles'): 128 x 4096 x 4096 (32 tiles) 14.0 and 14.6, 700 x 300 x 4000 (18) 7.7 and 14.0; 384 x 2048 x 2048 (48) 10.4
+    // and 9.4, 256 x 4096 x 4096 (64) 25 and 15, 632 x 2025 x 224 (80) 11.0 and 6.3. Large tiles need nearly one for each unit (us, of 128 x 128
+    // and 256 x 256): 2048 x 4096 x 4096 (128 large ones) 33 and 39, 2560 x 4096 x 4096 (160) 47 and 40, 8192 x 8192 x 4096 235 and 184.
     if (p.K <= kMostTiledK) {
         if (sp::ceil_div(p.M, 256) * sp::ceil_div(p.N, 256) >= 160) return tiled<BF16, 2, 4, 4, 2>(p, st);
         if (sp::ceil_div(p.M, 128) * sp::ceil_div(p.N, 128) >= 48) return tiled<BF16, 2, 2, 2, 2>(p, st);

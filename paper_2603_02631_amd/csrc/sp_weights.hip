@@ -2,18 +2,18 @@
 // of a token is the attention that it draws, Appendix A.1.1, there over all layers at once and here for one layer's cache).
 //
 //   w[b, h, j] = old + sum_{r, g} exp(scale <q[r, g], k[b, h, j]> - lse[r, g])
-// over the rows r that see key j and the query heads g of kv head h; lse is what sp_attend wrote. A key's weight is the sum over the rows of a kv head, so a wave
-// that holds a block of keys goes through the rows and no sum crosses workgroups: nothing is added atomically, the order is fixed by the lengths.
-// The products are Q K^T with a key in a lane column: a lane adds up its rows, and the lanes of a column meet once at the end. Keys are bf16 or become it, exactly; logits,
-// exponentials and sums are fp32.
+// over the rows r that see key j and the query heads g of kv head h; lse is what sp_attend wrote. A key's weight is the sum over the rows of a kv
+// head, so a wave that holds a block of keys goes through the rows and no sum crosses workgroups: nothing is added atomically, the order is fixed
+// by the lengths. The products are Q K^T with a key in a lane column: a lane adds up its rows, and the lanes of a column meet once at the end. Keys
+// are bf16 or become it, exactly; logits, exponentials and sums are fp32.
 #include "sp_context.hpp"
 
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-// Rows of a kv head that sp_weights_few_kernel takes at most: what a wave's tile holds. 12 rows of 16 contexts of 16000 tokens (8 heads of 64, MX4) take 23 us there and 33 in the other kernel, of 4 (8 of 128,
-// bf16) 32 and 30.
+// Rows of a kv head that sp_weights_few_kernel takes at most: what a wave's tile holds. 12 rows of 16 contexts of 16000 tokens (8 heads of 64, MX4)
+// take 23 us there and 33 in the other kernel, of 4 (8 of 128, bf16) 32 and 30.
 constexpr int kFewRows = 16;
 constexpr int kManyRows = 32;           // rows of a tile of sp_weights_many_kernel
 constexpr int64_t kUnits = 256;         // compute units
@@ -66,13 +66,14 @@ __device__ __forceinline__ float gather2(float x0, float x1)
     return __uint_as_float(__builtin_amdgcn_permlane32_swap(__float_as_uint(x0), __float_as_uint(x1), false, false)[0]);
 }
 
-// Requests of up to 16 rows a kv head (none too: their weights are what they were). A wave has its rows in registers and takes pairs of blocks of 32 tokens, one of
-// its workgroup's in turn, a pair ahead. After the products lane 16 g + c holds rows 4g .. 4g + 3 of a column's key. With at most four rows (LIVE = 1) only lanes of group 0
-// hold any, so four tiles of 16 keys are gathered into all lanes before the exponentials, with at most eight (LIVE = 2) two (48 contexts of MX4: 72 us without the
-// gathering, 66 with).
-// Bound by reading, and by starting: 48 contexts of 2048 to 65536 tokens, 8 kv heads of 64, 4 query heads each, MX4 (271 MB with old and new weights) take 66 us, 4.1 TB/s; 48 of
-// 16384 59, 4.5, and of E4M3 90, 5.0. A short line's workgroups are a chain of offsets, lengths, block table, keys for one or two pairs. Not kept: two pairs
-// ahead (66), the pairs of all lines in equal shares over the resident workgroups (72: finding a share's start takes longer than its lines' ends leave idle).
+// Requests of up to 16 rows a kv head (none too: their weights are what they were). A wave has its rows in registers and takes pairs of blocks of
+// 32 tokens, one of its workgroup's in turn, a pair ahead. After the products lane 16 g + c holds rows 4g .. 4g + 3 of a column's key. With at most
+// four rows (LIVE = 1) only lanes of group 0 hold any, so four tiles of 16 keys are gathered into all lanes before the exponentials, with at most
+// eight (LIVE = 2) two (48 contexts of MX4: 72 us without the gathering, 66 with).
+// Bound by reading, and by starting: 48 contexts of 2048 to 65536 tokens, 8 kv heads of 64, 4 query heads each, MX4 (271 MB with old and new
+// weights) take 66 us, 4.1 TB/s; 48 of 16384 59, 4.5, and of E4M3 90, 5.0. A short line's workgroups are a chain of offsets, lengths, block table,
+// keys for one or two pairs. Not kept: two pairs ahead (66), the pairs of all lines in equal shares over the resident workgroups (72: finding a
+// share's start takes longer than its lines' ends leave idle).
 template <int D, int KIND, int LIVE>
 __global__ __launch_bounds__(kThreads) void sp_weights_few_kernel(WeightArgs a)
 {
@@ -217,10 +218,11 @@ __global__ __launch_bounds__(kThreads) void sp_weights_few_kernel(WeightArgs a)
     }
 }
 
-// Requests with more rows: a wave holds 32 or 64 keys as bf16 and goes through tiles of 32 rows, which its workgroup brings to LDS, two buffers in turn. A block's E4M3
-// scale goes into the factor. R fours of waves have the same keys and take the tiles in turn; their sums are added in their order.
-// The last 64 of 32768 tokens, 16 heads over 8 of 128, bf16: 67 MB of keys in 25 us. One read of the keys (11 us) and four tiles of rows (9 us of products, and their exponentials) come
-// after each other in a wave; four waves a SIMD fill in for one another (two, with twice the keys each: 27 us; all rows in LDS and the keys streamed past them: 29).
+// Requests with more rows: a wave holds 32 or 64 keys as bf16 and goes through tiles of 32 rows, which its workgroup brings to LDS, two buffers in
+// turn. A block's E4M3 scale goes into the factor. R fours of waves have the same keys and take the tiles in turn; their sums are added in their
+// order. The last 64 of 32768 tokens, 16 heads over 8 of 128, bf16: 67 MB of keys in 25 us. One read of the keys (11 us) and four tiles of rows (9
+// us of products, and their exponentials) come after each other in a wave; four waves a SIMD fill in for one another (two, with twice the keys
+// each: 27 us; all rows in LDS and the keys streamed past them: 29).
 template <int D, int KIND, int R>
 __global__ __launch_bounds__(kThreads * R, 4) void sp_weights_many_kernel(WeightArgs a)
 {
@@ -450,9 +452,10 @@ extern "C" sp_status sp_attend_weights(const sp_cache_desc *desc, const void *q_
         tiles += n;
         longest_tiles = n > longest_tiles ? n : longest_tiles;
     }
-    // A workgroup goes through the tiles of its line's rows, 1.1 us each; several fours of waves share them. That pays where the longest line, and not the work of a compute unit, takes the
-    // time, and costs where there is work for all, since each four loads the keys. One, two, four fours in us, at one longest line a unit's work: 8192 rows by 8192 keys, 8 heads of 64 284, 182, 132; at half of
-    // it: 4096 rows, 8 of 128 160, 118, 128; at a quarter: 16 requests of 2048 rows by 2000 keys 142, 145, 160; few rows (128 by 32768, 8 of 128) 25, 32, 56.
+    // A workgroup goes through the tiles of its line's rows, 1.1 us each; several fours of waves share them. That pays where the longest line, and
+    // not the work of a compute unit, takes the time, and costs where there is work for all, since each four loads the keys. One, two, four fours
+    // in us, at one longest line a unit's work: 8192 rows by 8192 keys, 8 heads of 64 284, 182, 132; at half of it: 4096 rows, 8 of 128 160, 118,
+    // 128; at a quarter: 16 requests of 2048 rows by 2000 keys 142, 145, 160; few rows (128 by 32768, 8 of 128) 25, 32, 56.
     const int64_t unit = sp::ceil_div(max_len, 32 * many_blocks(desc->head_dim) * kWaves) * desc->n_kv_heads * tiles / kUnits;
     const int fours = tiles == 0 ? 0 : longest_tiles < 16 || 3 * longest_tiles < unit ? 1 : 4 * longest_tiles < 3 * unit ? 2 : 4;
     WeightArgs a{};
@@ -462,8 +465,9 @@ extern "C" sp_status sp_attend_weights(const sp_cache_desc *desc, const void *q_
     a.old = old_dev;
     a.weights = weights_dev;
     a.stride = weights_stride;
-    // Pairs of blocks of a wave: as many as leave two waves a SIMD, at most 8. One, two, four, eight of them in us: 65536 keys, 8 heads of 64, 10.6, 8.7, 9.0, 10.5; 16 times 16000 34, 26, 22, 20; 4 times
-    // 16000, 8 of 128, 43, 35, 32, 33; 48 of up to 65536 115, 74 to 81, 66, 67, and 138 with sixteen.
+    // Pairs of blocks of a wave: as many as leave two waves a SIMD, at most 8. One, two, four, eight of them in us: 65536 keys, 8 heads of 64,
+    // 10.6, 8.7, 9.0, 10.5; 16 times 16000 34, 26, 22, 20; 4 times 16000, 8 of 128, 43, 35, 32, 33; 48 of up to 65536 115, 74 to 81, 66, 67, and
+    // 138 with sixteen.
     const int64_t pairs = sp::ceil_div(max_len, 2 * kBlock) * B * desc->n_kv_heads;
     a.per = 1;
     while (a.per < 8 && pairs > (int64_t)a.per * 2048) a.per *= 2;
