@@ -218,6 +218,41 @@ def test_weights_and_eviction_far_into_a_pool():
         np.testing.assert_array_equal(moved, keys[tokens, h])
 
 
+@pytest.mark.parametrize("B,kv,most", [(40, 8, 2000), (20, 4, 2000), (6, 8, 2000)])
+@pytest.mark.parametrize("n", [1, 2])
+def test_weights_of_many_contexts(B, kv, most, n):
+    """As many pairs of blocks as make a wave take eight, four, two of them; contexts that end before, at and behind a pair's end."""
+    H, d, page = 2 * kv, 64, 64
+    g = torch.Generator(device=DEV).manual_seed(B)
+    lens = [0, 1, 63, 64, 65, most, *np.random.default_rng(B).integers(1, most, B).tolist()][:B]
+    width = -(-most // page)
+    pool = torch.randn(B * width, kv, page, d, generator=g, device=DEV).bfloat16()
+    table = torch.randperm(B * width, generator=g, device=DEV).to(torch.int32).view(B, width)
+    q = torch.randn(B * n, H, d, generator=g, device=DEV).bfloat16()
+    lse, old = torch.rand(B * n, H, generator=g, device=DEV) + 2, torch.rand(B, kv, most, generator=g, device=DEV)
+    w = torch.full_like(old, 7.5)
+    off = list(range(0, B * n + 1, n))
+    desc = sp.CacheDesc(H, kv, d, sp.SP_CACHE_BF16, B * width, page, kv * page * d, page * d, d)
+    sp.sp_attend_weights(desc, q, off, torch.tensor(off, device=DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), most, table, pool, None, d ** -0.5, lse, old, w)
+    for b, L in enumerate(lens):
+        assert bool((w[b, :, L:] == 7.5).all())
+        if not L:
+            continue
+        k = pool[table[b].long()].transpose(1, 2).reshape(-1, kv, d)[:L].double()
+        rows = q[b * n:(b + 1) * n].double().view(n, kv, 2, d)
+        for h in range(kv):
+            x = rows[:, h].reshape(-1, d) @ k[:, h].t().contiguous() * d ** -0.5
+            S = rows[:, h].reshape(-1, d).abs() @ k[:, h].t().contiguous().abs() * d ** -0.5
+            z = lse[b * n:(b + 1) * n, 2 * h:2 * h + 2].double().reshape(-1, 1)
+            sees = torch.arange(L, device=DEV)[None, :] <= L - n + torch.arange(n, device=DEV).repeat_interleave(2)[:, None]
+            p = torch.where(sees, torch.exp(x - z), 0.0)
+            before = torch.where(torch.arange(L, device=DEV) < L - n, old[b, h, :L].double(), 0.0)
+            want = before + p.sum(dim=0)
+            # as for the other contexts: a logit is off by (d + 4) 2^-24 S, what follows adds 2^-22 (|x| + |lse| + 1), the sum half a step for each of its terms
+            tol = (2 * p * ((d + 4) * 2.0 ** -24 * S + 2.0 ** -22 * (x.abs() + z.abs() + 1))).sum(dim=0) + (2 * n + 1) * 2.0 ** -24 * want
+            assert bool(((w[b, h, :L].double() - want).abs() <= tol).all()), (b, h)
+
+
 def test_a_projection_whose_codes_pass_two_gigabytes():
     """The last rows of a weight matrix of 2^31 bytes and more of codes, for few rows and for many."""
     K, N = 1 << 14, (1 << 18) + 40
