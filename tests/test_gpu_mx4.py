@@ -142,6 +142,27 @@ def test_far_scales_and_nan_rows(M, N):
     np.testing.assert_array_equal(np.isnan(got), nan)
 
 
+@pytest.mark.parametrize("M,N,K", [(1030, 2100, 288), (1030, 2100, 480), (3090, 4110, 96), (3090, 4110, 352)])
+def test_what_lies_behind_a_row_adds_nothing_to_tiles(M, N, K):
+    """A last step that is not full, with scales far apart, rows of zeros and rows that say NaN in their last group."""
+    a, sa, w, sw = operands(M, N, K, 8, spread=25)
+    a[::7], w[::5] = 0, 8                                                   # zeros of both signs
+    sa[11, -1] = 255
+    sw[N - 3, -1] = 255
+    got = product(a, sa, w, sw, False)
+    nan = np.zeros((M, N), dtype=bool)
+    nan[11], nan[:, N - 3] = True, True
+    np.testing.assert_array_equal(np.isnan(got), nan)
+    zero = np.zeros((M, N), dtype=bool)
+    zero[::7], zero[:, ::5] = True, True
+    assert (got[zero & ~nan] == 0).all()
+    sa[11, -1], sw[N - 3, -1] = 127, 127
+    keep = ~nan
+    x, y = mu.values(a, sa), mu.values(w, sw)
+    want, size = x @ y.T, np.abs(x) @ np.abs(y).T
+    assert (np.abs(got - want)[keep] <= (K * 2.0 ** -24 * size)[keep]).all()
+
+
 def test_extreme_scale_bytes():
     a, sa, w, sw = operands(5, 20, 64, 6)
     a[:], w[:] = 2, 2
