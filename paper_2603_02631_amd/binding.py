@@ -537,6 +537,13 @@ def _rows(t, what: str, rows: int, width: int, stride: Optional[int], known: set
     return t.data_ptr(), (strides[0] if rows > 1 else (width + 7) & ~7)
 
 
+def _rows_or_none(t, what: str, rows: int, width: int, stride: Optional[int], known: set):
+    """As _rows; without rows the stride is the given one, or a dense row's. A stride of 0 stays one, which the library refuses."""
+    if t is None:
+        return None, width if stride is None else stride
+    return _rows(t, what, rows, width, stride, known)
+
+
 def _table(block_table, B: int, table_stride: Optional[int], what: str = "block_table"):
     """(address, entries of a request) of a dense [B][table_stride] int32 block table."""
     if isinstance(block_table, int) or block_table is None:
@@ -645,11 +652,11 @@ def sp_logprobs(logits, n_rows: int, vocab: int, targets, n_top: int, logprob, e
         if not _BF16:
             _learn_types()
         dtype = SP_LOGITS_BF16 if logits.dtype in _BF16 else SP_LOGITS_F32        # which refuses what is neither
-    x, stride = _rows(logits, "logits", n_rows, vocab, row_stride, _FP32 if dtype == SP_LOGITS_F32 else _BF16)
+    x, stride = _rows_or_none(logits, "logits", n_rows, vocab, row_stride, _FP32 if dtype == SP_LOGITS_F32 else _BF16)
     n, k = max(n_rows, 0), max(n_top, 0)
     ws_at, ws_size = _workspace(ws, ws_bytes)
     status = (_lib or load_library()).sp_logprobs(
-        x, dtype, n_rows, vocab, stride or row_stride or vocab, _typed(targets, "targets", 4 * n, _INT32), n_top,
+        x, dtype, n_rows, vocab, stride, _typed(targets, "targets", 4 * n, _INT32), n_top,
         _typed(logprob, "logprob", 4 * n, _FP32), _typed(entropy, "entropy", 4 * n, _FP32), _typed(top_ids, "top_ids", 4 * n * k, _INT32),
         _typed(top_logprobs, "top_logprobs", 4 * n * k, _FP32), ws_at, ws_size, _stream(stream))
     if status:
@@ -723,9 +730,9 @@ def _float_kind(t, what: str, dtype: Optional[int]) -> int:
 
 def sp_mx4_quantise(x, rows: int, K: int, codes, scales, dtype: Optional[int] = None, row_stride: Optional[int] = None, stream=None) -> None:
     dtype = _float_kind(x, "x", dtype)
-    at, stride = _rows(x, "x", rows, K, row_stride, _FP32 if dtype == SP_LOGITS_F32 else _BF16)
+    at, stride = _rows_or_none(x, "x", rows, K, row_stride, _FP32 if dtype == SP_LOGITS_F32 else _BF16)
     n, k = max(rows, 0), max(K, 0)
-    status = (_lib or load_library()).sp_mx4_quantise(at, dtype, rows, K, stride or row_stride or K, _typed(codes, "codes", n * k // 2, _BYTES),
+    status = (_lib or load_library()).sp_mx4_quantise(at, dtype, rows, K, stride, _typed(codes, "codes", n * k // 2, _BYTES),
                                                       _typed(scales, "scales", n * (k // SP_MX4_GROUP), _BYTES), _stream(stream))
     if status:
         _check(status)
@@ -734,11 +741,11 @@ def sp_mx4_quantise(x, rows: int, K: int, codes, scales, dtype: Optional[int] = 
 def sp_mx4_matmul(a_codes, a_scales, M: int, w_codes, w_scales, N: int, K: int, out, dtype: Optional[int] = None,
                   out_stride: Optional[int] = None, stream=None) -> None:
     dtype = _float_kind(out, "out", dtype)
-    to, stride = _rows(out, "out", M, N, out_stride, _FP32 if dtype == SP_LOGITS_F32 else _BF16)
+    to, stride = _rows_or_none(out, "out", M, N, out_stride, _FP32 if dtype == SP_LOGITS_F32 else _BF16)
     m, n, k = max(M, 0), max(N, 0), max(K, 0)
     status = (_lib or load_library()).sp_mx4_matmul(
         _typed(a_codes, "a_codes", m * k // 2, _BYTES), _typed(a_scales, "a_scales", m * (k // SP_MX4_GROUP), _BYTES), M,
         _typed(w_codes, "w_codes", n * k // 2, _BYTES), _typed(w_scales, "w_scales", n * (k // SP_MX4_GROUP), _BYTES), N, K, to, dtype,
-        stride or out_stride or N, _stream(stream))
+        stride, _stream(stream))
     if status:
         _check(status)

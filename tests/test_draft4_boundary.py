@@ -247,6 +247,26 @@ def test_numbers_of_a_product_of_another_type_are_refused(fn, name):
             assert refused(1, fn, **{name: OnGpu(t), "dtype": given, ("row_stride" if name == "x" else "out_stride"): None}).startswith(name + " ")
 
 
+def logprobs(**kw):
+    a = dict(logits=FAKE, n_rows=3, vocab=96, targets=None, n_top=1, logprob=None, entropy=FAKE, top_ids=FAKE, top_logprobs=FAKE, ws=FAKE, dtype=sp.SP_LOGITS_F32,
+             ws_bytes=1 << 30, stream=0)
+    a.update(kw)
+    sp.sp_logprobs(**a)
+
+
+@pytest.mark.parametrize("fn,name,width", [(quantise, "x", 96), (matmul, "out", 5), (logprobs, "logits", 96)])
+def test_rows_that_lie_on_top_of_one_another_are_refused(fn, name, width):
+    """A row that was expanded holds one row's elements: no other stride may stand in for its 0, or rows behind it would be read or written."""
+    import torch
+    stride = "out_stride" if name == "out" else "row_stride"
+    for dtype, kind in ((torch.float32, sp.SP_LOGITS_F32), (torch.bfloat16, sp.SP_LOGITS_BF16)):
+        t = torch.zeros(1, width, dtype=dtype).expand(3, width)
+        for given in (None, 0):
+            assert "stride" in refused(1, fn, **{name: OnGpu(t), "dtype": kind, stride: given})
+        refused(1, fn, **{name: OnGpu(t), "dtype": kind, stride: width})
+    assert "stride" in refused(1, fn, **{stride: 0})
+
+
 def test_host_tensors_are_refused():
     import torch
     refused(1, weights, q=torch.zeros(4, 8, 64, dtype=torch.bfloat16))
