@@ -607,7 +607,7 @@ sp_status sp_attend_weights(const sp_cache_desc *desc, const void *q_dev, const 
  *     scales are powers of two, but for what falls among the subnormals;
  *   - kept_dev[b, h, i] (int32 [B][n_kv_heads][max_budget]): which token it was;
  *   - new_weights_dev[b, h, i] (optional, float [B][n_kv_heads][max_budget], not overlapping
- *     weights_dev): its weight.
+ *     weights_dev): its weight, bit for bit.
  * new_lens_dev[b] = n (int32, neither lens_dev nor budget_dev itself). Entries and slots at and
  * behind n are left as they were, but for the scale of the E4M3 block that holds slot n - 1.
  * Keys keep the rotation of their old position: new tokens go on from there (sp_cache_append's

@@ -46,13 +46,12 @@ struct Share {
     }
 };
 
-// Bits that order as the weights do (0 added: -0 counts as 0), and back.
+// Bits that order as the weights do (0 added: -0 counts as 0).
 __device__ __forceinline__ uint32_t ordered(float x)
 {
     const uint32_t u = __float_as_uint(x + 0.f);
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ float weight_of(uint32_t x) { return __uint_as_float(x & 0x80000000u ? x & 0x7fffffffu : ~x); }
 
 // A wave's stretch of a line's contenders, in order: R times 64 neighbours at a time, as their ordered bits. Stretches that have no more are read
 // once (HELD). Places without a token hold 0, which is below every weight (but for one NaN) and behind all tokens. R is small: code that is long
@@ -74,20 +73,24 @@ struct Stretch {
         }
     }
 
-    // f(the first of 64 tokens, this lane's bits) in the tokens' order, all lanes together
+    // f(the first of 64 tokens, this lane's bits, and its weight as it is) in the tokens' order, all lanes together
     template <class F>
     __device__ __forceinline__ void each(F f)
     {
         if constexpr (!HELD) load(first);
         for (int at = first; at < last; at += 64 * R) {
             uint32_t bits[R];
+            float weight[R];
 #pragma unroll
-            for (int r = 0; r < R; ++r) bits[r] = ordered(x[r]);
+            for (int r = 0; r < R; ++r) {
+                weight[r] = x[r];
+                bits[r] = ordered(x[r]);
+            }
             if constexpr (!HELD)
                 if (at + 64 * R < last) load(at + 64 * R);
 #pragma unroll
             for (int r = 0; r < R; ++r)
-                if (at + 64 * r < last) f(at + 64 * r, bits[r]);
+                if (at + 64 * r < last) f(at + 64 * r, bits[r], weight[r]);
         }
     }
 };
@@ -184,7 +187,7 @@ __global__ __launch_bounds__(THREADS) void sp_evict_select_kernel(EvictArgs a)
         __syncthreads();
     };
     clear();
-    mine.each([&](int, uint32_t x) { atomicAdd(&bins[x >> 21], 1u); });         // counts: their order changes nothing
+    mine.each([&](int, uint32_t x, float) { atomicAdd(&bins[x >> 21], 1u); });         // counts: their order changes nothing
     if (tid == 0) listed = 0;
     if (tid < kWaves) wave_equal[tid] = 0;
     __syncthreads();
@@ -197,10 +200,10 @@ __global__ __launch_bounds__(THREADS) void sp_evict_select_kernel(EvictArgs a)
     uint32_t below = all ? least - 1 : 0;
     int more = 0;                       // of this wave, certain to stay
     if (all) {
-        mine.each([&](int, uint32_t x) { more += __popcll(__ballot(x > below)); });
+        mine.each([&](int, uint32_t x, float) { more += __popcll(__ballot(x > below)); });
         if (lane == 0) wave_above[wave] = more;
     } else if (f.count <= kList) {
-        mine.each([&](int, uint32_t x) {
+        mine.each([&](int, uint32_t x, float) {
             more += __popcll(__ballot(x >> 21 > top));
             if (x >> 21 == top) {
                 const int at = atomicAdd(&listed, 1);       // in any order: they are only counted
@@ -232,7 +235,7 @@ __global__ __launch_bounds__(THREADS) void sp_evict_select_kernel(EvictArgs a)
             const int known = digit == 0 ? 21 : 10, shift = digit == 0 ? 10 : 0, values = digit == 0 ? 2047 : 1023;
             const uint32_t same = least >> known;
             clear();
-            mine.each([&](int, uint32_t x) {
+            mine.each([&](int, uint32_t x, float) {
                 if (x >> known == same) atomicAdd(&bins[x >> shift & values], 1u);
             });
             __syncthreads();
@@ -242,7 +245,7 @@ __global__ __launch_bounds__(THREADS) void sp_evict_select_kernel(EvictArgs a)
         all = f.above + f.count == (uint32_t)want;
         below = all ? least - 1 : least;
         int equal = 0;
-        mine.each([&](int, uint32_t x) {
+        mine.each([&](int, uint32_t x, float) {
             more += __popcll(__ballot(x > below));
             equal += __popcll(__ballot(x == least));        // looked at where not all of them stay
         });
@@ -260,25 +263,25 @@ __global__ __launch_bounds__(THREADS) void sp_evict_select_kernel(EvictArgs a)
             tied += wave_equal[v];
         }
     if (all) {
-        mine.each([&](int token, uint32_t x) {
+        mine.each([&](int token, uint32_t x, float weight) {
             const uint64_t up = __ballot(x > below);
             if (x > below) {
                 const uint32_t at = rank + rank_in(up);
                 kept[at] = token + lane;
-                if (out) out[at] = weight_of(x);
+                if (out) out[at] = weight;
             }
             rank += __popcll(up);
         });
         return;
     }
     const int ties = want - f.above;    // of the equal ones the first so many stay
-    mine.each([&](int token, uint32_t x) {
+    mine.each([&](int token, uint32_t x, float weight) {
         const uint64_t up = __ballot(x > least), eq = __ballot(x == least);
         const int e = min(tied + rank_in(eq), ties);
         if (x > least || (x == least && e < ties)) {
             const uint32_t at = rank + rank_in(up) + e;
             kept[at] = token + lane;
-            if (out) out[at] = weight_of(x);
+            if (out) out[at] = weight;
         }
         rank += __popcll(up);
         tied += __popcll(eq);

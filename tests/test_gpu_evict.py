@@ -379,6 +379,89 @@ def test_evict_orders_nan_and_infinity():
         np.testing.assert_array_equal(kept[0, 0], want)
 
 
+@pytest.mark.parametrize("L,m", [(40, 100), (300, 120), (3000, 2999), (6000, 700), (9000, 8999)])
+def test_evict_passes_weights_on_as_they_are(L, m):
+    """Bit for bit, whatever the selection takes them for: the sign of zero, and what a NaN carries."""
+    rng = np.random.default_rng(L)
+    w = (rng.integers(-3, 4, (1, 1, L)) / np.float32(2)).astype(np.float32)
+    bits = w.view(np.uint32)
+    bits[w == 0] = rng.choice(np.array([0, 1 << 31], dtype=np.uint32), int((w == 0).sum()))
+    at = rng.choice(L, 12, replace=False)
+    bits[0, 0, at[:8]] = [0x7FC00001, 0x7FC12345, 0x7F800001, 0x7FBFFFFF, 0x7FFFFFFE, 0x7F800000, 0x00000001, 0x80000001]
+    c, _, _, _ = filled("mx4", 2, 1, 64, [0], [L], 4096, spare=5)
+    free = [p for p in range(c.n_pages) if p not in c.table[0].tolist()]
+    dst = np.array([free[:-(-m // 4096)]], dtype=np.int32)
+    _, new_lens, kept, new_w = evict("mx4", c, 2, [L], [m], 4, 8, w, dst)
+    n = int(new_lens[0])
+    assert n == min(L, m)
+    np.testing.assert_array_equal(new_w[0, 0, :n].view(np.uint32), bits[0, 0, kept[0, 0, :n]])
+
+
+def by_bits(bits, lo, hi, want):
+    """The `want` largest of tokens lo .. hi - 1 as the order of weights has them: by their bits (NaN quiet, -0 as 0), negative ones reversed, ties to the earlier."""
+    u = bits.astype(np.uint64)
+    nan = (u & 0x7FFFFFFF) > 0x7F800000
+    u = np.where(nan, u | 0x400000, np.where(u == 0x80000000, 0, u))
+    key = np.where(u >> 31 == 1, 0xFFFFFFFF - u, u + 0x80000000).astype(np.int64)
+    return sorted(sorted(range(lo, hi), key=lambda j: (-key[j], j))[:want])
+
+
+@pytest.mark.parametrize("L,m,spread", [(6000, 5000, 900), (6000, 5990, 900), (9000, 4000, 6000), (9000, 8990, 6000), (3000, 2995, 400)])
+def test_evict_where_the_last_to_stay_is_nan(L, m, spread):
+    """Long lines of which many weights are the NaN below all numbers, whose bits are those of places without a token; with ties, and other NaNs among them."""
+    rng = np.random.default_rng(L + m)
+    w = rng.standard_normal((1, 1, L)).astype(np.float32)
+    bits = w.view(np.uint32)
+    at = rng.permutation(L)
+    bits[0, 0, at[:spread]] = 0xFFFFFFFF
+    bits[0, 0, at[spread:spread + 90]] = np.repeat(np.array([0xFFC00000, 0xFFFFFFFE, 0x7FC00000, 0x7FFFFFFF, 0xFF800000, 0x7F800000], dtype=np.uint32), 15)
+    c, _, _, _ = filled("mx4", 2, 1, 64, [0], [L], 4096, spare=8)
+    dst = np.array([[p for p in range(c.n_pages) if p not in c.table[0].tolist()][:-(-m // 4096)]], dtype=np.int32)
+    for sinks, recent in ((0, 0), (4, 32)):
+        _, _, kept, new_w = evict("mx4", c, 2, [L], [m], sinks, recent, w, dst)
+        stay = [*range(sinks), *by_bits(bits[0, 0], sinks, L - recent, m - sinks - recent), *range(L - recent, L)]
+        np.testing.assert_array_equal(kept[0, 0], stay)
+        np.testing.assert_array_equal(new_w[0, 0].view(np.uint32), bits[0, 0, stay])
+
+
+@pytest.mark.parametrize("scales", [[1.0, 2.0 ** -70, 2.0 ** 60, 2.0 ** -20], [0.0, 1.0, 0.0, 2.0], [0.0, 0.0, 0.0, 0.0], [np.nan, 1.0, 4.0, np.nan], [3.0, 0.7, 1.1, 2.9],
+                                    [2.0 ** -126, 2.0 ** 126, 1.0, 2.0 ** 120]])
+def test_evict_blocks_of_very_different_scales(scales):
+    """Blocks of E4M3 codes of every kind under scales that are far apart, zero, NaN or no powers of two, whose tokens meet in one block: the largest scale, and
+    E4M3 (code * (scale / s)), each step in float. Under a NaN all of a block is NaN."""
+    kv, d, page, L, m = 1, 64, 32, 256, 70
+    c, _, _, _ = filled("e4m3", 2, kv, d, [0], [L], page, spare=4)
+    rng = np.random.default_rng(7)
+    for pool in (c.k, c.v):
+        for j in range(L):
+            pool[c.at(0, 0, j):c.at(0, 0, j) + d] = rng.integers(0, 256, d)
+    for i in range(L // page):
+        c.ks[c.table[0, i], 0, 0], c.vs[c.table[0, i], 0, 0] = scales[i % 4], scales[(i + 1) % 4]
+    dst = np.array([[p for p in range(c.n_pages) if p not in c.table[0].tolist()][:3]], dtype=np.int32)
+    w = rng.random((1, kv, L)).astype(np.float32)
+    pools, _, kept, _ = evict("e4m3", c, 2, [L], [m], 0, 0, w, dst)
+    stay = kept[0, 0]
+    for pool, of, got, new in ((c.k, c.ks, pools[0], pools[2]), (c.v, c.vs, pools[1], pools[3])):
+        got, new = got.cpu().numpy(), new.cpu().numpy()
+        for i0 in range(0, m, 32):
+            block = stay[i0:i0 + 32]
+            old = np.array([of[c.table[0, j // page], 0, 0] for j in block], dtype=np.float32)
+            top = np.float32(np.nan) if np.isnan(old).any() else old.max()
+            np.testing.assert_array_equal(new[dst[0, i0 // page], 0, 0], top)
+            for i, j in enumerate(block):
+                to = int(dst[0, i0 // page]) * c.page_stride + i * c.stride_token
+                mine = got[to:to + d]
+                if np.isnan(top):
+                    continue
+                with np.errstate(under="ignore"):
+                    x = ou.E4M3[pool[c.at(0, 0, j):c.at(0, 0, j) + d]].astype(np.float32)
+                    y = x if old[i] == top else x * np.float32(old[i] / top)
+                want = ou.e4m3_codes(y.astype(np.float64))
+                nan = np.isnan(y)
+                np.testing.assert_array_equal(np.isnan(ou.E4M3[mine]), nan)
+                np.testing.assert_array_equal(mine[~nan], want[~nan])
+
+
 @pytest.mark.parametrize("L,m", [(40000, 9000), (70001, 70000), (65536, 64), (5000, 4097)])
 def test_evict_from_long_contexts(L, m):
     check_evict("mx4", 1, 64, [L, 3], [m, 2], 4, 32, page=4096)
