@@ -236,6 +236,40 @@ def test_weights_of_keys_behind_a_window_whose_pages_hold_anything(kind, n):
     assert torch.equal(got[0], got[1]) and torch.equal(got[1][..., :160], before[..., :160]) and not torch.equal(got[1], before)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n", [1, 4, 40])
+@pytest.mark.parametrize("where", ["query", "key"])
+def test_a_nan_that_a_row_sees_gets_into_the_weights(kind, n, where):
+    """With the lse of the attention itself: the row's is NaN then, and so is what it adds to. Nothing gets into the other request."""
+    H, kv, d, lens = 4, 2, 64, [100, 90]
+    c, held, off, q = filled(kind, H, kv, d, [n, n], lens, 32)
+    bits = ou.bf16_bits(q)
+    k, ks, vs = c.k.copy(), c.ks.copy(), c.vs.copy()
+    if where == "query":
+        bits[0, 3, 17] = 0x7FC0                         # a head of the second kv head
+    elif kind == "bf16":
+        k[c.at(0, 1, 20) + 5] = 0x7FC0
+    elif kind == "e4m3":
+        ks[c.table[0, 0], 1] = np.nan
+    else:
+        ks[c.table[0, 0], 1, 20, 1] = 255
+    desc, qd, top = desc_of(c, H, kind), dev(bits), dev(np.asarray(lens, dtype=np.int32))
+    args = (qd, off.tolist(), dev(off), top, 100, dev(c.table))
+    scales = (dev(ks), dev(vs)) if kind != "bf16" else (None, None)
+    kd, out, lse = dev(k), torch.empty(2 * n, H, d, dtype=torch.bfloat16, device=DEV), torch.empty(2 * n, H, device=DEV)
+    ws = torch.empty(max(256, sp.sp_attend_workspace(desc, off.tolist(), 2, 100)), dtype=torch.uint8, device=DEV)
+    sp.sp_attend(desc, *args, kd, dev(c.v), *scales, 0.125, out, lse, ws)
+    assert torch.isnan(lse[0, 3]).item() and bool(torch.isfinite(lse[n:]).all())
+    w = torch.full((2, kv, 100), 7.5, device=DEV)
+    sp.sp_attend_weights(desc, *args, kd, scales[0], 0.125, lse, None, w)
+    got = w.cpu().numpy()
+    assert np.isnan(got[0, 1, :101 - n]).all() and np.isfinite(got[1]).all()
+    if where == "key":                                  # with another lse the key's own weight still says so
+        sp.sp_attend_weights(desc, *args, kd, scales[0], 0.125, torch.zeros_like(lse), None, w)
+        got = w.cpu().numpy()
+        assert np.isnan(got[0, 1, 20]) and np.isfinite(got[1]).all()
+
+
 # ---- eviction --------------------------------------------------------------------------------------------------------
 
 def choice(w, L, m, sinks, recent):

@@ -163,6 +163,40 @@ def test_what_lies_behind_a_row_adds_nothing_to_tiles(M, N, K):
     assert (np.abs(got - want)[keep] <= (K * 2.0 ** -24 * size)[keep]).all()
 
 
+@pytest.mark.parametrize("M,N", [(5, 20), (24, 40), (40, 72), (1030, 1100), (3090, 4110)])
+@pytest.mark.parametrize("small", [18, 20, 22, 23])
+def test_products_far_below_another_one_are_not_dropped(M, N, small):
+    """One product of 1, in another group of 32 for every row, and products of 2^-small everywhere else of its row: whatever order they are added in, every
+    partial sum is a multiple of 2^-23 below 2, which fp32 holds, so the result is exact."""
+    K = 512
+    a, w = np.full((M, K), 2, dtype=np.uint8), np.full((N, K), 2, dtype=np.uint8)
+    sa, sw = np.full((M, K // 32), 127 - small, dtype=np.uint8), np.full((N, K // 32), 127, dtype=np.uint8)
+    for m in range(M):
+        g = m % (K // 32)
+        sa[m, g] = 127
+        a[m, 32 * g:32 * g + 32] = 0
+        a[m, 32 * g + 7 * m % 32] = 2 if m % 3 else 10
+    want = np.where(np.arange(M) % 3, 1.0, -1.0) + (K - 32) * 2.0 ** -small
+    np.testing.assert_array_equal(product(a, sa, w, sw, False), np.broadcast_to(want[:, None], (M, N)))
+
+
+@pytest.mark.parametrize("M,N", [(3, 20), (20, 20), (40, 70), (700, 1000)])
+def test_rows_longer_than_tiles_take(M, N):
+    """K just above 2^22: more tiles than few rows have, and still the kernel of few rows; a few elements of a row are not zero, the last ones among them."""
+    K = (1 << 22) + 32
+    rng = np.random.default_rng(M)
+    at = np.unique(np.concatenate([rng.integers(0, K // 2, 60), [0, (1 << 21) - 1, 1 << 21, K // 2 - 1]]))         # bytes
+    dense = []
+    for n in (M, N):
+        codes = torch.zeros(n, K // 2, dtype=torch.uint8, device=DEV)
+        some = rng.integers(0, 256, (n, at.size)).astype(np.uint8)
+        codes[:, torch.from_numpy(at).to(DEV)] = torch.from_numpy(some).to(DEV)
+        dense.append((codes, torch.full((n, K // 32), 127, dtype=torch.uint8, device=DEV), mu.VALUES[mu.unpack(some)]))
+    out = torch.empty(M, N, device=DEV)
+    sp.sp_mx4_matmul(dense[0][0], dense[0][1], M, dense[1][0], dense[1][1], N, K, out)
+    np.testing.assert_array_equal(out.cpu().numpy(), dense[0][2] @ dense[1][2].T)                                # quarters below 2^14: exact
+
+
 def test_extreme_scale_bytes():
     a, sa, w, sw = operands(5, 20, 64, 6)
     a[:], w[:] = 2, 2
