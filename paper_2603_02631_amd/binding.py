@@ -663,7 +663,7 @@ def sp_logprobs(logits, n_rows: int, vocab: int, targets, n_top: int, logprob, e
         _check(status)
 
 
-def _line_stride(t, what: str, lines: int, width: int, stride: Optional[int]) -> int:
+def _line_stride(t, what: str, width: int, stride: Optional[int]) -> int:
     """Entries of a (request, kv head) line of a dense [requests][kv heads][entries] array."""
     if stride is not None:
         return stride
@@ -682,8 +682,8 @@ def sp_attend_weights(desc: CacheDesc, q, offsets_host, offsets_dev, lens, max_l
     T = off[B] if B >= 0 and off[B] > 0 else 0
     tab, width = _table(block_table, B, table_stride)
     H, kv, d, elems, of_scales, pool, scales = _cache_bytes(desc)
-    entries = _line_stride(weights, "weights", B * kv, max_len, weights_stride)
-    if old is not None and entries != _line_stride(old, "old", B * kv, max_len, weights_stride):
+    entries = _line_stride(weights, "weights", max_len, weights_stride)
+    if old is not None and entries != _line_stride(old, "old", max_len, weights_stride):
         raise SpError(1, "old and weights differ in shape")
     size = 4 * B * kv * max(entries, 0)
     status = (_lib or load_library()).sp_attend_weights(
@@ -706,7 +706,7 @@ def sp_cache_evict(desc: CacheDesc, lens, max_len: int, budget, max_budget: int,
     tab, width = _table(block_table, n, table_stride)
     dst, dst_width = _table(dst_table, n, dst_stride, "dst_table")
     _, kv, _, elems, of_scales, pool, scales = _cache_bytes(desc)
-    entries = _line_stride(weights, "weights", n * kv, max_len, weights_stride)
+    entries = _line_stride(weights, "weights", max_len, weights_stride)
     held = 4 * n * kv * max(max_budget, 0)
     status = (_lib or load_library()).sp_cache_evict(
         ctypes.byref(desc), B, _typed(lens, "lens", 4 * n, _INT32), max_len, _typed(budget, "budget", 4 * n, _INT32), max_budget, sinks, recent,

@@ -1,5 +1,5 @@
-// The paged cache as the kernels see it, and the host's checks of what describes it: shared by sp_cache_append and
-// sp_attend.
+// The paged cache as the kernels see it, and the host's checks of what describes it: shared by the calls that fill, read
+// and thin out a cache.
 #pragma once
 
 #include "sp_common.hpp"

@@ -22,7 +22,8 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
     return __builtin_bit_cast(uint32_t, r);
 }
 
-// Four neighbouring lanes have a group, eight elements each. Bound by HBM: 8192 rows of 4096 in bf16, 85 MB read and written, 18 us, 4.7 TB/s.
+// Four neighbouring lanes have a group, eight elements each. Bound by HBM: 8192 rows of 4096 in bf16, 85 MB read and written, 18 us, 4.7 TB/s, in fp32
+// 26 us, 5.8 TB/s (three inputs in turn).
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void sp_mx4_quantise_kernel(const void *x, int64_t octets, int64_t row_octets, int64_t row_stride, uint32_t *codes,
                                                                     uint8_t *scales)
@@ -125,17 +126,18 @@ struct Scales16 {
 // neighbouring bytes for a lane, loaded in four pieces, 13 and 55); by launching and one chain of loads where they are few (48 x 4096 x 4096, 9 MB:
 // 8.4 us). Sixteen weight rows and 16 MT activation rows a workgroup. Its waves take stretches of 512 elements of the rows in turn, four
 // instructions of 128 (of a row a lane has one group in each, so that a load takes 64 neighbouring bytes of sixteen rows), and add up in LDS.
-template <bool BF16, int MT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void sp_mx4_few_kernel(MatmulArgs p)
+template <bool BF16, int MT>
+__global__ __launch_bounds__(kThreads) void sp_mx4_few_kernel(MatmulArgs p)
 {
-    __shared__ f32x4 part[WAVES][MT][64];
+    constexpr int kWaves = kThreads / 64;
+    __shared__ f32x4 part[kWaves][MT][64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
     const int64_t m0 = (int64_t)(blockIdx.x / p.tiles_n) * 16 * MT, n0 = (int64_t)(blockIdx.x % p.tiles_n) * 16, groups = p.K / kGroup;
     const int64_t n = min(n0 + c, p.N - 1);
     f32x4 acc[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int64_t k = 16 * wave; k < groups; k += 16 * WAVES) {
+    for (int64_t k = 16 * wave; k < groups; k += 16 * kWaves) {
         const u32x4 *w = reinterpret_cast<const u32x4 *>(p.w) + n * groups + k + g;
         u32x4 u[4];
 #pragma unroll
@@ -162,18 +164,13 @@ __global__ __launch_bounds__(64 * WAVES) void sp_mx4_few_kernel(MatmulArgs p)
                 acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(u[s]), operand(v[s]), acc[t], 4, 4, 0, (int)su.w[s], 0, (int)sv.w[s]);
         }
     }
-    if (WAVES > 1) {
 #pragma unroll
-        for (int t = 0; t < MT; ++t) part[wave][t][lane] = acc[t];
-        __syncthreads();
-    }
-    for (int t = wave; t < MT; t += WAVES) {
-        f32x4 y = acc[0];
-        if (WAVES > 1) {
-            y = part[0][t][lane];
+    for (int t = 0; t < MT; ++t) part[wave][t][lane] = acc[t];
+    __syncthreads();
+    for (int t = wave; t < MT; t += kWaves) {
+        f32x4 y = part[0][t][lane];
 #pragma unroll
-            for (int v = 1; v < WAVES; ++v) y += part[v][t][lane];
-        }
+        for (int v = 1; v < kWaves; ++v) y += part[v][t][lane];
         const int64_t m = m0 + 16 * t + c;
         if (m < p.M) store4<BF16>(p, m, n0 + 4 * g, y);
     }
@@ -231,8 +228,8 @@ struct Codes {
     }
 };
 
-// 8192 x 8192 x 4096 takes 172 to 195 us by the clock that the power leaves, 2.8 to 3.2 PFLOP/s, where the instructions alone run at 6.7 on random
-// data and a large bf16 product reaches 1.3. Copies without loads take 150, without products 136, without results 176: products, operands from LDS
+// 8192 x 8192 x 4096 takes 172 to 195 us by the clock that the power leaves (calls behind each other, by events; the first ten after a pause 215 to
+// 228, as in a profile), 2.8 to 3.2 PFLOP/s, where the instructions alone run at 6.7 on random data and a large bf16 product reaches 1.3. Copies without loads take 150, without products 136, without results 176: products, operands from LDS
 // and tiles to LDS share the time, and the first operands of a step come after a barrier. The next step's loads are requested behind the first
 // products, whose issue they would hold up (181 to 174). Not kept: buffers for four steps, steps in another order for each workgroup, 128 x 128
 // results a wave (the same or slower); operands requested across the barrier, which takes all registers (168, but 128 x 128 tiles 15.4 to 16.3).
@@ -374,7 +371,7 @@ sp_status few(MatmulArgs p, hipStream_t st)
 {
     p.tiles_m = (int32_t)sp::ceil_div(p.M, 16 * MT);
     p.tiles_n = (int32_t)sp::ceil_div(p.N, 16);
-    hipLaunchKernelGGL((sp_mx4_few_kernel<BF16, MT, 4>), dim3((unsigned)((int64_t)p.tiles_m * p.tiles_n)), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((sp_mx4_few_kernel<BF16, MT>), dim3((unsigned)((int64_t)p.tiles_m * p.tiles_n)), dim3(kThreads), 0, st, p);
     SP_HIP_CHECK(hipGetLastError());
     return SP_OK;
 }
@@ -387,7 +384,9 @@ sp_status run(const MatmulArgs &p, hipStream_t st)
     // Tiles take as long however few they are (0.35 us for 128 elements of K), the workgroups for few rows as long as what they read from L2, by
     // turns (us, few rows' and tiles'): 128 x 4096 x 4096 (32 tiles) 14.0 and 14.6, 700 x 300 x 4000 (18) 7.7 and 14.0; 384 x 2048 x 2048 (48) 10.4
     // and 9.4, 256 x 4096 x 4096 (64) 25 and 15, 632 x 2025 x 224 (80) 11.0 and 6.3. Large tiles need nearly one for each unit (us, of 128 x 128
-    // and 256 x 256): 2048 x 4096 x 4096 (128 large ones) 33 and 39, 2560 x 4096 x 4096 (160) 47 and 40, 8192 x 8192 x 4096 235 and 184.
+    // and 256 x 256): 2048 x 4096 x 4096 (128 large ones) 33 and 39, 2560 x 4096 x 4096 (160) 47 and 40, 8192 x 8192 x 4096 235 and 184. Of up to 128 rows
+    // half a large tile and more is rows that are not there, and still they are near: 128 x 40960 x 4096 (160) 42 and 39, 48 x 40960 x 4096 33 and
+    // 34, 128 x 128256 x 4096 (501) 90 and 93, 48 x 128256 x 4096 79 and 85, but 48 x 65536 x 2048 (256) 16 and 21 (few rows' workgroups 50 to 360).
     if (p.K <= kMostTiledK) {
         if (sp::ceil_div(p.M, 256) * sp::ceil_div(p.N, 256) >= 160) return tiled<BF16, 2, 4, 4, 2>(p, st);
         if (sp::ceil_div(p.M, 128) * sp::ceil_div(p.N, 128) >= 48) return tiled<BF16, 2, 2, 2, 2>(p, st);
